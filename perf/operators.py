@@ -100,7 +100,7 @@ def draw(rng):
         return {"kind": kind, "rows": rows, "vocab": vocab, "mix": rng.choice(["usual", "each", "plain"]),
                 "masked": rng.choice([0.0, 0.0, rng.uniform(0.1, 0.99)])}
     Hq, Hkv = rng.choice(_HEADS)
-    case = {"kind": kind, "heads": Hq, "kv_heads": Hkv, "page": 2 ** rng.randint(3, 8),
+    case = {"kind": kind, "heads": Hq, "kv_heads": Hkv, "page": 2 ** rng.randint(4, 8),
             "slot_major": rng.random() < 0.3, "pad": rng.choice([0, 0, rng.randint(1, 40)])}
     if kind == "append":
         B = _log_int(rng, 1, 64)
