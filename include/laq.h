@@ -521,6 +521,131 @@ laq_status laq_decode_attention_qkv_f16(const void *qkv, const void *q_norm_weig
  * MISALIGNED. */
 laq_status laq_silu_mul_f16(const void *gate_up, void *y, int64_t M, int64_t I, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Batched serving: several sequences at once, each with its keys and values
+ * in pages of a common cache, and the choice of the next tokens.  fp16 in and
+ * out, fp32 sums and softmax statistics, deterministic.  Head dimension 128.
+ * Same conventions as above.
+ * ------------------------------------------------------------------------ */
+
+/* laq_paged_batch -- the rows of one step and where their caches lie.
+ *
+ * Sequence b (of B) owns rows token_start[b] .. token_start[b + 1] - 1 of the
+ * step's T rows (one row when it decodes, many in a prompt's chunk, none when
+ * it waits); they are the LAST of its seq_len[b] positions, so its row i has
+ * position seq_len[b] - (token_start[b + 1] - token_start[b]) + i.  Position
+ * t's key of key/value head g is the 128 fp16 values at
+ *   k_pages + page_table[b * table_stride + t / page_size] * page_stride
+ *           + g * head_stride + (t % page_size) * slot_stride    (elements)
+ * and its value is at the same place of v_pages.  Pages may lie anywhere, in
+ * any order, and be shared by sequences that only read them.
+ *
+ * page_table, token_start and seq_len are DEVICE arrays that the host does not
+ * read: a captured graph follows their contents.  token_start must not
+ * decrease.  Rows below token_start[0] or from token_start[B] on belong to no
+ * sequence: their outputs are left as they were.  What the arrays hold is
+ * checked on the device: a page number outside 0..num_pages-1 (-1, say, for a
+ * page that was given back) is a page that is not there, positions from
+ * table_pages * page_size on do not exist.
+ */
+typedef struct laq_paged_batch {
+    void *k_pages;              /* fp16, 16-byte aligned */
+    void *v_pages;              /* fp16, 16-byte aligned */
+    const int32_t *page_table;  /* [B] rows of table_pages entries */
+    const int32_t *token_start; /* [B + 1] */
+    const int32_t *seq_len;     /* [B] */
+    int64_t num_pages;          /* pages of the cache, >= 1 */
+    int64_t page_size;          /* positions per page: a power of two, 16..2^20 */
+    int64_t page_stride;        /* elements between pages, a multiple of 8 */
+    int64_t head_stride;        /* between key/value heads, a multiple of 8 */
+    int64_t slot_stride;        /* between positions, a multiple of 8, <= 2^26 */
+    int64_t table_pages;        /* entries of a table row; x page_size <= 2^30 */
+    int64_t table_stride;       /* elements between table rows, >= table_pages */
+    int64_t B;                  /* sequences, 0..2^20 */
+    int64_t T;                  /* rows, padding included; T * Hq <= 2^30 */
+} laq_paged_batch;
+
+/* laq_paged_append_f16 -- laq_qk_norm_rope_f16 for every row of a batch: row
+ * r's projection output qkv[r] fp16 [(Hq + 2*Hkv) * 128] (q heads, k heads, v
+ * heads), its q and k heads RMS-normalized with q_norm_weight / k_norm_weight
+ * (fp16 [128], either may be NULL: those heads are not normalized), rotated
+ * by row pos of cos_sin (fp32 [rope_rows][128], as for laq_qk_norm_rope_f16)
+ * at the row's position pos and rounded to fp16.  q goes to q_out fp16
+ * [T][Hq][128], k and v to the row's place in the pages.
+ *   qkv_stride  elements between rows, >= (Hq + 2*Hkv) * 128, multiple of 8.
+ * A row whose position lies outside the rotation table or the page table
+ * leaves q zero and appends nothing; one whose page is not there appends
+ * nothing.  Two rows of a call must not name the same place in the pages.
+ * B == 0 or T == 0: nothing is done.
+ * Errors: NULL_POINTER; BAD_SHAPE (sizes above, head_dim != 128, Hq not a
+ * multiple of Hkv, Hq > 4096, bad eps); MISALIGNED (fp16 arrays 16-byte,
+ * cos_sin and the batch's arrays 4-byte, strides). */
+laq_status laq_paged_append_f16(const laq_paged_batch *batch, const void *qkv, int64_t qkv_stride,
+                                const void *q_norm_weight, const void *k_norm_weight, const float *cos_sin,
+                                int64_t rope_rows, int64_t Hq, int64_t Hkv, int64_t head_dim, float eps,
+                                void *q_out, void *stream);
+
+/* laq_paged_attention_workspace_bytes -- workspace (bytes) with which
+ * laq_paged_attention_f16 runs a batch of B sequences and T rows whatever
+ * their lengths, capacity = table_pages * page_size; at most 68 MB.  0 when the call needs
+ * none, and for invalid sizes. */
+int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+
+/* laq_paged_attention_f16 -- causal attention of every row of a batch over
+ * its sequence's pages, its own position included (append first): query head
+ * h of the row at position p reads key/value head h / (Hq / Hkv),
+ *   out[r][h] = sum_t softmax_t(q[r][h] . k[t] / sqrt(128)) v[t]
+ * over the positions t <= p (and t > p - window, when window > 0) whose page
+ * is there; zeros when there are none.  q and out fp16 [T][Hq][128].
+ * Whatever positions that a row does not see hold (infinities and NaN too)
+ * does not change that row.
+ * Probabilities of batches with more than 16 / (Hq / Hkv) rows a sequence on
+ * average are rounded to fp16 (half a step, 2^-11 of each) before they weigh
+ * the values; sums and denominators are fp32.
+ * One or two kernels: items of at most 128 query rows and a range of
+ * positions, and where a sequence's positions are split, the joining of its
+ * ranges in position order.  The split follows the lengths on the device.
+ *   workspace  [scratch] device memory, 16-byte aligned, any contents, at
+ *              least laq_paged_attention_workspace_bytes(B, T, Hq, Hkv,
+ *              table_pages * page_size) bytes; may be NULL when that is 0.
+ *              Calls in flight need separate workspaces.
+ * B == 0 or T == 0: nothing is done.
+ * Errors: NULL_POINTER; BAD_SHAPE (sizes above, head_dim != 128, Hq not a
+ * multiple of Hkv, Hq > 4096, window outside 0..2^30, workspace too small);
+ * MISALIGNED. */
+laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, int64_t Hq, int64_t Hkv,
+                                   int64_t head_dim, int64_t window, void *out, void *workspace,
+                                   int64_t workspace_bytes, void *stream);
+
+/* laq_sample_f16 -- draws one token per row from logits fp16 [rows][V]
+ * (logits_stride elements between rows, >= V), each row with its own settings
+ * and its own uniform number u.  With the tokens ordered by logit, largest
+ * first and equal ones by index, and weights w = exp((logit - largest) /
+ * temperature):
+ *   top_k[r] > 0     keeps the first top_k tokens;
+ *   top_p[r] < 1     keeps, of those, the shortest prefix whose weight is at
+ *                    least top_p times theirs (one token at least);
+ *   min_p[r] > 0     keeps the tokens with w >= min(min_p, 1);
+ * all three leave a prefix of the order, and the shortest is kept.  token[r]
+ * is the first of its tokens at which the running weight passes u[r] times
+ * its weight, prob[r] that token's share of it.
+ *   temperature <= 0 (or NaN): the largest logit, the first of equal ones,
+ *                    prob 1.  NULL: 1.
+ *   top_k, top_p, min_p  NULL: off; top_k <= 0, top_p >= 1 or NaN, min_p <= 0
+ *                    or NaN: off for that row.
+ *   u [in] fp32 [rows] in [0, 1); NaN and smaller ones count as 0, and from
+ *                    1 on it is the last token kept.
+ * NaN logits count as -inf, and a token of -inf is never drawn; a row with
+ * nothing else gives token -1 and prob 0.  Weights and sums are fp64.
+ *   token [out] int32 [rows].  prob [out] fp32 [rows], or NULL.
+ * rows == 0: nothing is done.
+ * Errors: NULL_POINTER (logits, u, token); BAD_SHAPE (V outside 1..2^24, rows
+ * < 0 or >= 2^31, logits_stride below V or above 2^32); MISALIGNED (logits
+ * 2-byte, the others 4-byte). */
+laq_status laq_sample_f16(const void *logits, int64_t logits_stride, int64_t rows, int64_t V, const float *u,
+                          const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                          int32_t *token, float *prob, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

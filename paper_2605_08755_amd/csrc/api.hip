@@ -544,6 +544,149 @@ laq_status laq_silu_mul_f16(const void* gate_up, void* y, int64_t M, int64_t I, 
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
+// Batched serving: paged caches, sampling
+// ---------------------------------------------------------------------------
+namespace {
+
+bool finite_eps(float eps) { return eps >= 0.0f && eps < INFINITY; }
+
+// Checks a batch's sizes (no pointers: an empty batch may have none).
+laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int64_t Hkv, int64_t head_dim) {
+  if (!b) return fail(LAQ_ERR_NULL_POINTER, fn, "null batch");
+  if (head_dim != kHeadDimAbi) return fail(LAQ_ERR_BAD_SHAPE, fn, "head_dim must be 128");
+  if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "Hq must be a positive multiple of Hkv, at most 4096");
+  if (b->B < 0 || b->B > (1 << 20) || b->T < 0 || b->T > (1LL << 30) || b->T * Hq > (1LL << 30))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= B <= 2^20 and 0 <= T, T * Hq <= 2^30");
+  if (b->page_size < 16 || b->page_size > (1 << 20) || (b->page_size & (b->page_size - 1)) != 0)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "page_size must be a power of two from 16 to 2^20");
+  if (b->num_pages < 1 || b->num_pages > 0x7FFFFFFFLL) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= num_pages < 2^31");
+  if (b->table_pages < 1 || b->table_pages > (1LL << 30) / b->page_size)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= table_pages and table_pages * page_size <= 2^30");
+  if (b->table_stride < b->table_pages && b->B > 1)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "table_stride must be at least table_pages");
+  if (b->table_stride < 0 || b->table_stride > (1LL << 40)) return fail(LAQ_ERR_BAD_SHAPE, fn, "table_stride must be in 0..2^40");
+  if (b->slot_stride < kHeadDimAbi || b->slot_stride > (1 << 26) || b->head_stride < kHeadDimAbi ||
+      b->head_stride > (1LL << 40) || b->page_stride < kHeadDimAbi || b->page_stride > (1LL << 40))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be at least 128 (slots at most 2^26, heads and pages 2^40)");
+  if (b->slot_stride % 8 != 0 || b->head_stride % 8 != 0 || b->page_stride % 8 != 0)
+    return fail(LAQ_ERR_MISALIGNED, fn, "strides must be multiples of 8 elements");
+  return LAQ_OK;
+}
+
+laq_status check_batch_pointers(const char* fn, const laq_paged_batch* b) {
+  if (!b->k_pages || !b->v_pages || !b->page_table || !b->token_start || !b->seq_len)
+    return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer in the batch");
+  if (!aligned(b->k_pages, 16) || !aligned(b->v_pages, 16) || !aligned(b->page_table, 4) ||
+      !aligned(b->token_start, 4) || !aligned(b->seq_len, 4))
+    return fail(LAQ_ERR_MISALIGNED, fn, "pages must be 16-byte, page_table, token_start and seq_len 4-byte aligned");
+  return LAQ_OK;
+}
+
+laq::PagedBatch internal_batch(const laq_paged_batch& b) {
+  laq::PagedBatch p;
+  p.k = static_cast<uint16_t*>(b.k_pages);
+  p.v = static_cast<uint16_t*>(b.v_pages);
+  p.page_table = b.page_table;
+  p.token_start = b.token_start;
+  p.seq_len = b.seq_len;
+  p.page_stride = b.page_stride;
+  p.head_stride = b.head_stride;
+  p.table_stride = b.table_stride;
+  p.slot_stride = (int)b.slot_stride;
+  p.page_shift = __builtin_ctzll((unsigned long long)b.page_size);
+  p.num_pages = (int)b.num_pages;
+  p.table_pages = (int)b.table_pages;
+  p.B = (int)b.B;
+  p.T = (int)b.T;
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+laq_status laq_paged_append_f16(const laq_paged_batch* batch, const void* qkv, int64_t qkv_stride,
+                                const void* q_norm_weight, const void* k_norm_weight, const float* cos_sin,
+                                int64_t rope_rows, int64_t Hq, int64_t Hkv, int64_t head_dim, float eps, void* q_out,
+                                void* stream) {
+  const char* fn = "laq_paged_append_f16";
+  const laq::LaunchEvents ev = take_events();
+  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim);
+  if (st != LAQ_OK) return st;
+  if (rope_rows < 1 || rope_rows > (1LL << 31)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= rope_rows <= 2^31");
+  if (qkv_stride < (Hq + 2 * Hkv) * head_dim || qkv_stride > (1LL << 40))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "qkv_stride must be at least (Hq + 2 Hkv) * 128");
+  if (qkv_stride % 8 != 0) return fail(LAQ_ERR_MISALIGNED, fn, "qkv_stride must be a multiple of 8 elements");
+  if (!finite_eps(eps)) return fail(LAQ_ERR_BAD_SHAPE, fn, "eps must be finite and >= 0");
+  if (batch->B == 0 || batch->T == 0) return ok();
+  if (!qkv || !cos_sin || !q_out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
+  if (!aligned(qkv, 16) || !aligned(q_norm_weight, 16) || !aligned(k_norm_weight, 16) || !aligned(cos_sin, 4) ||
+      !aligned(q_out, 16))
+    return fail(LAQ_ERR_MISALIGNED, fn, "cos_sin must be 4-byte, fp16 arrays 16-byte aligned");
+  return hip_status(fn, laq::launch_paged_append(
+                            internal_batch(*batch), static_cast<const uint16_t*>(qkv), qkv_stride,
+                            static_cast<const uint16_t*>(q_norm_weight), static_cast<const uint16_t*>(k_norm_weight),
+                            cos_sin, rope_rows, Hq, Hkv, eps, static_cast<uint16_t*>(q_out),
+                            static_cast<hipStream_t>(stream), ev));
+}
+
+int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  if (B < 1 || B > (1 << 20) || T < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096 || T > (1LL << 30) ||
+      T * Hq > (1LL << 30) || capacity < 1 || capacity > (1LL << 30))
+    return 0;
+  return laq::paged_attention_workspace(B, T, Hq, Hkv, capacity);
+}
+
+laq_status laq_paged_attention_f16(const laq_paged_batch* batch, const void* q, int64_t Hq, int64_t Hkv,
+                                   int64_t head_dim, int64_t window, void* out, void* workspace,
+                                   int64_t workspace_bytes, void* stream) {
+  const char* fn = "laq_paged_attention_f16";
+  const laq::LaunchEvents ev = take_events();
+  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim);
+  if (st != LAQ_OK) return st;
+  if (window < 0 || window > (1LL << 30)) return fail(LAQ_ERR_BAD_SHAPE, fn, "window must be in 0..2^30");
+  if (batch->B == 0 || batch->T == 0) return ok();
+  if (!q || !out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
+  const int64_t capacity = batch->table_pages * batch->page_size;
+  const int64_t need = laq::paged_attention_workspace(batch->B, batch->T, Hq, Hkv, capacity);
+  if (need > 0 && !workspace) return fail(LAQ_ERR_NULL_POINTER, fn, "null workspace");
+  if (workspace_bytes < need)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below laq_paged_attention_workspace_bytes");
+  if (laq::paged_attention_grid(batch->B, batch->T, Hq, Hkv, capacity) > 0x7FFFFFFFLL)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
+    return fail(LAQ_ERR_MISALIGNED, fn, "q, out and workspace must be 16-byte aligned");
+  return hip_status(fn, laq::launch_paged_attention(internal_batch(*batch), static_cast<const uint16_t*>(q), Hq, Hkv,
+                                                    window, static_cast<uint16_t*>(out),
+                                                    static_cast<float*>(workspace), static_cast<hipStream_t>(stream),
+                                                    ev));
+}
+
+laq_status laq_sample_f16(const void* logits, int64_t logits_stride, int64_t rows, int64_t V, const float* u,
+                          const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                          int32_t* token, float* prob, void* stream) {
+  const char* fn = "laq_sample_f16";
+  const laq::LaunchEvents ev = take_events();
+  if (rows < 0 || rows > 0x7FFFFFFFLL) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= rows < 2^31");
+  if (V < 1 || V > (1 << 24)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= V <= 2^24");
+  if (logits_stride < V && rows > 1) return fail(LAQ_ERR_BAD_SHAPE, fn, "logits_stride must be at least V");
+  if (logits_stride < 0 || logits_stride > (1LL << 32)) return fail(LAQ_ERR_BAD_SHAPE, fn, "logits_stride must be in 0..2^32");
+  if (rows == 0) return ok();
+  if (!logits || !u || !token) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if (!aligned(logits, 2)) return fail(LAQ_ERR_MISALIGNED, fn, "logits must be 2-byte aligned");
+  if (!aligned(u, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
+      !aligned(token, 4) || !aligned(prob, 4))
+    return fail(LAQ_ERR_MISALIGNED, fn, "per-row arrays must be 4-byte aligned");
+  return hip_status(fn, laq::launch_sample(static_cast<const uint16_t*>(logits), logits_stride, rows, V, u, temperature,
+                                           top_k, top_p, min_p, token, prob, static_cast<hipStream_t>(stream), ev));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
 // The linear without a caller workspace and without allocation: split-K
 // partial sums in a scratch array the library holds on each GPU.
 // ---------------------------------------------------------------------------

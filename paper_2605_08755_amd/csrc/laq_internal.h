@@ -249,6 +249,29 @@ hipError_t launch_decode_attention_qkv(const uint16_t* qkv, const uint16_t* qw, 
                                        const float* cos_sin, int64_t pos, int64_t Hq, int64_t Hkv, float eps,
                                        uint16_t* kc, uint16_t* vc, int64_t S_max, uint16_t* out, float* ws,
                                        hipStream_t stream, const LaunchEvents& ev);
+
+// A batch over paged caches (laq_paged_batch of include/laq.h, checked).
+struct PagedBatch {
+  uint16_t* k;
+  uint16_t* v;
+  const int* page_table;
+  const int* token_start;
+  const int* seq_len;
+  int64_t page_stride, head_stride, table_stride;
+  int slot_stride, page_shift, num_pages, table_pages, B, T;
+};
+hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
+                               const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv,
+                               float eps, uint16_t* q_out, hipStream_t stream, const LaunchEvents& ev);
+// Workspace bytes and blocks of the attention, for any lengths within the
+// table's capacity (positions a sequence can have).
+int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+int64_t paged_attention_grid(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,
+                                  uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev);
+hipError_t launch_sample(const uint16_t* logits, int64_t stride, int64_t rows, int64_t V, const float* u,
+                         const float* temperature, const int* top_k, const float* top_p, const float* min_p, int* token,
+                         float* prob, hipStream_t stream, const LaunchEvents& ev);
 hipError_t launch_silu_mul(const uint16_t* gu, uint16_t* y, int64_t M, int64_t I, hipStream_t stream,
                            const LaunchEvents& ev);
 

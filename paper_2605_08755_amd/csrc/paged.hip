@@ -1,0 +1,997 @@
+// Batched serving over paged key/value caches: per-head q/k RMSNorm with the
+// rotary embedding and the append of new rows, and the attention of new rows
+// (one per sequence when decoding, many in a prompt's chunk) over each
+// sequence's pages.  fp16 in and out, fp32 sums and softmax statistics, fixed
+// reduction orders (deterministic).  Head dimension 128.
+//
+// A batch of B sequences: sequence b owns rows token_start[b] ..
+// token_start[b + 1] - 1, which are the last of its seq_len[b] positions;
+// position t lies in page page_table[b][t / page_size].  These arrays live in
+// device memory and the host never reads them, so a captured graph serves a
+// growing batch.  Nothing read from them is trusted as an address: rows are
+// clamped to 0 .. T, positions to the table's width, and a page outside the
+// cache is a page that is not there.
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "mfma_util.h"
+
+namespace laq {
+
+namespace {
+
+constexpr int kHeadDim = 128;
+constexpr float kScaleLog2 = 0.08838834764831845f * 1.4426950408889634f;  // log2(e) / sqrt(128)
+constexpr float kNoMax = -1e30f;  // running maximum before the first visible score (finite: no inf - inf)
+
+typedef float float16_t __attribute__((ext_vector_type(16)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+
+
+__device__ __forceinline__ int readlane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int v, int old) {
+  return __builtin_amdgcn_update_dpp(old, v, CTRL, 0xF, 0xF, false);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float v) {
+  return __builtin_bit_cast(float, dpp_i<CTRL>(__builtin_bit_cast(int, v), 0));
+}
+// Sum over the eight lanes of a half DPP row / maximum and sum over the 16
+// lanes of a row, in every lane.
+__device__ __forceinline__ float sum8(float v) {
+  v += dpp_f<0xB1>(v);   // quad_perm [1,0,3,2]
+  v += dpp_f<0x4E>(v);   // quad_perm [2,3,0,1]
+  v += dpp_f<0x141>(v);  // row_half_mirror
+  return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v = sum8(v);
+  v += dpp_f<0x140>(v);  // row_mirror
+  return v;
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, dpp_f<0xB1>(v));
+  v = fmaxf(v, dpp_f<0x4E>(v));
+  v = fmaxf(v, dpp_f<0x141>(v));
+  return fmaxf(v, dpp_f<0x140>(v));
+}
+// Inclusive prefix sum over the 64 lanes: shifts by 1, 2, 4, 8 within each
+// 16-lane row (lanes shifted in read 0), then the rows' totals.
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+  v += dpp_i<0x111>(v, 0);
+  v += dpp_i<0x112>(v, 0);
+  v += dpp_i<0x114>(v, 0);
+  v += dpp_i<0x118>(v, 0);
+  const int t0 = readlane(v, 15), t1 = readlane(v, 31), t2 = readlane(v, 47);
+  return v + (lane >= 16 ? t0 : 0) + (lane >= 32 ? t1 : 0) + (lane >= 48 ? t2 : 0);
+}
+// Sum over the 64 lanes of whole numbers below 2^53 (exact in any order).
+__device__ __forceinline__ double wave_sum_exact(double v) {
+#pragma unroll
+  for (int s = 32; s >= 1; s >>= 1) v += __shfl_xor(v, s);
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// append
+// ---------------------------------------------------------------------------
+
+// A wave takes one row and every waves_per_row-th group of eight heads, eight
+// lanes a head: lane i holds dimensions 8i .. 8i + 7 and their rotation partners 64
+// further, so a head's two 128-byte halves are loaded and stored whole and the
+// norm needs one sum over eight lanes.  What bounds it: the bytes of the rows
+// in and out; the row's table line is read once per wave.
+// The row's sequence is found by counting the sequences that end at or before
+// it, 64 per step, while the row's first loads are in flight.
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const uint16_t* __restrict__ qkv,
+                                                           int64_t qkv_stride, const uint16_t* __restrict__ qw,
+                                                           const uint16_t* __restrict__ kw,
+                                                           const float* __restrict__ cos_sin, int rope_rows, int Hq,
+                                                           int Hkv, float eps, uint16_t* __restrict__ q_out,
+                                                           int waves_per_row) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+  const int row = uniform((int)(wave / waves_per_row));
+  const int first = uniform((int)(wave - (int64_t)row * waves_per_row));
+  if (row >= pb.T) return;
+  const int i = lane & 7;
+  const int H = Hq + 2 * Hkv;
+  const int groups = (H + 7) >> 3;
+  const uint16_t* const src = qkv + row * qkv_stride;
+
+  auto load = [&](int grp, u32x4& a, u32x4& b) {
+    const int h = min(grp * 8 + (lane >> 3), H - 1);
+    const uint16_t* p = src + (int64_t)h * kHeadDim + 8 * i;
+    a = *reinterpret_cast<const u32x4*>(p);
+    b = *reinterpret_cast<const u32x4*>(p + 64);
+  };
+  u32x4 a, b;
+  load(first, a, b);
+
+  int seq = 0;
+  for (int b0 = 0; b0 < pb.B; b0 += 64) {
+    const bool before = b0 + lane < pb.B && pb.token_start[b0 + lane + 1] <= row;
+    seq += __popcll(__ballot(before));
+  }
+  seq = uniform(seq);
+  if (seq >= pb.B) return;  // behind the last sequence
+  const int s0 = pb.token_start[seq], s1 = min(pb.token_start[seq + 1], pb.T);
+  if (row < s0) return;     // before the first
+  const int64_t pos = (int64_t)pb.seq_len[seq] - s1 + row;
+  const int64_t cap = (int64_t)pb.table_pages << pb.page_shift;
+  const bool placed = pos >= 0 && pos < cap && pos < rope_rows;
+  int page = -1;
+  if (placed) page = pb.page_table[seq * pb.table_stride + (pos >> pb.page_shift)];
+  const bool keep = (unsigned)page < (unsigned)pb.num_pages;
+  const int64_t slot = keep ? page * pb.page_stride + (pos & ((1LL << pb.page_shift) - 1)) * pb.slot_stride : 0;
+
+  const float* const cs = cos_sin + (placed ? pos : 0) * kHeadDim + 8 * i;
+  float c[8], s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c[e] = cs[e], s[e] = cs[64 + e];
+
+  for (int grp = first; grp < groups;) {
+    const int h = grp * 8 + (lane >> 3);
+    half8_t x = __builtin_bit_cast(half8_t, a), y = __builtin_bit_cast(half8_t, b);
+    const u32x4 va = a, vb = b;
+    const int next = grp + waves_per_row;
+    if (next < groups) load(next, a, b);
+    if (h < Hq + Hkv) {
+      float u[8], v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = (float)x[e], v[e] = (float)y[e];
+      const uint16_t* const w = h < Hq ? qw : kw;
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(u[e], u[e], fmaf(v[e], v[e], ss));
+      ss = sum8(ss);
+      if (w != nullptr) {
+        const float r = 1.0f / sqrtf(ss * (1.0f / kHeadDim) + eps);
+        const half8_t wa = *reinterpret_cast<const half8_t*>(w + 8 * i);
+        const half8_t wb = *reinterpret_cast<const half8_t*>(w + 64 + 8 * i);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = u[e] * r * (float)wa[e], v[e] = v[e] * r * (float)wb[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = (_Float16)(u[e] * c[e] - v[e] * s[e]);
+        y[e] = (_Float16)(v[e] * c[e] + u[e] * s[e]);
+      }
+      if (h < Hq) {
+        if (!placed) x = half8_t{}, y = half8_t{};
+        uint16_t* d = q_out + ((int64_t)row * Hq + h) * kHeadDim + 8 * i;
+        *reinterpret_cast<half8_t*>(d) = x;
+        *reinterpret_cast<half8_t*>(d + 64) = y;
+      } else if (keep) {
+        uint16_t* d = pb.k + slot + (h - Hq) * pb.head_stride + 8 * i;
+        *reinterpret_cast<half8_t*>(d) = x;
+        *reinterpret_cast<half8_t*>(d + 64) = y;
+      }
+    } else if (h < H && keep) {
+      uint16_t* d = pb.v + slot + (h - Hq - Hkv) * pb.head_stride + 8 * i;
+      *reinterpret_cast<u32x4*>(d) = va;
+      *reinterpret_cast<u32x4*>(d + 64) = vb;
+    }
+    grp = next;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention: the work of a batch
+// ---------------------------------------------------------------------------
+
+// The work of one key/value head is cut into items: a tile of BM query rows
+// (row r = token r / R, query head r % R of the head's R) of one sequence, and
+// a range of its positions.  A sequence's positions are split into ranges of
+// `chunk` units of 64 positions; the chunk is chosen on the device from the
+// batch's own lengths, so that all items together are about kItems<BM> per
+// launch: a long sequence among short ones, or a single one, still occupies
+// the chip, and a sequence that fits one range is written without a second
+// pass.  Every block derives the same numbers from the same arrays; the grid
+// and the workspace are sized by bounds that hold for any lengths:
+//   items <= kItems / Hkv + tiles,  records (ranges of split tiles) <= 2 kItems / Hkv,
+//   split tiles <= kItems / Hkv     per key/value head,
+// since a sequence of x units has ceil(x / chunk) < x / chunk + 1 ranges, at
+// most 2 x / chunk where it is split, and chunk >= (sum of tiles x units) Hkv / kItems.
+constexpr int kUnit = 64;
+constexpr int kSmallRows = 16, kLargeRows = 128;
+template <int BM>
+constexpr int kItems = BM == kSmallRows ? 512 : 512;
+template <int BM>
+constexpr int kMinChunk = BM == kSmallRows ? 4 : 4;  // units: a shorter range costs more in records than it gains
+
+// One sequence, seen from one lane.
+struct Seq {
+  int s0, n, pos0, end, lo;  // first row, rows, first row's position, positions there are, first position of the ranges
+  int tiles, units;
+};
+
+template <int BM>
+__device__ __forceinline__ Seq load_seq(const PagedBatch& pb, int b, int R, int window) {
+  Seq q{0, 0, 0, 0, 0, 0, 0};
+  if (b < pb.B) {
+    q.s0 = min(max(pb.token_start[b], 0), pb.T);
+    const int s1 = min(max(pb.token_start[b + 1], q.s0), pb.T);
+    const int len = max(pb.seq_len[b], 0);
+    q.n = s1 - q.s0;
+    q.pos0 = len - q.n;
+    q.end = min(len, pb.table_pages << pb.page_shift);
+    if (window > 0) q.lo = max(q.pos0 - window + 1, 0) & -kUnit;
+    if (q.n > 0) {
+      q.tiles = (q.n * R + BM - 1) / BM;
+      q.units = max((q.end - q.lo + kUnit - 1) / kUnit, 1);  // rows that see nothing are an item too
+    }
+  }
+  return q;
+}
+
+struct Item {
+  bool found;
+  int b, s0, n, pos0, end, lo;
+  int tile, split, splits, chunk;
+  int rec;  // first record of the tile's ranges
+};
+
+// Item `idx` of a key/value head (SPLIT: the idx-th split tile).
+template <int BM, bool SPLIT>
+__device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, int Hkv, int window, int lane) {
+  double total = 0.0;
+  Seq q = load_seq<BM>(pb, lane, R, window);
+  total = wave_sum_exact((double)q.tiles * q.units);
+  for (int b0 = 64; b0 < pb.B; b0 += 64) {
+    const Seq x = load_seq<BM>(pb, b0 + lane, R, window);
+    total += wave_sum_exact((double)x.tiles * x.units);
+  }
+  Item it;
+  it.found = false;
+  const double share = total * Hkv * (1.0 / kItems<BM>);
+  it.chunk = uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
+  int items = 0, recs = 0;
+  for (int b0 = 0; b0 < pb.B; b0 += 64) {
+    if (b0 > 0) q = load_seq<BM>(pb, b0 + lane, R, window);
+    const int splits = (q.units + it.chunk - 1) / it.chunk;
+    const int rec = splits > 1 ? q.tiles * splits : 0;
+    const int own = SPLIT ? (splits > 1 ? q.tiles : 0) : q.tiles * splits;
+    const int upto = items + wave_scan(own, lane);
+    const int rupto = recs + wave_scan(rec, lane);
+    const uint64_t past = __ballot(upto > idx);
+    if (past) {
+      const int l = __ffsll((unsigned long long)past) - 1;
+      it.found = true;
+      it.b = b0 + l;
+      it.s0 = readlane(q.s0, l);
+      it.n = readlane(q.n, l);
+      it.pos0 = readlane(q.pos0, l);
+      it.end = readlane(q.end, l);
+      it.lo = readlane(q.lo, l);
+      it.splits = readlane(splits, l);
+      const int i = idx - readlane(upto - own, l);
+      // the last tiles of a prompt see the most positions: they go first
+      it.tile = readlane(q.tiles, l) - 1 - (SPLIT ? i : i / it.splits);
+      it.split = SPLIT ? 0 : i % it.splits;
+      it.rec = readlane(rupto - rec, l) + it.tile * it.splits;
+      return it;
+    }
+    items = readlane(upto, 63);
+    recs = readlane(rupto, 63);
+  }
+  return it;
+}
+
+// The positions that an item's rows j0 .. j1 (tokens) can see within its range.
+struct Span {
+  int lo, hi;          // lo a multiple of kUnit
+  int all_lo, all_hi;  // positions that every row sees
+};
+__device__ __forceinline__ Span span_of(const Item& it, int j0, int j1, int window) {
+  Span s;
+  const int first = it.pos0 + j0, last = it.pos0 + j1;
+  const int lo = window > 0 ? max(first - window + 1, 0) & -kUnit : 0;
+  s.lo = max(lo, it.lo + it.split * it.chunk * kUnit);
+  s.hi = min(last + 1, it.end);
+  if (it.split + 1 < it.splits) s.hi = min(s.hi, it.lo + (it.split + 1) * it.chunk * kUnit);
+  s.all_lo = window > 0 ? max(last - window + 1, 0) : 0;
+  s.all_hi = min(first + 1, it.end);
+  return s;
+}
+
+// Sixteen positions from t on (t a multiple of 16, in one page) of one head as
+// a buffer: rows from `end` on, and all rows of a page that is not there, lie
+// past its extent and read as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows16(const PagedBatch& pb, const uint16_t* base, int g, int page,
+                                                         int t, int end) {
+  const bool there = (unsigned)page < (unsigned)pb.num_pages && t < end;
+  const int64_t at = (int64_t)(there ? page : 0) * pb.page_stride + g * pb.head_stride +
+                     (int64_t)(t & ((1 << pb.page_shift) - 1)) * pb.slot_stride;
+  const int rows = min(end - t, 16);
+  const uint32_t bytes = there ? (uint32_t)((rows - 1) * pb.slot_stride + kHeadDim) * 2 : 0;
+  return rsrc(base + (there ? at : 0), bytes);
+}
+
+// Bits of the halves of x that are infinite or NaN: 0x8000 in each.
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) { return ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t x) { return x & ~((not_finite(x) >> 15) * 0xFFFFu); }
+__device__ __forceinline__ u32x4 finite_or_zero(u32x4 x) {
+  return u32x4{finite_or_zero(x.x), finite_or_zero(x.y), finite_or_zero(x.z), finite_or_zero(x.w)};
+}
+__device__ __forceinline__ uint32_t not_finite(u32x4 x) {
+  return not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w);
+}
+
+// Results of one item: rows of partial sums (split) or of outputs.
+struct Out {
+  uint16_t* out;
+  float* ws;
+  int Hq, rec_bound;
+};
+
+// ---------------------------------------------------------------------------
+// attention of up to 16 rows per tile: the cache bytes bound it
+// ---------------------------------------------------------------------------
+
+// A block of four waves holds the 16 query rows of one item (decoding: the R
+// heads of one token) and each wave walks its own steps of 32 positions with a
+// running maximum, denominator and value sums, as the single-sequence
+// long-context kernel does: keys go memory -> LDS directly (piece p of row r
+// at position p ^ (r & 15)), scores on the matrix cores in fp16, values
+// straight into registers as the operand of the fp32 16x16x4 instruction, so
+// the probabilities stay in 32 bits.  Two blocks per compute unit: one's
+// search for its item, first loads and last joining lie under the other's
+// stream.  The page numbers of 32 steps sit in one register of a wave (lane l:
+// half l & 1 of step l >> 1) and become scalar buffer descriptors.
+constexpr int kWaves = 4;
+constexpr int kStep = 32;
+constexpr int kStride = kWaves * kStep;
+constexpr int kRowBytes = (kStep + 4) * 4;         // a row of probabilities (4 words of padding)
+constexpr int kKeyBytes = kStep * kHeadDim * 2;    // a step's keys
+constexpr int kSmallLds = kWaves * (2 * kKeyBytes + 16 * kRowBytes);
+
+__device__ __forceinline__ void lds_read4(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+  asm volatile(
+      "ds_read_b128 %0, %4\n\t"
+      "ds_read_b128 %1, %5\n\t"
+      "ds_read_b128 %2, %6\n\t"
+      "ds_read_b128 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+      : "v"(a0), "v"(a1), "v"(a2), "v"(a3)
+      : "memory");
+}
+__device__ __forceinline__ void lds_put(uint32_t addr, float v) {
+  asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory");
+}
+
+__global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(PagedBatch pb,
+                                                                             const uint16_t* __restrict__ q, int R,
+                                                                             int Hkv, int window, Out o_) {
+  typedef __attribute__((address_space(3))) void lds_void;
+  extern __shared__ u32x4 small_lds[];
+  char* const lds = reinterpret_cast<char*>(small_lds);
+  const int lane = threadIdx.x & 63;
+  const int w = uniform(threadIdx.x >> 6);
+  const int n = lane & 15, j = lane >> 4;
+  const int g = uniform(blockIdx.x % Hkv);
+  const Item it = find_item<kSmallRows, false>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  if (!it.found) return;
+  const int rows = min(it.n * R - it.tile * kSmallRows, kSmallRows);
+  const int r0 = it.tile * kSmallRows;
+  const Span sp = span_of(it, r0 / R, (r0 + rows - 1) / R, window);
+
+  // q as matrix operand: lane (m, j), window i: dimensions 32 i + 8 j .. + 7 of row m.
+  u32x4 qa[4];
+  {
+    const int r = r0 + min(n, rows - 1);
+    const uint16_t* p = q + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 8 * j;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qa[i] = *reinterpret_cast<const u32x4*>(p + 32 * i);
+  }
+  // Rows 4j + r of the results: the positions they see.
+  int see_lo[4], see_hi[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int m = 4 * j + r;
+    const int pos = it.pos0 + (r0 + m) / R;
+    see_hi[r] = m < rows ? min(pos + 1, it.end) : 0;
+    see_lo[r] = window > 0 ? pos - window + 1 : 0;
+  }
+
+  char* const keys = lds + w * 2 * kKeyBytes;
+  const uint32_t probs = lds_byte(lds + kWaves * 2 * kKeyBytes + w * 16 * kRowBytes);
+  const int p_first = sp.lo + w * kStep;
+  const int* const table = pb.page_table + it.b * pb.table_stride;
+  // Page numbers of the 32 steps from step s on (a multiple of 32).
+  auto pages_from = [&](int s) {
+    const int t = p_first + (s + (lane >> 1)) * kStride + 16 * (lane & 1);
+    return t < sp.hi ? table[t >> pb.page_shift] : -1;
+  };
+  int pages = pages_from(0);
+
+  constexpr int kLoads = kStep / 4;  // load instructions per step for the keys, and for the values
+  u32x4 vv[2][kLoads];
+  int bad[2];  // whether a page of the step's first (1) or second (2) half is not there
+  auto request = [&](auto bc, int s, int p) {
+    constexpr int B = decltype(bc)::value;
+    if (s > 0 && (s & 31) == 0) pages = pages_from(s);
+    const int pg[2] = {readlane(pages, 2 * (s & 31)), readlane(pages, 2 * (s & 31) + 1)};
+    bad[B] = ((unsigned)pg[0] >= (unsigned)pb.num_pages ? 1 : 0) | ((unsigned)pg[1] >= (unsigned)pb.num_pages ? 2 : 0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = 4 * i + j;
+      const __amdgpu_buffer_rsrc_t kr = rows16(pb, pb.k, g, pg[i >> 2], p + 16 * (i >> 2), sp.hi);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(keys + B * kKeyBytes + i * 1024), 16,
+                                               (uint32_t)(r & 15) * pb.slot_stride * 2 + 16 * (n ^ (r & 15)), 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // the keys' wait below counts the values' loads as the later ones
+    // values of step k = 4 kk + i: positions 16 kk + 4 j + i
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const __amdgpu_buffer_rsrc_t vr = rows16(pb, pb.v, g, pg[k >> 2], p + 16 * (k >> 2), sp.hi);
+      vv[B][k] =
+          __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(4 * j + (k & 3)) * pb.slot_stride * 2 + 16 * n, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  float m[4], l[4];
+  float4_t o[8];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) m[r] = kNoMax, l[r] = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = float4_t{0.f, 0.f, 0.f, 0.f};
+
+  // One step: B the buffers that hold it, MORE whether the next step's loads
+  // are in flight (compile-time, so that the waits for this step's values,
+  // which the compiler counts, leave them in flight).
+  auto step = [&](auto bc, auto mc, int p) {
+    constexpr int B = decltype(bc)::value;
+    constexpr bool MORE = decltype(mc)::value;
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vmcnt<(MORE ? 3 : 1) * kLoads>();  // the keys: this step's values and the next step's loads may be outstanding
+    __builtin_amdgcn_sched_barrier(0);
+    const bool masked = bad[B] != 0 || p < sp.all_lo || p + kStep > sp.all_hi || p + kStep > sp.hi;
+    float sc[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      u32x4 f[4];
+      const uint32_t a = lds_byte(keys + B * kKeyBytes) + (16 * t + n) * 256;
+      lds_read4(f, a + 16 * (j ^ n), a + 16 * ((4 + j) ^ n), a + 16 * ((8 + j) ^ n), a + 16 * ((12 + j) ^ n));
+      float4_t c[4];  // a sum per window of 32 dimensions, added pairwise
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        c[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, qa[i]),
+                                                      __builtin_bit_cast(half8_t, f[i]),
+                                                      float4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      const float4_t cc = (c[0] + c[1]) + (c[2] + c[3]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sc[t][r] = cc[r] * kScaleLog2;
+      if (masked) {
+        const int at = p + 16 * t + n;
+        const bool there = at < sp.hi && !(bad[B] >> t & 1);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sc[t][r] = there && at >= see_lo[r] && at < see_hi[r] ? sc[t][r] : -INFINITY;
+      }
+    }
+    float alpha[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float mn = fmaxf(m[r], row_max(fmaxf(sc[0][r], sc[1][r])));
+      alpha[r] = __builtin_amdgcn_exp2f(m[r] - mn);
+      m[r] = mn;
+      const float p0 = __builtin_amdgcn_exp2f(sc[0][r] - mn), p1 = __builtin_amdgcn_exp2f(sc[1][r] - mn);
+      l[r] = fmaf(l[r], alpha[r], p0 + p1);
+      const uint32_t row = probs + (4 * j + r) * kRowBytes + 4 * n;
+      lds_put(row, p0);
+      lds_put(row + 64, p1);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[e][r] *= alpha[r];
+    u32x4 pa[4];
+    const uint32_t a = probs + n * kRowBytes + 16 * j;  // lane (m, j): positions 16 kk + 4 j .. + 3 of row m
+    lds_read4(pa, a, a + 64, a, a + 64);
+    __builtin_amdgcn_sched_barrier(0);  // no value is waited for before the softmax is done
+    if (masked) {
+      // A value that only some rows see may be infinite or NaN, and 0 times it
+      // is NaN: such values leave the product and are added to the rows that
+      // see them (the result is infinite or NaN whatever their weight).
+      uint32_t nf = 0;
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) nf |= not_finite(vv[B][k]);
+      if (__ballot(nf != 0)) {
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+          for (int jt = 0; jt < 4; ++jt) {
+            const int at = p + 16 * (k >> 2) + 4 * jt + (k & 3);
+            const bool there = at < sp.hi && !(bad[B] >> (k >> 2) & 1);
+            u32x4 x;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) x[d] = __shfl(vv[B][k][d], 16 * jt + n);
+            const half8_t v = __builtin_bit_cast(half8_t, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float f = (float)v[e];
+              const bool add = there && !(fabsf(f) < INFINITY);
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                o[e][r] += add && at >= see_lo[r] && at < see_hi[r] ? f : 0.0f;
+            }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) vv[B][k] = finite_or_zero(vv[B][k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const u32x4 pk = pa[k >> 2];
+      const uint32_t pbits = (k & 3) == 0 ? pk.x : (k & 3) == 1 ? pk.y : (k & 3) == 2 ? pk.z : pk.w;
+      const float pf = __builtin_bit_cast(float, pbits);
+      const half8_t v = __builtin_bit_cast(half8_t, vv[B][k]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(pf, (float)v[e], o[e], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr std::integral_constant<int, 0> b0;
+  constexpr std::integral_constant<int, 1> b1;
+  if (p_first < sp.hi) {
+    int p = p_first, s = 0;
+    request(b0, 0, p);
+    for (; p + 2 * kStride < sp.hi; p += 2 * kStride, s += 2) {
+      request(b1, s + 1, p + kStride);
+      step(b0, std::true_type{}, p);
+      request(b0, s + 2, p + 2 * kStride);
+      step(b1, std::true_type{}, p + kStride);
+    }
+    if (p + kStride < sp.hi) {
+      request(b1, s + 1, p + kStride);
+      step(b0, std::true_type{}, p);
+      step(b1, std::false_type{}, p + kStride);
+    } else {
+      step(b0, std::false_type{}, p);
+    }
+  }
+
+  // The waves' results, in wave order: 128 value sums per (wave, row) over the
+  // keys' place, maxima and denominators over the probabilities'.
+  __syncthreads();
+  float* const osum = reinterpret_cast<float*>(lds);                              // [4][16][128]
+  float* const stat = reinterpret_cast<float*>(lds + kWaves * 2 * kKeyBytes);     // [4][16][2]
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int h = 4 * j + r;
+    const float lt = row_sum(l[r]);
+    float* d = osum + (w * 16 + h) * kHeadDim + 8 * n;
+    *reinterpret_cast<float4_t*>(d) = float4_t{o[0][r], o[1][r], o[2][r], o[3][r]};
+    *reinterpret_cast<float4_t*>(d + 4) = float4_t{o[4][r], o[5][r], o[6][r], o[7][r]};
+    if (n == 0) {
+      stat[(w * 16 + h) * 2] = m[r];
+      stat[(w * 16 + h) * 2 + 1] = lt;
+    }
+  }
+  __syncthreads();
+  const int rec = it.rec + it.split;
+  if (it.splits > 1 && rec >= o_.rec_bound) return;  // token_start out of order
+  float* const wp = o_.ws + ((int64_t)g * o_.rec_bound + rec) * (kSmallRows * (kHeadDim + 2));
+  for (int idx = threadIdx.x; idx < rows * kHeadDim; idx += 64 * kWaves) {
+    const int h = idx / kHeadDim, d = idx % kHeadDim;
+    float M = kNoMax;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, stat[(i * 16 + h) * 2]);
+    float den = 0.0f, num = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float e = __builtin_amdgcn_exp2f(stat[(i * 16 + h) * 2] - M);
+      den = fmaf(e, stat[(i * 16 + h) * 2 + 1], den);
+      num = fmaf(e, osum[(i * 16 + h) * kHeadDim + d], num);
+    }
+    if (it.splits > 1) {
+      wp[idx] = num;
+      if (d == 0) {
+        wp[kSmallRows * kHeadDim + 2 * h] = M;
+        wp[kSmallRows * kHeadDim + 2 * h + 1] = den;
+      }
+    } else {
+      const int r = r0 + h;
+      const _Float16 y = (_Float16)(den > 0.0f ? num / den : 0.0f);
+      o_.out[((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + d] = __builtin_bit_cast(uint16_t, y);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// attention of prompts' chunks: the matrix cores bound it
+// ---------------------------------------------------------------------------
+
+// A block of four waves holds 128 query rows of one item, 32 a wave, and walks
+// the positions in tiles of 64.  Scores are formed transposed, keys (rows) x
+// queries (columns), so that a lane holds 32 scores of one query: the running
+// maximum and the denominator need one exchange between the two halves of the
+// wave, and the probabilities are already the second product's operand
+// (columns: queries) in the order in which the transposing LDS reads deliver
+// the values (lane half h: positions 16 s + 4 h .. + 3 and 8 further).
+//
+// Probabilities are rounded to fp16 for the matrix cores (half a step: 2^-11
+// of each, their errors independent).  They are 2^8 times exp(score - ref),
+// where the reference ref only follows the maximum once that has grown by more
+// than 2^7: so they stay below 2^15 and full precision reaches down to 2^-22
+// of the largest, and the value sums are rarely rescaled.  The denominator is
+// the fp32 sum of the unrounded ones.
+//
+// Tiles of keys and values go memory -> registers -> LDS, two buffers, so that
+// a tile's loads are in flight while the one before is computed and a block
+// meets once per tile.  Piece p (16 bytes) of key row r sits at p ^ (r & 15)
+// and of value row r at p ^ 4 (r & 3): the operand reads touch each bank once.
+constexpr int kTile = 64;
+constexpr int kTileBytes = kTile * kHeadDim * 2;
+constexpr int kLargeLds = 4 * kTileBytes + 64;
+constexpr float kProbLog2 = 8.0f, kLagLog2 = 7.0f;
+
+__global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBatch pb, const uint16_t* __restrict__ q,
+                                                                         int R, int Hkv, int window, Out o_) {
+  extern __shared__ u32x4 large_lds[];
+  char* const lds = reinterpret_cast<char*>(large_lds);
+  int* const flags = reinterpret_cast<int*>(lds + 4 * kTileBytes);  // [2]: tile whose values are not all finite
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int w = uniform(tid >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const int g = uniform(blockIdx.x % Hkv);
+  const Item it = find_item<kLargeRows, false>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  if (!it.found) return;
+  const int r0 = it.tile * kLargeRows;
+  const int rows = min(it.n * R - r0, kLargeRows);
+  const Span sp = span_of(it, r0 / R, (r0 + rows - 1) / R, window);
+
+  // This lane's query row and what it sees; its operand: dimensions 16 s + 8 h .. + 7.
+  const int my = 32 * w + n;
+  const bool live = my < rows;
+  const int token = (r0 + min(my, rows - 1)) / R;
+  const int64_t qrow = (int64_t)(it.s0 + token) * o_.Hq + g * R + (r0 + min(my, rows - 1)) % R;
+  const int pos = it.pos0 + token;
+  const int see_hi = live ? min(pos + 1, it.end) : 0;
+  const int see_lo = window > 0 ? pos - window + 1 : 0;
+  // Tiles beyond these no row of the wave sees.
+  int wave_lo, wave_hi;
+  {
+    const int j0 = (r0 + min(32 * w, rows - 1)) / R, j1 = (r0 + min(32 * w + 31, rows - 1)) / R;
+    wave_lo = window > 0 ? it.pos0 + j0 - window + 1 : 0;
+    wave_hi = 32 * w < rows ? it.pos0 + j1 + 1 : 0;
+  }
+  half8_t qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const half8_t*>(q + qrow * kHeadDim + 16 * s + 8 * h);
+
+  const int* const table = pb.page_table + it.b * pb.table_stride;
+  auto pages_from = [&](int t0) {  // page numbers of the 64 groups of 16 positions from t0 on
+    const int t = t0 + 16 * lane;
+    return t < sp.hi ? table[t >> pb.page_shift] : -1;
+  };
+  int pages = pages_from(sp.lo), pages_at = sp.lo;
+
+  // Staging: thread (row tid / 16 of each group of 16, piece tid % 16).
+  const int sr = tid >> 4, spc = tid & 15;
+  const uint32_t src_at = (uint32_t)sr * pb.slot_stride * 2 + 16 * spc;
+  u32x4 kreg[4], vreg[4];
+  int bad = 0;  // groups of the staged tile whose page is not there
+  auto load_tile = [&](int t0) {
+    if (t0 - pages_at >= 64 * 16) pages = pages_from(t0), pages_at = t0;
+    bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int page = readlane(pages, (t0 - pages_at) / 16 + i);
+      bad |= (unsigned)page >= (unsigned)pb.num_pages ? 1 << i : 0;
+      kreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows16(pb, pb.k, g, page, t0 + 16 * i, sp.hi), src_at, 0, 0);
+      vreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows16(pb, pb.v, g, page, t0 + 16 * i, sp.hi), src_at, 0, 0);
+    }
+  };
+  auto is_masked = [&](int t0, int bad_groups) {
+    return bad_groups != 0 || t0 < sp.all_lo || t0 + kTile > sp.all_hi || t0 + kTile > sp.hi;
+  };
+  auto store_tile = [&](int B, int t0) {
+    char* const kd = lds + B * 2 * kTileBytes;
+    char* const vd = kd + kTileBytes;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = 16 * i + sr;
+      *reinterpret_cast<u32x4*>(kd + r * 256 + 16 * (spc ^ (r & 15))) = kreg[i];
+      *reinterpret_cast<u32x4*>(vd + r * 256 + 16 * (spc ^ (4 * (r & 3)))) = vreg[i];
+    }
+    if (is_masked(t0, bad)) {
+      uint32_t nf = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nf |= not_finite(vreg[i]);
+      if (nf) flags[B] = t0;
+    }
+  };
+
+  float ref = kNoMax, l = 0.0f;
+  float16_t o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
+
+  auto compute = [&](auto mc, int B, int t0, int bad_groups) {
+    constexpr bool MASKED = decltype(mc)::value;
+    const char* const kd = lds + B * 2 * kTileBytes;
+    const char* const vd = kd + kTileBytes;
+    float16_t s[2];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        const half8_t a = *reinterpret_cast<const half8_t*>(kd + (32 * kt + n) * 256 + 16 * ((2 * ks + h) ^ (n & 15)));
+        s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, qf[ks], s[kt], 0, 0, 0);
+      }
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int at = t0 + 32 * kt + 8 * (r >> 2) + 4 * h + (r & 3);
+          const bool there = !(bad_groups >> (2 * kt + (r >> 3)) & 1) && at < sp.hi;
+          s[kt][r] = there && at >= see_lo && at < see_hi ? s[kt][r] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
+    {
+      auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx), __builtin_bit_cast(uint32_t, mx),
+                                                false, false);
+      mx = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
+    }
+    if (__ballot(mx > ref + kLagLog2)) {
+      const float mn = mx > ref + kLagLog2 ? mx : ref;  // each query by itself: no row depends on its neighbours
+      const float alpha = __builtin_amdgcn_exp2f(ref - mn);
+      ref = mn;
+      l *= alpha;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+    }
+    const float bias = kProbLog2 - ref;
+    half8_t pf[4];
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kt][r], kScaleLog2, bias));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kt][r + 1], kScaleLog2, bias));
+        l += p0 + p1;
+        const half2_t pk = __builtin_convertvector((float2_t{p0, p1}), half2_t);
+        pf[2 * kt + (r >> 3)][r & 7] = pk[0];
+        pf[2 * kt + (r >> 3)][(r & 7) + 1] = pk[1];
+      }
+    // values: 16 lanes read 4 positions x 16 dimensions and receive a column each
+    const int gl = lane & 15;
+    const int vrow = 4 * h + (gl >> 2);
+    const int vcol = 16 * ((lane >> 4) & 1) + 4 * (gl & 3);  // dimension within 32
+    bool nf = false;
+    if constexpr (MASKED) nf = uniform(flags[B]) == t0;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        typedef short short4_t __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) short4_t lds_short4;
+        const int piece = (32 * d + vcol) >> 3;
+        const int ra = 16 * ks + vrow;  // vrow + 8: the same bits 0 and 1
+        const char* const a = vd + ra * 256 + 16 * (piece ^ (4 * (ra & 3))) + 2 * (vcol & 7);
+        const short4_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a));
+        const short4_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a + 8 * 256));
+        u32x4 v = __builtin_bit_cast(u32x4, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+        if constexpr (MASKED)
+          if (nf) v = finite_or_zero(v);
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, v), pf[ks], o[d], 0, 0, 0);
+      }
+    }
+    if constexpr (MASKED) {
+      // Values that are infinite or NaN were left out of the product (0 times
+      // one is NaN): the rows that see one receive it here, whatever its weight.
+      if (nf) {
+        for (int t = 0; t < kTile; ++t) {
+          const int at = t0 + t;
+          const bool sees = at < sp.hi && !(bad_groups >> (t >> 4) & 1) && at >= see_lo && at < see_hi;
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int dim = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
+              const _Float16 x = *reinterpret_cast<const _Float16*>(vd + t * 256 + 16 * ((dim >> 3) ^ (4 * (t & 3))) +
+                                                                    2 * (dim & 7));
+              const float f = (float)x;
+              o[d][r] += sees && !(fabsf(f) < INFINITY) ? f : 0.0f;
+            }
+        }
+      }
+    }
+  };
+
+  if (tid < 2) flags[tid] = -1;
+  __syncthreads();
+  if (sp.lo < sp.hi) {
+    load_tile(sp.lo);
+    int bad_now = bad;
+    store_tile(0, sp.lo);
+    int B = 0;
+    if (sp.lo + kTile < sp.hi) load_tile(sp.lo + kTile);
+    __syncthreads();
+    for (int t0 = sp.lo; t0 < sp.hi; t0 += kTile) {
+      const int bad_next = bad;
+      if (t0 + kTile < sp.hi) store_tile(B ^ 1, t0 + kTile);
+      if (t0 + 2 * kTile < sp.hi) load_tile(t0 + 2 * kTile);
+      if (t0 < wave_hi && t0 + kTile > wave_lo) {
+        if (is_masked(t0, bad_now))
+          compute(std::true_type{}, B, t0, bad_now);
+        else
+          compute(std::false_type{}, B, t0, 0);
+      }
+      __syncthreads();
+      B ^= 1;
+      bad_now = bad_next;
+    }
+  }
+  // the two halves of the wave hold different positions' parts of the denominator
+  {
+    auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, l), __builtin_bit_cast(uint32_t, l), false,
+                                              false);
+    l = __builtin_bit_cast(float, (uint32_t)x[0]) + __builtin_bit_cast(float, (uint32_t)x[1]);
+  }
+  if (!live) return;
+  if (it.splits > 1) {
+    const int rec = it.rec + it.split;
+    if (rec >= o_.rec_bound) return;  // token_start out of order
+    float* const wp = o_.ws + ((int64_t)g * o_.rec_bound + rec) * (kLargeRows * (kHeadDim + 2));
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<float4_t*>(wp + my * kHeadDim + 32 * d + 2 * r + 4 * h) =
+            float4_t{o[d][r], o[d][r + 1], o[d][r + 2], o[d][r + 3]};
+    if (h == 0) {
+      wp[kLargeRows * kHeadDim + 2 * my] = ref;
+      wp[kLargeRows * kHeadDim + 2 * my + 1] = l;
+    }
+    return;
+  }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  uint16_t* const dst = o_.out + qrow * kHeadDim;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<half4_t*>(dst + 32 * d + 2 * r + 4 * h) =
+          half4_t{(_Float16)(o[d][r] * inv), (_Float16)(o[d][r + 1] * inv), (_Float16)(o[d][r + 2] * inv),
+                  (_Float16)(o[d][r + 3] * inv)};
+    }
+}
+
+// Joins the ranges of the split tiles in position order: block (split tile,
+// key/value head, 16 rows of the tile), a wave per four rows, a lane per two
+// dimensions.  A row's records are weighted by 2^(their maximum - the largest).
+template <int BM>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
+  const int lane = threadIdx.x & 63;
+  const int w = uniform(threadIdx.x >> 6);
+  const int g = uniform(blockIdx.x % Hkv);
+  const Item it = find_item<BM, true>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  if (!it.found || it.rec + it.splits > o_.rec_bound) return;
+  const int r0 = it.tile * BM;
+  const int rows = min(it.n * R - r0, BM);
+  constexpr int kRec = BM * (kHeadDim + 2);
+  const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
+  for (int i = 0; i < 4; ++i) {
+    const int row = blockIdx.y * 16 + w * 4 + i;
+    if (row >= rows) break;
+    const float* const stat = base + BM * kHeadDim + 2 * row;
+    float M = kNoMax;
+    for (int s = lane; s < it.splits; s += 64) M = fmaxf(M, stat[(int64_t)s * kRec]);
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
+    float den = 0.0f;
+    float2_t num = {0.0f, 0.0f};
+    for (int s = 0; s < it.splits; ++s) {
+      const float e = __builtin_amdgcn_exp2f(stat[(int64_t)s * kRec] - M);
+      const float2_t x = *reinterpret_cast<const float2_t*>(base + (int64_t)s * kRec + row * kHeadDim + 2 * lane);
+      den = fmaf(e, stat[(int64_t)s * kRec + 1], den);
+      num[0] = fmaf(e, x[0], num[0]);
+      num[1] = fmaf(e, x[1], num[1]);
+    }
+    const int r = r0 + row;
+    const float y0 = den > 0.0f ? num[0] / den : 0.0f, y1 = den > 0.0f ? num[1] / den : 0.0f;
+    *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
+        half2_t{(_Float16)y0, (_Float16)y1};
+  }
+}
+
+// Which kernel takes a batch, and its bounds: a pure function of the sizes.
+struct AttentionPlan {
+  bool large;
+  int64_t items, split_tiles, records;  // per key/value head
+  int64_t floats;                       // workspace
+};
+
+template <int BM>
+AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
+  AttentionPlan p;
+  p.large = BM == kLargeRows;
+  const int64_t tiles = (T * R + std::min(B, T) * (BM - 1)) / BM;
+  const int64_t per_head = (kItems<BM> + Hkv - 1) / Hkv;
+  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit;
+  p.items = tiles + (split ? per_head : 0);
+  p.split_tiles = split ? std::min(per_head, tiles) : 0;
+  const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
+  p.records = split ? std::min(2 * per_head, tiles * most) : 0;
+  p.floats = p.records * Hkv * BM * (kHeadDim + 2);
+  return p;
+}
+
+// Up to 16 rows per sequence on average: decoding.
+AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
+  if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity);
+  return plan_of<kLargeRows>(B, T, R, Hkv, capacity);
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
+                               const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv,
+                               float eps, uint16_t* q_out, hipStream_t stream, const LaunchEvents& ev) {
+  // A wave per row where rows alone fill the chip, else a wave per group of eight heads.
+  const int64_t groups = (Hq + 2 * Hkv + 7) / 8;
+  const int64_t per = std::max<int64_t>(1, std::min<int64_t>(groups, kResidentWaves / pb.T));
+  launch(paged_append_kernel, dim3((unsigned)((pb.T * per + 3) / 4)), dim3(256), 0, stream, ev, pb, qkv, qkv_stride, qw,
+         kw, cos_sin, (int)std::min<int64_t>(rope_rows, 0x7FFFFFFF), (int)Hq, (int)Hkv, eps, q_out, (int)per);
+  return hipGetLastError();
+}
+
+int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  return attention_plan(B, T, Hq / Hkv, Hkv, capacity).floats * (int64_t)sizeof(float);
+}
+
+int64_t paged_attention_grid(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  return attention_plan(B, T, Hq / Hkv, Hkv, capacity).items * Hkv;
+}
+
+hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,
+                                  uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev) {
+  const int64_t R = Hq / Hkv;
+  const AttentionPlan p = attention_plan(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift);
+  LaunchEvents e1 = ev, e2;
+  if (p.split_tiles > 0) {  // the measurement hook spans both kernels
+    e1.stop = nullptr;
+    e2.stop = ev.stop;
+  }
+  const Out o{out, ws, (int)Hq, (int)p.records};
+  const dim3 grid((unsigned)(p.items * Hkv)), join((unsigned)(p.split_tiles * Hkv), p.large ? kLargeRows / 16 : 1);
+  if (p.large) {
+    launch(paged_attention_rows128_kernel, grid, dim3(256), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv, (int)window,
+           o);
+    if (p.split_tiles > 0)
+      launch(paged_attention_join_kernel<kLargeRows>, join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
+             o);
+  } else {
+    launch(paged_attention_rows16_kernel, grid, dim3(64 * kWaves), kSmallLds, stream, e1, pb, q, (int)R, (int)Hkv,
+           (int)window, o);
+    if (p.split_tiles > 0)
+      launch(paged_attention_join_kernel<kSmallRows>, join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
+             o);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace laq

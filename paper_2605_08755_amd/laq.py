@@ -34,7 +34,8 @@ EXPORTS = ("laq_abi_version", "laq_status_string", "laq_last_error", "laq_profil
            "laq_decode_attention_qkv_f16", "laq_add_rmsnorm_linear_w3g128", "laq_add_rmsnorm_linear_w4g128",
            "laq_add_rmsnorm_linear_swiglu_w3g128", "laq_add_rmsnorm_linear_swiglu_w4g128",
            "laq_mlp_workspace_bytes", "laq_add_rmsnorm_mlp_w3g128", "laq_linear_residual_w3g128",
-           "laq_linear_residual_w4g128")
+           "laq_linear_residual_w4g128", "laq_paged_append_f16", "laq_paged_attention_workspace_bytes",
+           "laq_paged_attention_f16", "laq_sample_f16")
 HEAD_DIM = 128
 
 
@@ -42,6 +43,14 @@ class LinearCall(ctypes.Structure):
     """laq_linear_call of include/laq.h."""
     _fields_ = [("x", ctypes.c_void_p), ("qweight", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("zeros", ctypes.c_void_p), ("y", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int64)]
+
+
+class PagedBatch(ctypes.Structure):
+    """laq_paged_batch of include/laq.h."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "token_start", "seq_len")] +
+                [(n, ctypes.c_int64) for n in ("num_pages", "page_size", "page_stride", "head_stride", "slot_stride",
+                                               "table_pages", "table_stride", "B", "T")])
+
 
 _lib = None
 
@@ -122,6 +131,15 @@ def lib():
         L.laq_mlp_workspace_bytes.restype = I64
         L.laq_add_rmsnorm_mlp_w3g128.argtypes = [P, P, P, F32, P, P, P, P, P, P, P, P, I64, I64, P, I64, P]
         L.laq_add_rmsnorm_mlp_w3g128.restype = ctypes.c_int32
+        PB = ctypes.POINTER(PagedBatch)
+        L.laq_paged_append_f16.argtypes = [PB, P, I64, P, P, P, I64, I64, I64, I64, F32, P, P]
+        L.laq_paged_append_f16.restype = ctypes.c_int32
+        L.laq_paged_attention_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+        L.laq_paged_attention_workspace_bytes.restype = I64
+        L.laq_paged_attention_f16.argtypes = [PB, P, I64, I64, I64, I64, P, P, I64, P]
+        L.laq_paged_attention_f16.restype = ctypes.c_int32
+        L.laq_sample_f16.argtypes = [P, I64, I64, I64, P, P, P, P, P, P, P, P]
+        L.laq_sample_f16.restype = ctypes.c_int32
         _lib = L
     return _lib
 
@@ -517,3 +535,143 @@ def silu_mul(gate_up, out=None):
         out = torch.empty((M, I2 // 2), dtype=torch.float16, device=gate_up.device)
     _check(lib().laq_silu_mul_f16(_ptr(gate_up), _ptr(out), M, I2 // 2, _stream(gate_up.device)))
     return out
+
+
+# ---------------------------------------------------------------------------
+# batched serving: paged caches, sampling (head dimension 128)
+# ---------------------------------------------------------------------------
+def _on(device):
+    """Makes `device` the current one for a launch on its stream (a no-op where
+    it already is)."""
+    import contextlib
+
+    import torch
+    if torch.cuda.current_device() == device.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T):
+    import torch
+    assert k_pages.is_cuda and k_pages.dtype == torch.float16 and v_pages.dtype == torch.float16
+    assert k_pages.dim() == 4 and k_pages.shape[3] == HEAD_DIM and k_pages.stride(3) == 1
+    assert v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
+    assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.stride(1) == 1
+    B = seq_len.numel()
+    assert token_start.dtype == torch.int32 and token_start.is_contiguous() and token_start.numel() == B + 1
+    assert seq_len.dtype == torch.int32 and seq_len.is_contiguous() and page_table.shape[0] == B
+    dev = k_pages.device
+    assert v_pages.device == dev and page_table.device == dev and token_start.device == dev and seq_len.device == dev
+    num_pages, _, page_size, _ = k_pages.shape
+    # a dimension of one element has any stride; the library wants a real one
+    page_stride, head_stride, slot_stride = (s if n > 1 else max(s, HEAD_DIM)
+                                             for s, n in zip(k_pages.stride(), k_pages.shape[:3]))
+    return PagedBatch(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), token_start.data_ptr(),
+                      seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, slot_stride,
+                      page_table.shape[1], page_table.stride(0), B, T)
+
+
+def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, page_table, token_start, seq_len, Hq,
+                 eps, q_out=None):
+    """qk_norm_rope for the rows of several sequences with paged caches: fp16
+    qkv [T][(Hq + 2 Hkv) * 128] (rows may be strided) -> normalized, rotated q
+    (returned, fp16 [T][Hq][128]); k and v written to the rows' places.
+
+    k_pages / v_pages fp16 [num_pages][Hkv][page_size][128], of any strides
+    with contiguous rows of 128 (a transposed [num_pages][page_size][Hkv][128]
+    for instance); page_table int32 [B][pages], token_start int32 [B + 1],
+    seq_len int32 [B] (the new rows included), as laq_paged_batch of
+    include/laq.h describes them.  q_norm_weight / k_norm_weight fp16 [128] or
+    None.  cos_sin fp32 [positions][128] (decode.rope_table)."""
+    import torch
+    T = qkv.shape[0]
+    Hkv = k_pages.shape[1]
+    dev = qkv.device
+    assert qkv.is_cuda and qkv.dtype == torch.float16 and qkv.dim() == 2 and qkv.stride(1) == 1
+    assert qkv.shape[1] == (Hq + 2 * Hkv) * HEAD_DIM and k_pages.device == dev
+    assert cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.shape[1] == HEAD_DIM
+    assert cos_sin.is_contiguous() and cos_sin.device == dev
+    for w in (q_norm_weight, k_norm_weight):
+        if w is not None:
+            assert w.dtype == torch.float16 and w.numel() == HEAD_DIM and w.is_contiguous() and w.device == dev
+    if q_out is None:
+        q_out = torch.zeros((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+    else:
+        assert q_out.dtype == torch.float16 and q_out.shape == (T, Hq, HEAD_DIM) and q_out.is_contiguous()
+        assert q_out.device == dev
+    batch = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
+    with _on(dev):
+        _check(lib().laq_paged_append_f16(
+            batch, qkv.data_ptr(), qkv.stride(0) if T > 1 else qkv.shape[1],
+            None if q_norm_weight is None else q_norm_weight.data_ptr(),
+            None if k_norm_weight is None else k_norm_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0], Hq, Hkv,
+            HEAD_DIM, float(eps), q_out.data_ptr(), _stream(dev)))
+    return q_out
+
+
+@functools.lru_cache(maxsize=4096)
+def paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity):
+    """Workspace of paged_attention for B sequences and T rows, of any lengths
+    up to capacity = pages of a table row x page_size."""
+    return int(lib().laq_paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity))
+
+
+def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, window=0, out=None, workspace=None):
+    """Causal attention of the rows of several sequences over their paged
+    caches (after paged_append): fp16 q [T][Hq][128] -> fp16 [T][Hq][128].
+    window > 0: a row sees its own and the window - 1 positions before it.
+    The cache and the batch as for paged_append.  workspace: uint8, at least
+    paged_attention_workspace_bytes; taken from torch's allocator on the
+    current stream when not given."""
+    import torch
+    dev = q.device
+    assert q.is_cuda and q.dtype == torch.float16 and q.dim() == 3 and q.shape[2] == HEAD_DIM and q.is_contiguous()
+    assert k_pages.device == dev
+    T, Hq, _ = q.shape
+    Hkv = k_pages.shape[1]
+    batch = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
+    if out is None:
+        out = torch.zeros((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+    else:
+        assert out.dtype == torch.float16 and out.shape == q.shape and out.is_contiguous() and out.device == dev
+    nbytes = 0
+    if workspace is None:
+        nbytes = paged_attention_workspace_bytes(batch.B, T, Hq, Hkv, batch.table_pages * batch.page_size)
+        if nbytes:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        assert workspace.device == dev and workspace.is_contiguous()
+        nbytes = workspace.numel() * workspace.element_size()
+    with _on(dev):
+        _check(lib().laq_paged_attention_f16(batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, int(window), out.data_ptr(),
+                                             None if workspace is None else workspace.data_ptr(), nbytes,
+                                             _stream(dev)))
+    return out
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None, probs=None):
+    """Draws a token per row of fp16 logits [rows][V] (rows may be strided) by
+    the uniform numbers u (fp32 [rows]) -> (tokens int32 [rows], probabilities
+    fp32 [rows] among what was kept).  temperature, top_p, min_p fp32 [rows],
+    top_k int32 [rows], or None; laq_sample_f16 of include/laq.h defines them."""
+    import torch
+    assert logits.is_cuda and logits.dtype == torch.float16 and logits.dim() == 2 and logits.stride(1) == 1
+    rows, V = logits.shape
+    dev = logits.device
+    assert u.dtype == torch.float32
+    assert top_k is None or top_k.dtype == torch.int32
+    if out is None:
+        out = torch.empty((rows,), dtype=torch.int32, device=dev)
+    if probs is None:
+        probs = torch.empty((rows,), dtype=torch.float32, device=dev)
+    assert out.dtype == torch.int32
+    for t in (temperature, top_p, min_p, probs):
+        assert t is None or t.dtype == torch.float32
+    ptr = []
+    for t in (u, temperature, top_k, top_p, min_p, out, probs):
+        assert t is None or (t.numel() == rows and t.is_contiguous() and t.device == dev)
+        ptr.append(None if t is None else t.data_ptr())
+    with _on(dev):
+        _check(lib().laq_sample_f16(logits.data_ptr(), logits.stride(0) if rows > 1 else V, rows, V, *ptr,
+                                    _stream(dev)))
+    return out, probs
