@@ -70,10 +70,30 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
   return v + (lane >= 16 ? t0 : 0) + (lane >= 32 ? t1 : 0) + (lane >= 48 ? t2 : 0);
 }
 // Sum over the 64 lanes of whole numbers below 2^53 (exact in any order).
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)u, 0), hi = (uint32_t)dpp_i<CTRL>((int)(u >> 32), 0);
+  return __builtin_bit_cast(double, hi << 32 | lo);
+}
+__device__ __forceinline__ double lane_d(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)readlane((int)(u >> 32), l) << 32 |
+                                        (uint32_t)readlane((int)(uint32_t)u, l));
+}
 __device__ __forceinline__ double wave_sum_exact(double v) {
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) v += __shfl_xor(v, s);
-  return v;
+  v += dpp_d<0xB1>(v);
+  v += dpp_d<0x4E>(v);
+  v += dpp_d<0x141>(v);
+  v += dpp_d<0x140>(v);
+  return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
+}
+__device__ __forceinline__ int wave_sum(int v) {
+  v += dpp_i<0xB1>(v, 0);
+  v += dpp_i<0x4E>(v, 0);
+  v += dpp_i<0x141>(v, 0);
+  v += dpp_i<0x140>(v, 0);
+  return (readlane(v, 0) + readlane(v, 16)) + (readlane(v, 32) + readlane(v, 48));
 }
 
 // ---------------------------------------------------------------------------
@@ -248,8 +268,21 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, 
   }
   Item it;
   it.found = false;
+  // The smallest chunk by that bound, then up to a third larger until the items
+  // are no more than the blocks that run at once (a few more would run alone).
   const double share = total * Hkv * (1.0 / kItems<BM>);
-  it.chunk = uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
+  const int least = uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
+  it.chunk = least;
+  if (pb.B <= 64) {
+    for (int i = 0; i < 4; ++i) {
+      const int c = least + least * i / 8 + (i > 0);
+      if (wave_sum(q.tiles * ((q.units + c - 1) / c)) * Hkv <= kItems<BM>) {
+        it.chunk = c;
+        break;
+      }
+    }
+    it.chunk = uniform(it.chunk);
+  }
   int items = 0, recs = 0;
   for (int b0 = 0; b0 < pb.B; b0 += 64) {
     if (b0 > 0) q = load_seq<BM>(pb, b0 + lane, R, window);
@@ -271,8 +304,10 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, 
       it.splits = readlane(splits, l);
       const int i = idx - readlane(upto - own, l);
       // the last tiles of a prompt see the most positions: they go first
-      it.tile = readlane(q.tiles, l) - 1 - (SPLIT ? i : i / it.splits);
-      it.split = SPLIT ? 0 : i % it.splits;
+      // (divisions of uniform values are vector instructions: their results are made uniform again)
+      const int back = SPLIT ? i : uniform(i / it.splits);
+      it.tile = readlane(q.tiles, l) - 1 - back;
+      it.split = SPLIT ? 0 : i - back * it.splits;
       it.rec = readlane(rupto - rec, l) + it.tile * it.splits;
       return it;
     }
@@ -304,12 +339,11 @@ __device__ __forceinline__ Span span_of(const Item& it, int j0, int j1, int wind
 // past its extent and read as zeros.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows16(const PagedBatch& pb, const uint16_t* base, int g, int page,
                                                          int t, int end) {
-  const bool there = (unsigned)page < (unsigned)pb.num_pages && t < end;
-  const int64_t at = (int64_t)(there ? page : 0) * pb.page_stride + g * pb.head_stride +
+  const uint32_t there = ((unsigned)page < (unsigned)pb.num_pages) & (t < end);  // (arithmetic, so that no branch is made)
+  const int64_t at = (int64_t)page * pb.page_stride + g * pb.head_stride +
                      (int64_t)(t & ((1 << pb.page_shift) - 1)) * pb.slot_stride;
-  const int rows = min(end - t, 16);
-  const uint32_t bytes = there ? (uint32_t)((rows - 1) * pb.slot_stride + kHeadDim) * 2 : 0;
-  return rsrc(base + (there ? at : 0), bytes);
+  const uint32_t bytes = (uint32_t)((min(end - t, 16) - 1) * pb.slot_stride + kHeadDim) * 2;
+  return rsrc(base + (at & -(int64_t)there), bytes & -there);
 }
 
 // Bits of the halves of x that are infinite or NaN: 0x8000 in each.
@@ -365,7 +399,7 @@ __device__ __forceinline__ void lds_put(uint32_t addr, float v) {
   asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory");
 }
 
-__global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(PagedBatch pb,
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(PagedBatch pb,
                                                                              const uint16_t* __restrict__ q, int R,
                                                                              int Hkv, int window, Out o_) {
   typedef __attribute__((address_space(3))) void lds_void;
@@ -374,12 +408,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(Pag
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int n = lane & 15, j = lane >> 4;
-  const int g = uniform(blockIdx.x % Hkv);
-  const Item it = find_item<kSmallRows, false>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
+  const Item it = find_item<kSmallRows, false>(pb, at_item, R, Hkv, window, lane);
   if (!it.found) return;
   const int rows = min(it.n * R - it.tile * kSmallRows, kSmallRows);
   const int r0 = it.tile * kSmallRows;
-  const Span sp = span_of(it, r0 / R, (r0 + rows - 1) / R, window);
+  const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
 
   // q as matrix operand: lane (m, j), window i: dimensions 32 i + 8 j .. + 7 of row m.
   u32x4 qa[4];
@@ -452,7 +486,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(Pag
     __builtin_amdgcn_sched_barrier(0);
     wait_vmcnt<(MORE ? 3 : 1) * kLoads>();  // the keys: this step's values and the next step's loads may be outstanding
     __builtin_amdgcn_sched_barrier(0);
-    const bool masked = bad[B] != 0 || p < sp.all_lo || p + kStep > sp.all_hi || p + kStep > sp.hi;
+    const bool masked = (bad[B] != 0) | (p < sp.all_lo) | (p + kStep > sp.all_hi) | (p + kStep > sp.hi);
     float sc[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -470,9 +504,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(Pag
       for (int r = 0; r < 4; ++r) sc[t][r] = cc[r] * kScaleLog2;
       if (masked) {
         const int at = p + 16 * t + n;
-        const bool there = at < sp.hi && !(bad[B] >> t & 1);
+        const bool there = (at < sp.hi) & !(bad[B] >> t & 1);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sc[t][r] = there && at >= see_lo[r] && at < see_hi[r] ? sc[t][r] : -INFINITY;
+        for (int r = 0; r < 4; ++r) sc[t][r] = (there & (at >= see_lo[r]) & (at < see_hi[r])) ? sc[t][r] : -INFINITY;
       }
     }
     float alpha[4];
@@ -505,9 +539,13 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(Pag
       if (__ballot(nf != 0)) {
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
+#pragma unroll 1
           for (int jt = 0; jt < 4; ++jt) {
             const int at = p + 16 * (k >> 2) + 4 * jt + (k & 3);
-            const bool there = at < sp.hi && !(bad[B] >> (k >> 2) & 1);
+            const bool there = (at < sp.hi) & !(bad[B] >> (k >> 2) & 1);
+            bool sees[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sees[r] = there & (at >= see_lo[r]) & (at < see_hi[r]);
             u32x4 x;
 #pragma unroll
             for (int d = 0; d < 4; ++d) x[d] = __shfl(vv[B][k][d], 16 * jt + n);
@@ -515,10 +553,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_rows16_kernel(Pag
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float f = (float)v[e];
-              const bool add = there && !(fabsf(f) < INFINITY);
+              const float add = fabsf(f) < INFINITY ? 0.0f : f;
 #pragma unroll
-              for (int r = 0; r < 4; ++r)
-                o[e][r] += add && at >= see_lo[r] && at < see_hi[r] ? f : 0.0f;
+              for (int r = 0; r < 4; ++r) o[e][r] += sees[r] ? add : 0.0f;
             }
           }
         }
@@ -641,12 +678,12 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
   const int lane = tid & 63;
   const int w = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const int g = uniform(blockIdx.x % Hkv);
-  const Item it = find_item<kLargeRows, false>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
+  const Item it = find_item<kLargeRows, false>(pb, at_item, R, Hkv, window, lane);
   if (!it.found) return;
   const int r0 = it.tile * kLargeRows;
   const int rows = min(it.n * R - r0, kLargeRows);
-  const Span sp = span_of(it, r0 / R, (r0 + rows - 1) / R, window);
+  const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
 
   // This lane's query row and what it sees; its operand: dimensions 16 s + 8 h .. + 7.
   const int my = 32 * w + n;
@@ -659,7 +696,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
   // Tiles beyond these no row of the wave sees.
   int wave_lo, wave_hi;
   {
-    const int j0 = (r0 + min(32 * w, rows - 1)) / R, j1 = (r0 + min(32 * w + 31, rows - 1)) / R;
+    const int j0 = uniform((r0 + min(32 * w, rows - 1)) / R), j1 = uniform((r0 + min(32 * w + 31, rows - 1)) / R);
     wave_lo = window > 0 ? it.pos0 + j0 - window + 1 : 0;
     wave_hi = 32 * w < rows ? it.pos0 + j1 + 1 : 0;
   }
@@ -691,7 +728,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
     }
   };
   auto is_masked = [&](int t0, int bad_groups) {
-    return bad_groups != 0 || t0 < sp.all_lo || t0 + kTile > sp.all_hi || t0 + kTile > sp.hi;
+    return (bad_groups != 0) | (t0 < sp.all_lo) | (t0 + kTile > sp.all_hi) | (t0 + kTile > sp.hi);
   };
   auto store_tile = [&](int B, int t0) {
     char* const kd = lds + B * 2 * kTileBytes;
@@ -719,6 +756,9 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
 
   auto compute = [&](auto mc, int B, int t0, int bad_groups) {
     constexpr bool MASKED = decltype(mc)::value;
+    // (the two forms share no code: what the compiler moved out of both would be held in registers beyond 256)
+    if constexpr (MASKED) asm volatile("; masked" ::: "memory");
+    else asm volatile("; whole" ::: "memory");
     const char* const kd = lds + B * 2 * kTileBytes;
     const char* const vd = kd + kTileBytes;
     float16_t s[2];
@@ -738,8 +778,8 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int at = t0 + 32 * kt + 8 * (r >> 2) + 4 * h + (r & 3);
-          const bool there = !(bad_groups >> (2 * kt + (r >> 3)) & 1) && at < sp.hi;
-          s[kt][r] = there && at >= see_lo && at < see_hi ? s[kt][r] : -INFINITY;
+          const bool there = !(bad_groups >> (2 * kt + (r >> 3)) & 1) & (at < sp.hi);
+          s[kt][r] = (there & (at >= see_lo) & (at < see_hi)) ? s[kt][r] : -INFINITY;
         }
     }
     float mx = s[0][0];
@@ -802,20 +842,25 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
       // Values that are infinite or NaN were left out of the product (0 times
       // one is NaN): the rows that see one receive it here, whatever its weight.
       if (nf) {
-        for (int t = 0; t < kTile; ++t) {
-          const int at = t0 + t;
-          const bool sees = at < sp.hi && !(bad_groups >> (t >> 4) & 1) && at >= see_lo && at < see_hi;
+        typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-          for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int dim = 32 * d + 8 * (r >> 2) + 4 * h + (r & 3);
-              const _Float16 x = *reinterpret_cast<const _Float16*>(vd + t * 256 + 16 * ((dim >> 3) ^ (4 * (t & 3))) +
-                                                                    2 * (dim & 7));
-              const float f = (float)x;
-              o[d][r] += sees && !(fabsf(f) < INFINITY) ? f : 0.0f;
+          for (int r = 0; r < 16; r += 4) {
+            const int piece = 4 * d + (r >> 2);
+#pragma unroll 1
+            for (int t = 0; t < kTile; ++t) {
+              const int at = t0 + t;
+              const bool sees =
+                  (at < sp.hi) & !(bad_groups >> (t >> 4) & 1) & (at >= see_lo) & (at < see_hi);
+              const half4_t x = *reinterpret_cast<const half4_t*>(vd + t * 256 + 16 * (piece ^ (4 * (t & 3))) + 8 * h);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float add = fabsf((float)x[e]) < INFINITY ? 0.0f : (float)x[e];
+                o[d][r + e] += sees ? add : 0.0f;
+              }
             }
-        }
+          }
       }
     }
   };
@@ -880,42 +925,74 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
     }
 }
 
-// Joins the ranges of the split tiles in position order: block (split tile,
-// key/value head, 16 rows of the tile), a wave per four rows, a lane per two
-// dimensions.  A row's records are weighted by 2^(their maximum - the largest).
-template <int BM>
+// Joins the ranges of the split tiles in position order: a wave takes every
+// WAVES-th record of a row, a lane two dimensions, and the waves of a row meet
+// in LDS.  Records are weighted by 2^(their maximum - the largest of all).
+// Few rows have many records (decoding a long sequence): four waves a row;
+// the rows of a chunk have few: a wave a row, four rows a block.
+template <int BM, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
+  __shared__ float2_t part[4][64];
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
-  const int g = uniform(blockIdx.x % Hkv);
-  const Item it = find_item<BM, true>(pb, uniform(blockIdx.x / Hkv), R, Hkv, window, lane);
+  const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
+  const Item it = find_item<BM, true>(pb, at_item, R, Hkv, window, lane);
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
   constexpr int kRec = BM * (kHeadDim + 2);
+  const int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + w;
+  if (WAVES == 4 && row >= rows) return;
+  const int row_c = min(row, rows - 1);
   const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
-  for (int i = 0; i < 4; ++i) {
-    const int row = blockIdx.y * 16 + w * 4 + i;
-    if (row >= rows) break;
-    const float* const stat = base + BM * kHeadDim + 2 * row;
-    float M = kNoMax;
-    for (int s = lane; s < it.splits; s += 64) M = fmaxf(M, stat[(int64_t)s * kRec]);
+  const float* const stat = base + BM * kHeadDim + 2 * row_c;
+  const float* const sums = base + row_c * kHeadDim + 2 * lane;
+  const int first = WAVES == 4 ? w : 0;
+  constexpr int kB = 8;
+  float2_t x[kB], st[kB];
+  auto load = [&](int s0) {
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) M = fmaxf(M, __shfl_xor(M, x));
-    float den = 0.0f;
-    float2_t num = {0.0f, 0.0f};
-    for (int s = 0; s < it.splits; ++s) {
-      const float e = __builtin_amdgcn_exp2f(stat[(int64_t)s * kRec] - M);
-      const float2_t x = *reinterpret_cast<const float2_t*>(base + (int64_t)s * kRec + row * kHeadDim + 2 * lane);
-      den = fmaf(e, stat[(int64_t)s * kRec + 1], den);
-      num[0] = fmaf(e, x[0], num[0]);
-      num[1] = fmaf(e, x[1], num[1]);
+    for (int i = 0; i < kB; ++i) {
+      const int64_t s = min(s0 + WAVES * i, it.splits - 1);
+      st[i] = *reinterpret_cast<const float2_t*>(stat + s * kRec);
+      x[i] = *reinterpret_cast<const float2_t*>(sums + s * kRec);
     }
-    const int r = r0 + row;
-    const float y0 = den > 0.0f ? num[0] / den : 0.0f, y1 = den > 0.0f ? num[1] / den : 0.0f;
-    *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
-        half2_t{(_Float16)y0, (_Float16)y1};
+  };
+  load(first);  // before the statistics: records of up to 32 ranges cost one memory round trip
+  float M = kNoMax, den = 0.0f;
+  for (int s0 = 0; s0 < it.splits; s0 += 64) {
+    const int s = s0 + lane;
+    const float2_t y = *reinterpret_cast<const float2_t*>(stat + (int64_t)min(s, it.splits - 1) * kRec);
+    const float top = fmaxf(M, row_max(y[0]));
+    const float all = fmaxf(fmaxf(__shfl(top, 0), __shfl(top, 16)), fmaxf(__shfl(top, 32), __shfl(top, 48)));
+    const float part_den = row_sum(s < it.splits ? __builtin_amdgcn_exp2f(y[0] - all) * y[1] : 0.0f);
+    den = den * __builtin_amdgcn_exp2f(M - all) +
+          ((__shfl(part_den, 0) + __shfl(part_den, 16)) + (__shfl(part_den, 32) + __shfl(part_den, 48)));
+    M = all;
   }
+  float2_t num = {0.0f, 0.0f};
+  for (int s0 = first; s0 < it.splits; s0 += WAVES * kB) {
+    if (s0 > first) load(s0);
+#pragma unroll
+    for (int i = 0; i < kB; ++i) {
+      const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[i][0] - M) : 0.0f;
+      num[0] = fmaf(e, x[i][0], num[0]);
+      num[1] = fmaf(e, x[i][1], num[1]);
+    }
+  }
+  if constexpr (WAVES == 4) {
+    part[w][lane] = num;
+    __syncthreads();
+    if (w > 0) return;
+    num = part[0][lane];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) num += part[i][lane];
+  }
+  if (row >= rows) return;
+  const int r = r0 + row;
+  const float inv = den > 0.0f ? 1.0f / den : 0.0f;
+  *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
+      half2_t{(_Float16)(num[0] * inv), (_Float16)(num[1] * inv)};
 }
 
 // Which kernel takes a batch, and its bounds: a pure function of the sizes.
@@ -977,18 +1054,19 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
     e2.stop = ev.stop;
   }
   const Out o{out, ws, (int)Hq, (int)p.records};
-  const dim3 grid((unsigned)(p.items * Hkv)), join((unsigned)(p.split_tiles * Hkv), p.large ? kLargeRows / 16 : 1);
+  const dim3 grid((unsigned)(p.items * Hkv)), join((unsigned)(p.split_tiles * Hkv),
+                                                              p.large ? kLargeRows / 4 : std::min<int64_t>(kSmallRows, pb.T * R));
   if (p.large) {
     launch(paged_attention_rows128_kernel, grid, dim3(256), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv, (int)window,
            o);
     if (p.split_tiles > 0)
-      launch(paged_attention_join_kernel<kLargeRows>, join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
+      launch((paged_attention_join_kernel<kLargeRows, 1>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
              o);
   } else {
     launch(paged_attention_rows16_kernel, grid, dim3(64 * kWaves), kSmallLds, stream, e1, pb, q, (int)R, (int)Hkv,
            (int)window, o);
     if (p.split_tiles > 0)
-      launch(paged_attention_join_kernel<kSmallRows>, join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
+      launch((paged_attention_join_kernel<kSmallRows, 4>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
              o);
   }
   return hipGetLastError();
