@@ -222,7 +222,7 @@ constexpr int kSmallRows = 16, kLargeRows = 128;
 template <int BM>
 constexpr int kItems = BM == kSmallRows ? 512 : 512;
 template <int BM>
-constexpr int kMinChunk = BM == kSmallRows ? 4 : 4;  // units: a shorter range costs more in records than it gains
+constexpr int kMinChunk = BM == kSmallRows ? 2 : 4;  // units: a shorter range costs more in records than it gains
 
 // One sequence, seen from one lane.
 struct Seq {
@@ -382,6 +382,10 @@ constexpr int kStep = 32;
 constexpr int kStride = kWaves * kStep;
 constexpr int kRowBytes = (kStep + 4) * 4;         // a row of probabilities (4 words of padding)
 constexpr int kKeyBytes = kStep * kHeadDim * 2;    // a step's keys
+// Keys and values pass once: loads that do not keep their lines (measured on
+// MI355X, three sequences of 131072, 77777 and 901 positions, 64:8 heads: 167 ->
+// 151 us; 16 sequences of up to 8192, 32:8: 44 -> 39).
+constexpr int kStreamed = 2;
 constexpr int kSmallLds = kWaves * (2 * kKeyBytes + 16 * kRowBytes);
 
 __device__ __forceinline__ void lds_read4(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
@@ -457,7 +461,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
       const int r = 4 * i + j;
       const __amdgpu_buffer_rsrc_t kr = rows16(pb, pb.k, g, pg[i >> 2], p + 16 * (i >> 2), sp.hi);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(keys + B * kKeyBytes + i * 1024), 16,
-                                               (uint32_t)(r & 15) * pb.slot_stride * 2 + 16 * (n ^ (r & 15)), 0, 0, 0);
+                                               (uint32_t)(r & 15) * pb.slot_stride * 2 + 16 * (n ^ (r & 15)), 0, 0, kStreamed);
     }
     __builtin_amdgcn_sched_barrier(0);  // the keys' wait below counts the values' loads as the later ones
     // values of step k = 4 kk + i: positions 16 kk + 4 j + i
@@ -465,7 +469,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
     for (int k = 0; k < kLoads; ++k) {
       const __amdgpu_buffer_rsrc_t vr = rows16(pb, pb.v, g, pg[k >> 2], p + 16 * (k >> 2), sp.hi);
       vv[B][k] =
-          __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(4 * j + (k & 3)) * pb.slot_stride * 2 + 16 * n, 0, 0);
+          __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(4 * j + (k & 3)) * pb.slot_stride * 2 + 16 * n, 0,
+                                                kStreamed);
     }
     __builtin_amdgcn_sched_barrier(0);
   };
@@ -925,14 +930,18 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
     }
 }
 
-// Joins the ranges of the split tiles in position order: a wave takes every
-// WAVES-th record of a row, a lane two dimensions, and the waves of a row meet
-// in LDS.  Records are weighted by 2^(their maximum - the largest of all).
-// Few rows have many records (decoding a long sequence): four waves a row;
-// the rows of a chunk have few: a wave a row, four rows a block.
+// Joins the ranges of the split tiles in position order.  Records are weighted
+// by 2^(their maximum - the largest of all); a lane holds two dimensions.
+// WAVES == 4: a block per row, its waves take every fourth record and meet in
+// LDS (decoding: few rows, many ranges).  WAVES == 1: a wave per four rows,
+// 16 rows a block (a chunk's rows have few ranges each, and most blocks of the
+// grid find nothing to do: they cost their search).
 template <int BM, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
+  constexpr int kRec = BM * (kHeadDim + 2);
+  constexpr int kRows = WAVES == 4 ? 1 : 4;  // rows of a wave
+  constexpr int kB = WAVES == 4 ? 8 : 4;     // records loaded at a time
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
@@ -940,59 +949,76 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
-  constexpr int kRec = BM * (kHeadDim + 2);
-  const int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 4 + w;
-  if (WAVES == 4 && row >= rows) return;
-  const int row_c = min(row, rows - 1);
-  const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
-  const float* const stat = base + BM * kHeadDim + 2 * row_c;
-  const float* const sums = base + row_c * kHeadDim + 2 * lane;
+  const int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4;
+  if (row >= rows) return;  // WAVES == 4: the whole block
   const int first = WAVES == 4 ? w : 0;
-  constexpr int kB = 8;
-  float2_t x[kB], st[kB];
+  const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
+  const float *stat[kRows], *sums[kRows];
+  float2_t x[kRows][kB], st[kRows][kB], num[kRows];
+  float M[kRows], den[kRows];
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    const int r = min(row + k, rows - 1);
+    stat[k] = base + BM * kHeadDim + 2 * r;
+    sums[k] = base + r * kHeadDim + 2 * lane;
+    num[k] = float2_t{0.0f, 0.0f};
+    M[k] = kNoMax, den[k] = 0.0f;
+  }
   auto load = [&](int s0) {
 #pragma unroll
-    for (int i = 0; i < kB; ++i) {
-      const int64_t s = min(s0 + WAVES * i, it.splits - 1);
-      st[i] = *reinterpret_cast<const float2_t*>(stat + s * kRec);
-      x[i] = *reinterpret_cast<const float2_t*>(sums + s * kRec);
-    }
+    for (int k = 0; k < kRows; ++k)
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        const int64_t s = min(s0 + WAVES * i, it.splits - 1);
+        st[k][i] = *reinterpret_cast<const float2_t*>(stat[k] + s * kRec);
+        x[k][i] = *reinterpret_cast<const float2_t*>(sums[k] + s * kRec);
+      }
   };
-  load(first);  // before the statistics: records of up to 32 ranges cost one memory round trip
-  float M = kNoMax, den = 0.0f;
+  load(first);  // before the statistics: up to WAVES * kB ranges cost one memory round trip
+  auto over_rows = [](float v, auto&& op) {  // of a value per 16-lane row
+    const int u = __builtin_bit_cast(int, v);
+    auto f = [](int x) { return __builtin_bit_cast(float, x); };
+    return op(op(f(readlane(u, 0)), f(readlane(u, 16))), op(f(readlane(u, 32)), f(readlane(u, 48))));
+  };
   for (int s0 = 0; s0 < it.splits; s0 += 64) {
-    const int s = s0 + lane;
-    const float2_t y = *reinterpret_cast<const float2_t*>(stat + (int64_t)min(s, it.splits - 1) * kRec);
-    const float top = fmaxf(M, row_max(y[0]));
-    const float all = fmaxf(fmaxf(__shfl(top, 0), __shfl(top, 16)), fmaxf(__shfl(top, 32), __shfl(top, 48)));
-    const float part_den = row_sum(s < it.splits ? __builtin_amdgcn_exp2f(y[0] - all) * y[1] : 0.0f);
-    den = den * __builtin_amdgcn_exp2f(M - all) +
-          ((__shfl(part_den, 0) + __shfl(part_den, 16)) + (__shfl(part_den, 32) + __shfl(part_den, 48)));
-    M = all;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int s = s0 + lane;
+      const float2_t y = *reinterpret_cast<const float2_t*>(stat[k] + (int64_t)min(s, it.splits - 1) * kRec);
+      const float top = fmaxf(M[k], over_rows(row_max(y[0]), [](float a, float b) { return fmaxf(a, b); }));
+      const float sum = over_rows(row_sum(s < it.splits ? __builtin_amdgcn_exp2f(y[0] - top) * y[1] : 0.0f),
+                                  [](float a, float b) { return a + b; });
+      den[k] = fmaf(den[k], __builtin_amdgcn_exp2f(M[k] - top), sum);
+      M[k] = top;
+    }
   }
-  float2_t num = {0.0f, 0.0f};
   for (int s0 = first; s0 < it.splits; s0 += WAVES * kB) {
     if (s0 > first) load(s0);
 #pragma unroll
-    for (int i = 0; i < kB; ++i) {
-      const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[i][0] - M) : 0.0f;
-      num[0] = fmaf(e, x[i][0], num[0]);
-      num[1] = fmaf(e, x[i][1], num[1]);
-    }
+    for (int k = 0; k < kRows; ++k)
+#pragma unroll
+      for (int i = 0; i < kB; ++i) {
+        const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[k][i][0] - M[k]) : 0.0f;
+        num[k][0] = fmaf(e, x[k][i][0], num[k][0]);
+        num[k][1] = fmaf(e, x[k][i][1], num[k][1]);
+      }
   }
   if constexpr (WAVES == 4) {
-    part[w][lane] = num;
+    part[w][lane] = num[0];
     __syncthreads();
     if (w > 0) return;
-    num = part[0][lane];
+    num[0] = part[0][lane];
 #pragma unroll
-    for (int i = 1; i < 4; ++i) num += part[i][lane];
+    for (int i = 1; i < 4; ++i) num[0] += part[i][lane];
   }
-  if (row >= rows) return;
-  const int r = r0 + row;
-  const float inv = den > 0.0f ? 1.0f / den : 0.0f;
-  *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
-      half2_t{(_Float16)(num[0] * inv), (_Float16)(num[1] * inv)};
+#pragma unroll
+  for (int k = 0; k < kRows; ++k) {
+    if (row + k >= rows) break;
+    const int r = r0 + row + k;
+    const float inv = den[k] > 0.0f ? 1.0f / den[k] : 0.0f;
+    *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
+        half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
+  }
 }
 
 // Which kernel takes a batch, and its bounds: a pure function of the sizes.
@@ -1055,7 +1081,7 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
   }
   const Out o{out, ws, (int)Hq, (int)p.records};
   const dim3 grid((unsigned)(p.items * Hkv)), join((unsigned)(p.split_tiles * Hkv),
-                                                              p.large ? kLargeRows / 4 : std::min<int64_t>(kSmallRows, pb.T * R));
+                                                              p.large ? kLargeRows / 16 : std::min<int64_t>(kSmallRows, pb.T * R));
   if (p.large) {
     launch(paged_attention_rows128_kernel, grid, dim3(256), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv, (int)window,
            o);

@@ -10,6 +10,12 @@
 // of one per token, and in 64 bits (a running sum over 150 000 tokens in 32
 // bits moves a border by whole tokens).  Counting is in whole numbers, sums
 // are added in a fixed order: the same token on every call.
+//
+// One block of 1024 threads per row, the logits in its registers (read once).
+// What bounds a row: the passes over its logits, about a microsecond of one
+// compute unit per vector instruction and 150 000 logits; so the logits are
+// turned into sortable numbers in place, two per instruction, and the
+// histogram holds two 16-bit counts per LDS word (all 65536 values in 128 KiB).
 #include <limits.h>
 #include <math.h>
 
@@ -21,33 +27,90 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWavesS = kThreads / 64;
-constexpr int kBins = 32768;                    // values counted at a time, 128 KiB of the compute unit's LDS
-constexpr int kPer = kBins / kThreads;          // consecutive bins of a thread
-constexpr uint32_t kLowest = 0x03FF;            // key of -inf
-constexpr int kSampleLds = kBins * 4 + 1024;
+constexpr int kWords = 32768;           // histogram words: values >= 0 in the upper halves, < 0 in the lower
+constexpr int kLines = 1024;            // 64 values each, in falling order
+constexpr int kLowest = -31745;         // sortable number of -inf (and of NaN)
+constexpr int kHighest = 31744;         // of +inf
+
+typedef short short2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// Order-preserving 16-bit key of a logit; NaN counts as -inf, -0 as 0.
-__device__ __forceinline__ uint32_t key_of(uint32_t h) {
-  const uint32_t k = h == 0x8000u ? 0x8000u : (h & 0x8000u) ? (~h & 0xFFFFu) : (h | 0x8000u);
-  return k > 0xFC00u || k < kLowest ? kLowest : k;
+// Sortable numbers of two logits: a larger logit has a larger 16-bit integer;
+// -0 is -1, +0 is 0, negative NaN lie below -inf and positive ones above +inf.
+__device__ __forceinline__ uint32_t sortable(uint32_t x) {
+  const short2_t s = __builtin_bit_cast(short2_t, x) >> 15;
+  return x ^ (__builtin_bit_cast(uint32_t, s) & 0x7FFF7FFFu);
 }
-__device__ __forceinline__ double logit_of(uint32_t key) {
-  const uint32_t h = (key & 0x8000u) ? (key & 0x7FFFu) : (~key & 0xFFFFu);
-  return (double)__builtin_bit_cast(_Float16, (uint16_t)h);
+__device__ __forceinline__ int half_of(uint32_t x, int e) { return (int)(short)(uint16_t)(e ? x >> 16 : x); }
+__device__ __forceinline__ double logit_of(int k) {
+  const uint16_t h = (uint16_t)(k < 0 ? k ^ 0x7FFF : k);
+  return (double)__builtin_bit_cast(_Float16, h);
+}
+// Values in falling order: place b = 32767 - k, line b / 64.
+__device__ __forceinline__ int place_of(int k) { return 32767 - k; }
+__device__ __forceinline__ int value_at(int b) { return 32767 - b; }
+
+// 2^y for y <= 0, to about 2^-50 of it: y = n + f, |f| <= 1/2, and the series
+// of exp(f ln 2), of which the term after the last is below 1e-14.
+__device__ __forceinline__ double exp2_neg(double y) {
+  y = fmax(y, -2000.0);
+  const double n = rint(y);
+  const double f = (y - n) * 0.69314718055994530942;
+  double r = 1.0 / 39916800.0;
+  r = fma(r, f, 1.0 / 3628800.0);
+  r = fma(r, f, 1.0 / 362880.0);
+  r = fma(r, f, 1.0 / 40320.0);
+  r = fma(r, f, 1.0 / 5040.0);
+  r = fma(r, f, 1.0 / 720.0);
+  r = fma(r, f, 1.0 / 120.0);
+  r = fma(r, f, 1.0 / 24.0);
+  r = fma(r, f, 1.0 / 6.0);
+  r = fma(r, f, 0.5);
+  r = fma(r, f, 1.0);
+  r = fma(r, f, 1.0);
+  return ldexp(r, (int)n);
 }
 
-// Bin b (b-th value below the largest) sits at word b with its place within
-// the line of 32 turned by the line: a thread reads a whole line, and the
-// threads of a wave then read different banks.
-__device__ __forceinline__ int bin_word(int b) { return b ^ ((b >> 5) & 31); }
+template <int CTRL>
+__device__ __forceinline__ int dpp_s(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, false);
+}
+__device__ __forceinline__ double lane_double(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(u >> 32), l);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_double(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = dpp_s<CTRL>((int)(uint32_t)u), hi = dpp_s<CTRL>((int)(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive prefix sums over the 64 lanes (shifts within 16-lane rows, lanes
+// shifted in read 0; then the rows' totals).
+__device__ __forceinline__ void wave_scan(double& v, int& c, int lane) {
+  v += dpp_double<0x111>(v), c += dpp_s<0x111>(c);
+  v += dpp_double<0x112>(v), c += dpp_s<0x112>(c);
+  v += dpp_double<0x114>(v), c += dpp_s<0x114>(c);
+  v += dpp_double<0x118>(v), c += dpp_s<0x118>(c);
+  const double t0 = lane_double(v, 15), t1 = t0 + lane_double(v, 31), t2 = t1 + lane_double(v, 47);
+  const int c0 = __builtin_amdgcn_readlane(c, 15), c1 = c0 + __builtin_amdgcn_readlane(c, 31),
+            c2 = c1 + __builtin_amdgcn_readlane(c, 47);
+  v += lane < 16 ? 0.0 : lane < 32 ? t0 : lane < 48 ? t1 : t2;
+  c += lane < 16 ? 0 : lane < 32 ? c0 : lane < 48 ? c1 : c2;
+}
 
 struct SampleShared {
+  double line_w[kLines];
+  int line_c[kLines];
   double wsum[kWavesS], weight;
-  int csum[kWavesS], low[kWavesS];
-  int bin, nth;
+  int csum[kWavesS];
+  int place, nth, found;
 };
+constexpr int kSampleLds = kWords * 4 + (int)sizeof(SampleShared);
+static_assert(kSampleLds <= 160 * 1024, "LDS of a compute unit");
 
 template <int NV>
 __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __restrict__ logits, int64_t stride, int V,
@@ -57,14 +120,13 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
                                                           float* __restrict__ prob) {
   extern __shared__ u32x4 sample_lds[];
   uint32_t* const bins = reinterpret_cast<uint32_t*>(sample_lds);
-  SampleShared& sh = *reinterpret_cast<SampleShared*>(bins + kBins);
-  static_assert(sizeof(SampleShared) <= 1024, "shared results");
+  SampleShared& sh = *reinterpret_cast<SampleShared*>(bins + kWords);
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
   const int row = blockIdx.x;
   const uint16_t* const x = logits + row * stride;
   const int nv = (V + 8 * kThreads - 1) / (8 * kThreads);
 
-  // Eight logits (v * 1024 + tid) * 8 .. + 7 as keys, -inf past the end.
+  // Sortable numbers of the eight logits (v * 1024 + tid) * 8 .. + 7, -inf past the end.
   auto fetch = [&](int v) {
     const int64_t at = ((int64_t)v * kThreads + tid) * 8;
     u32x4 r;
@@ -78,189 +140,229 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     }
     return r;
   };
+  auto to_sortable = [](u32x4 r) { return u32x4{sortable(r.x), sortable(r.y), sortable(r.z), sortable(r.w)}; };
   u32x4 keep[NV > 0 ? NV : 1];
   if constexpr (NV > 0) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) keep[v] = fetch(v);
-  }
-  // f(key, v, e) over this thread's logits.
-  auto each_vector = [&](auto&& f) {
-    if constexpr (NV > 0) {
+    for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int v = 0; v < NV; ++v) f(keep[v], v);
-    } else {
-      for (int v = 0; v < nv; ++v) f(fetch(v), v);
-    }
+    for (int v = 0; v < NV; ++v) keep[v] = to_sortable(keep[v]);
+  } else {
+    for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
+  }
+#define LAQ_EACH_VECTOR(body)                                    \
+  if constexpr (NV > 0) {                                        \
+    _Pragma("unroll") for (int v = 0; v < NV; ++v) body(keep[v], v); \
+  } else {                                                       \
+    for (int v = 0; v < nv; ++v) body(to_sortable(fetch(v)), v);  \
+  }
+  auto block_max = [&](int m) {
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) m = max(m, __shfl_xor(m, s));
+    if (lane == 0) sh.csum[w] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWavesS; ++i) m = max(m, sh.csum[i]);
+    __syncthreads();
+    return uni(m);
   };
-  auto key_at = [](const u32x4& r, int e) { return key_of((r[e >> 1] >> (16 * (e & 1))) & 0xFFFFu); };
 
-  // the largest, and the smallest that is not -inf
-  uint32_t top = 0, low = 0xFFFF;
-  each_vector([&](const u32x4& r, int) {
+  // The largest; positive NaN, which sort above it, are looked for only where there are some.
+  int top;
+  {
+    short2_t m = {-32768, -32768};
+    auto take = [&](const u32x4& r, int) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t k = key_at(r, e);
-      top = max(top, k);
-      low = min(low, k == kLowest ? 0xFFFFu : k);
-    }
-  });
-#pragma unroll
-  for (int s = 32; s >= 1; s >>= 1) {
-    top = max(top, (uint32_t)__shfl_xor((int)top, s));
-    low = min(low, (uint32_t)__shfl_xor((int)low, s));
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = r[i];  // (the cast takes element 0 of a vector element named in it)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(short2_t, two));
+      }
+    };
+    LAQ_EACH_VECTOR(take)
+    top = block_max(max((int)m[0], (int)m[1]));
   }
-  if (lane == 0) sh.csum[w] = (int)top, sh.low[w] = (int)low;
-  __syncthreads();
+  if (top > kHighest) {
+    int m = -32768;
+    auto take = [&](const u32x4& r, int) {
 #pragma unroll
-  for (int i = 0; i < kWavesS; ++i) top = max(top, (uint32_t)sh.csum[i]), low = min(low, (uint32_t)sh.low[i]);
-  top = (uint32_t)uni((int)top);
-  low = (uint32_t)uni((int)low);
-  __syncthreads();
-  if (top == kLowest) {  // nothing allowed
+      for (int e = 0; e < 8; ++e) {
+        const int k = half_of(r[e >> 1], e & 1);
+        m = max(m, k > kHighest ? -32768 : k);
+      }
+    };
+    LAQ_EACH_VECTOR(take)
+    top = block_max(m);
+  }
+  if (top <= kLowest) {  // nothing allowed
     if (tid == 0) {
       token[row] = -1;
       if (prob) prob[row] = 0.0f;
     }
     return;
   }
+  if (top == -1) top = 0;  // -0 counts as 0
+
   const float temp = t_ ? t_[row] : 1.0f;
-  const double largest = logit_of(top);
-  int pick = 0, nth = 0;  // bin of the drawn token, and which of the bin's tokens
+  int pick = place_of(top), nth = 0;  // place of the drawn value, and which of its tokens
   double chance = 1.0;
   if (temp > 0.0f) {
-    const double T = (double)temp;
-    auto weight = [&](int b) { return b == 0 ? 1.0 : exp((logit_of(top - b) - largest) / T); };
+    const double largest = logit_of(top), per = 1.4426950408889634074 / (double)temp;
+    const int first_place = place_of(top);
+    auto weight = [&](int b) { return b <= first_place ? 1.0 : exp2_neg((logit_of(value_at(b)) - largest) * per); };
     const int kk = k_ ? k_[row] : 0;
     const int top_k = kk > 0 ? kk : INT_MAX;
 
-    // This thread's bins of each window: the counts and weights up to the
-    // thread before it, and up to itself.
-    int cbefore[2] = {0, 0}, cupto[2] = {0, 0};
-    double wbefore[2] = {0.0, 0.0}, wupto[2] = {0.0, 0.0};
-    int ctotal = 0;
-    double wtotal = 0.0;
-    int loaded = -1;  // window whose counts are in LDS
-    auto count = [&](int win) {
-      if (loaded == win) return;
-      for (int i = tid; i < kBins / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
-      __syncthreads();
-      each_vector([&](const u32x4& r, int) {
+    // The histogram.  A value that occurs 65536 times carries into its
+    // neighbour or out of the word: the counts then do not add up to the
+    // tokens, and the values are counted again, 32 bits each, one sign at a
+    // time (a row of one repeated value, say).
+    int valid = 0;
+    {
+      auto add = [&](const u32x4& r, int) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const uint32_t k = key_at(r, e);
-          const int b = (int)(top - k) - win * kBins;
-          if (k != kLowest && b >= 0 && b < kBins) atomicAdd(&bins[bin_word(b)], 1u);
+          const int k = half_of(r[e >> 1], e & 1);
+          if (k > kLowest && k <= kHighest) {
+            ++valid;
+            atomicAdd(&bins[k & 0x7FFF], k < 0 ? 1u : 0x10000u);
+          }
         }
-      });
-      __syncthreads();
-      loaded = win;
-    };
-    auto total = [&](int win, int& call, double& wall) {
-      double ws = 0.0;
-      int cs = 0;
-      for (int i = 0; i < kPer; ++i) {
-        const int c = (int)bins[bin_word(tid * kPer + i)];
-        if (c) {
-          cs += c;
-          ws += c * weight(win * kBins + tid * kPer + i);
-        }
-      }
+      };
+      LAQ_EACH_VECTOR(add)
+    }
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const double x = __shfl_up(ws, d);
-        const int c = __shfl_up(cs, d);
-        if (lane >= d) ws += x, cs += c;
+    for (int s = 32; s >= 1; s >>= 1) valid += __shfl_xor(valid, s);
+    if (lane == 0) sh.csum[w] = valid;
+    __syncthreads();
+    valid = 0;
+#pragma unroll
+    for (int i = 0; i < kWavesS; ++i) valid += sh.csum[i];
+    const uint32_t zero = bins[0], minus_zero = bins[kWords - 1] & 0xFFFFu;  // tokens of +0 and -0: one value
+    __syncthreads();
+    if (tid == 0 && minus_zero) {
+      bins[0] = zero + (minus_zero << 16);
+      bins[kWords - 1] -= minus_zero;
+    }
+    bool packed = (zero >> 16) + minus_zero < 65536u;
+    int loaded = 2;  // sign whose values are counted (packed: both)
+    __syncthreads();
+
+    auto count_sign = [&](int neg) {  // 32-bit counts of the values >= 0 or < 0
+      if (packed || loaded == neg) return;
+      __syncthreads();
+      for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
+      __syncthreads();
+#pragma unroll 1
+      for (int v = 0; v < nv; ++v) {
+        const u32x4 r = to_sortable(fetch(v));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          int k = half_of(r[e >> 1], e & 1);
+          if (k == -1) k = 0;
+          if (k > kLowest && k <= kHighest && (k < 0) == (neg != 0)) atomicAdd(&bins[k & 0x7FFF], 1u);
+        }
       }
-      if (lane == 63) sh.wsum[w] = ws, sh.csum[w] = cs;
+      __syncthreads();
+      loaded = neg;
+    };
+    // Tokens of the value at place b; its sign's counts are loaded.
+    auto count_at = [&](int b) {
+      const int k = value_at(b);
+      const uint32_t word = bins[k & 0x7FFF];
+      return (int)(!packed ? word : k < 0 ? word & 0xFFFFu : word >> 16);
+    };
+    // Totals of the lines, a line's 64 values over the lanes of a wave; the
+    // waves take every 16th line.
+    auto line_totals = [&](int neg) {
+      for (int j = w; j < kLines / 2; j += kWavesS) {
+        const int line = neg * (kLines / 2) + j;
+        const int b = line * 64 + lane;
+        int c = count_at(b);
+        double ws = 0.0;
+        if (__ballot(c != 0)) {
+          ws = c ? c * weight(b) : 0.0;
+          wave_scan(ws, c, lane);
+        }
+        if (lane == 63) sh.line_w[line] = ws, sh.line_c[line] = c;
+      }
+    };
+    // Thread t holds line t: counts and weights of the lines before it, and
+    // with its own.
+    int cbefore, cupto, ctotal;
+    double wbefore, wupto, wtotal;
+    auto totals = [&]() {
+      for (int neg = 1; neg >= 0; --neg) {
+        count_sign(neg);
+        line_totals(neg);
+      }
+      __syncthreads();
+      wupto = sh.line_w[tid];
+      cupto = sh.line_c[tid];
+      wave_scan(wupto, cupto, lane);
+      if (lane == 63) sh.wsum[w] = wupto, sh.csum[w] = cupto;
       __syncthreads();
       double wb = 0.0;
       int cb = 0;
-      call = 0, wall = 0.0;
+      ctotal = 0, wtotal = 0.0;
 #pragma unroll
       for (int i = 0; i < kWavesS; ++i) {
-        if (i == w) wb = wall, cb = call;
-        wall += sh.wsum[i];
-        call += sh.csum[i];
+        if (i == w) wb = wtotal, cb = ctotal;
+        wtotal += sh.wsum[i];
+        ctotal += sh.csum[i];
       }
       __syncthreads();
-      wupto[win] = wb + ws;
-      cupto[win] = cb + cs;
+      wupto += wb;
+      cupto += cb;
       // the thread before's own numbers, so that no place falls between two
-      const double x = __shfl_up(wupto[win], 1);
-      const int c = __shfl_up(cupto[win], 1);
-      wbefore[win] = lane ? x : wb;
-      cbefore[win] = lane ? c : cb;
+      const double x = __shfl_up(wupto, 1);
+      const int c = __shfl_up(cupto, 1);
+      wbefore = lane ? x : wb;
+      cbefore = lane ? c : cb;
     };
-    // Values top .. top - 32767, then the rest, which top-k may not reach.
-    // The first window is counted last where that is known: it is the one
-    // that holds most places looked for below.
-    int windows = 1, c0, c1;
-    double w0, w1;
-    if (top - low >= kBins && top_k == INT_MAX) {
-      count(1);
-      total(1, c1, w1);
-      windows = 2;
-    }
-    count(0);
-    total(0, c0, w0);
-    if (top - low >= kBins && top_k != INT_MAX && top_k > c0) {
-      count(1);
-      total(1, c1, w1);
-      windows = 2;
-    }
-    ctotal = c0, wtotal = w0;
-    if (windows == 2) {
-      cbefore[1] += c0, cupto[1] += c0;
-      wbefore[1] += w0, wupto[1] += w0;
-      ctotal += c1;
-      wtotal = w0 + w1;
+#pragma unroll 1
+    for (;;) {
+      totals();
+      if (!packed || ctotal == valid) break;
+      packed = false;
     }
 
-    // The bins of one thread, one a lane (lanes 32 and up: none).
+    // The values of one line, one a lane, in the wave that holds the line.
     struct Line {
-      int bin, c, cb;      // the bin, its count, the counts before it
-      double w, wb, wupto; // its weight, the weights before it and up to it
+      int place, c, cb;     // the place, its count, the counts before it
+      double w, wb, wupto;  // its weight, the weights before it and up to it
     };
-    auto line = [&](int win, int l) {  // l: the owner's lane in this wave
+    auto line = [&](int l) {  // l: the line's lane in this wave
       Line r;
-      const int first = (w * 64 + l) * kPer;
-      r.bin = win * kBins + first + (lane & 31);
-      r.c = lane < kPer ? (int)bins[bin_word(first + (lane & 31))] : 0;
-      r.w = r.c ? weight(r.bin) : 0.0;
+      r.place = (w * 64 + l) * 64 + lane;
+      r.c = count_at(r.place);
+      r.w = r.c ? weight(r.place) : 0.0;
       double ws = r.c * r.w;
       int cs = r.c;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const double x = __shfl_up(ws, d);
-        const int c = __shfl_up(cs, d);
-        if (lane >= d) ws += x, cs += c;
-      }
-      const double base = __shfl(win ? wbefore[1] : wbefore[0], l);
-      r.cb = __shfl(win ? cbefore[1] : cbefore[0], l) + cs - r.c;
+      wave_scan(ws, cs, lane);
+      const double base = lane_double(wbefore, l);
+      r.cb = __builtin_amdgcn_readlane(cbefore, l) + cs - r.c;
       r.wupto = base + ws;
       const double x = __shfl_up(r.wupto, 1);
       r.wb = lane ? x : base;
       return r;
     };
-    // The first thread, in the order of values, that has tokens and for which
-    // reached(window) holds: its wave calls take(window, lane) with that window's counts in
-    // LDS.  False where there is none.
-    auto at_first = [&](auto&& reached, auto&& take) {
-      for (int win = 0; win < windows; ++win) {
-        const uint64_t m = __ballot((win ? cupto[1] > cbefore[1] : cupto[0] > cbefore[0]) && reached(win));
-        if (lane == 0) sh.csum[w] = m ? w * 64 + __ffsll((unsigned long long)m) - 1 : kThreads;
-        __syncthreads();
-        int owner = kThreads;
+    // The first line that has tokens and for which `reached` holds: its wave
+    // calls take(lane).  False where there is none.
+    auto at_first = [&](bool reached, auto&& take) {
+      const uint64_t m = __ballot(cupto > cbefore && reached);
+      if (lane == 0) sh.csum[w] = m ? w * 64 + __ffsll((unsigned long long)m) - 1 : kLines;
+      __syncthreads();
+      int owner = kLines;
 #pragma unroll
-        for (int i = 0; i < kWavesS; ++i) owner = min(owner, sh.csum[i]);
-        __syncthreads();
-        if (owner == kThreads) continue;
-        count(win);
-        if (uni(owner >> 6) == w) take(win, owner & 63);
-        __syncthreads();
-        return true;
+      for (int i = 0; i < kWavesS; ++i) owner = min(owner, sh.csum[i]);
+      owner = uni(owner);
+      if (owner < kLines) {
+        count_sign(owner >= kLines / 2);
+        if (owner >> 6 == w) take(owner & 63);
       }
-      return false;
+      __syncthreads();
+      return owner < kLines;
     };
     // The first lane of a line for which `in` holds (its last token's otherwise).
     auto first_lane = [&](const Line& r, bool in) {
@@ -268,20 +370,19 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
       return m ? __ffsll((unsigned long long)m) - 1 : 63 - __clzll((long long)any);
     };
 
-    // What is kept: all tokens of the bins before cut_bin, cut_count of its own.
-    int cut_bin = 65536, cut_count = 0;
+    // What is kept: all tokens of the values before cut, cut_count of its own.
+    int cut = 65536, cut_count = 0;
     double kept = wtotal;
     if (top_k < ctotal) {
-      at_first([&](int win) { return top_k <= (win ? cupto[1] : cupto[0]); },
-               [&](int win, int l) {
-                 const Line r = line(win, l);
-                 if (lane == first_lane(r, r.c && top_k <= r.cb + r.c)) {
-                   sh.bin = r.bin;
-                   sh.nth = top_k - r.cb;
-                   sh.weight = r.wb + (top_k - r.cb) * r.w;
-                 }
-               });
-      cut_bin = sh.bin;
+      at_first(top_k <= cupto, [&](int l) {
+        const Line r = line(l);
+        if (lane == first_lane(r, r.c && top_k <= r.cb + r.c)) {
+          sh.place = r.place;
+          sh.nth = top_k - r.cb;
+          sh.weight = r.wb + (top_k - r.cb) * r.w;
+        }
+      });
+      cut = sh.place;
       cut_count = sh.nth;
       kept = sh.weight;
       __syncthreads();
@@ -290,148 +391,181 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     const float pf = p_ ? p_[row] : 1.0f;
     if (pf < 1.0f) {
       const double target = fmax((double)pf, 0.0) * kept;
-      const bool found = at_first([&](int win) { return (win ? wupto[1] : wupto[0]) >= target; },
-                                  [&](int win, int l) {
-                                    const Line r = line(win, l);
-                                    if (lane == first_lane(r, r.c && r.wupto >= target)) {
-                                      // the smallest count whose weight reaches the target
-                                      double c = fmin(fmax(ceil((target - r.wb) / r.w), 1.0), (double)r.c);
-                                      if (c > 1.0 && r.wb + (c - 1.0) * r.w >= target) c -= 1.0;
-                                      if (c < r.c && r.wb + c * r.w < target) c += 1.0;
-                                      sh.bin = r.bin;
-                                      sh.nth = (int)c;
-                                    }
-                                  });
-      const int b = sh.bin, c = sh.nth;
+      const bool found = at_first(wupto >= target, [&](int l) {
+        const Line r = line(l);
+        if (lane == first_lane(r, r.c && r.wupto >= target)) {
+          // the smallest count whose weight reaches the target
+          double c = fmin(fmax(ceil((target - r.wb) / r.w), 1.0), (double)r.c);
+          if (c > 1.0 && r.wb + (c - 1.0) * r.w >= target) c -= 1.0;
+          if (c < r.c && r.wb + c * r.w < target) c += 1.0;
+          sh.place = r.place;
+          sh.nth = (int)c;
+          sh.weight = r.wb + c * r.w;
+        }
+      });
+      const int b = sh.place, c = sh.nth;
+      const double wt = sh.weight;
       __syncthreads();
-      if (found && (b < cut_bin || (b == cut_bin && c < cut_count))) cut_bin = b, cut_count = c, narrowed = true;
+      if (found && (b < cut || (b == cut && c < cut_count))) cut = b, cut_count = c, kept = wt;
     }
     const float mp = mp_ ? mp_[row] : 0.0f;
     if (mp > 0.0f) {
       // The last value with a weight of min-p: near the inverse, then by the weights themselves.
       const double least = fmin((double)mp, 1.0);
-      int b = 0;
+      int b = first_place;
       if (largest < INFINITY) {
-        const double edge = fmax(largest + T * log(least), -65504.0);
-        const int end = (int)(top - kLowest) - 1;
-        b = (int)(top - key_of(__builtin_bit_cast(uint16_t, (_Float16)(float)edge)));
-        b = min(max(b, 0), end);
-        while (b > 0 && weight(b) < least) --b;
+        const double edge = fmax(largest + (double)temp * log(least), -65504.0);
+        const int k = half_of(sortable(__builtin_bit_cast(uint16_t, (_Float16)(float)edge)), 0);
+        const int end = place_of(kLowest) - 1;
+        b = min(max(place_of(k), first_place), end);
+        while (b > first_place && weight(b) < least) --b;
         while (b < end && weight(b + 1) >= least) ++b;
       }
-      if (b + 1 <= cut_bin) cut_bin = b + 1, cut_count = 0, narrowed = true;
+      if (b + 1 <= cut) cut = b + 1, cut_count = 0, narrowed = true;
     }
-    if (narrowed) {
-      const int b = cut_count > 0 ? cut_bin : cut_bin - 1;
-      const int most = cut_count > 0 ? cut_count : INT_MAX;
-      const int owner = b % kBins / kPer;
-      if (b / kBins < windows) {
-        count(b / kBins);
-        if (w == owner >> 6) {
-          const Line r = line(b / kBins, owner & 63);
-          if (lane < kPer && r.bin == b) sh.weight = r.wb + min(r.c, most) * r.w;
-        }
-        __syncthreads();
-        kept = sh.weight;
-        __syncthreads();
-      } else {
-        kept = wtotal;  // every value that was counted
+    if (narrowed) {  // the weight of all values before cut
+      const int b = cut - 1, owner = b >> 6;
+      count_sign(owner >= kLines / 2);
+      if (w == owner >> 6) {
+        const Line r = line(owner & 63);
+        if (r.place == b) sh.weight = r.wupto;
       }
+      __syncthreads();
+      kept = sh.weight;
+      __syncthreads();
     }
     // The draw.
     const float uf = u_[row];
     const double target = (uf > 0.0f ? fmin((double)uf, 1.0) : 0.0) * kept;
-    bool drawn = at_first([&](int win) { return (win ? wupto[1] : wupto[0]) > target; },
-                          [&](int win, int l) {
-                            const Line r = line(win, l);
-                            if (lane == first_lane(r, r.c && r.wupto > target)) {
-                              double c = fmin(fmax(floor((target - r.wb) / r.w), 0.0), (double)(r.c - 1));
-                              if (c > 0.0 && r.wb + c * r.w > target) c -= 1.0;
-                              if (c + 1.0 < r.c && r.wb + (c + 1.0) * r.w <= target) c += 1.0;
-                              sh.bin = r.bin;
-                              sh.nth = (int)c;
-                            }
-                          });
-    if (drawn) pick = sh.bin, nth = sh.nth;
+    bool drawn = at_first(wupto > target, [&](int l) {
+      const Line r = line(l);
+      if (lane == first_lane(r, r.c && r.wupto > target)) {
+        double c = fmin(fmax(floor((target - r.wb) / r.w), 0.0), (double)(r.c - 1));
+        if (c > 0.0 && r.wb + c * r.w > target) c -= 1.0;
+        if (c + 1.0 < r.c && r.wb + (c + 1.0) * r.w <= target) c += 1.0;
+        sh.place = r.place;
+        sh.nth = (int)c;
+        sh.weight = r.w;
+      }
+    });
+    if (drawn) pick = sh.place, nth = sh.nth, chance = sh.weight / kept;
     __syncthreads();
-    if (drawn && (pick > cut_bin || (pick == cut_bin && nth >= cut_count))) drawn = false;
-    if (!drawn) {  // u = 1, or a border met by rounding: the last token kept
+    if (!drawn || pick > cut || (pick == cut && nth >= cut_count)) {
+      // u = 1, or a border met by rounding: the last token kept
       if (cut_count > 0) {
-        pick = cut_bin, nth = cut_count - 1;
+        pick = cut, nth = cut_count - 1;
       } else {
-        pick = 0, nth = 0;
-        for (int win = windows - 1; win >= 0; --win) {
-          count(win);
+        pick = first_place, nth = 0;
+        for (int neg = 1; neg >= 0; --neg) {
+          count_sign(neg);
           int mine = -1;
-          for (int i = 0; i < kPer; ++i)
-            if (win * kBins + tid * kPer + i < cut_bin && bins[bin_word(tid * kPer + i)]) mine = tid * kPer + i;
-#pragma unroll
-          for (int s = 32; s >= 1; s >>= 1) mine = max(mine, __shfl_xor(mine, s));
-          if (lane == 0) sh.csum[w] = mine;
-          __syncthreads();
-#pragma unroll
-          for (int i = 0; i < kWavesS; ++i) mine = max(mine, sh.csum[i]);
-          __syncthreads();
+          for (int i = 0; i < kWords / kThreads; ++i) {
+            const int b = neg * kWords + tid * (kWords / kThreads) + i;
+            if (b < cut && count_at(b)) mine = b;
+          }
+          mine = block_max(mine);
           if (mine >= 0) {
-            pick = win * kBins + mine;
-            nth = (int)bins[bin_word(mine)] - 1;
+            pick = mine;
+            nth = count_at(mine) - 1;
             break;
           }
         }
       }
+      chance = weight(pick) / kept;
     }
-    chance = weight(pick) / kept;
-    __syncthreads();  // the bins are done with
+    __syncthreads();  // the histogram is done with
   }
 
-  // The nth token with the drawn value, in the order of indices.
-  const uint32_t want = top - pick;
-  int* const found = reinterpret_cast<int*>(bins);  // per vector and wave; bins are done with
-  each_vector([&](const u32x4& r, int v) {
-    int c = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c += __popcll(__ballot(key_at(r, e) == want));
-    if (lane == 0 && v < nv) found[v * kWavesS + w] = c;
-  });
+  // The nth token of the drawn value, in the order of indices.
+  const int want = value_at(pick);
+  auto is_wanted = [&](int k) { return k == want || (want == 0 && k == -1); };
+  if (tid == 0) sh.found = 0;
   __syncthreads();
-  if (w == 0) {
-    int before = 0;
-    for (int i0 = 0; i0 < nv * kWavesS; i0 += 64) {
-      int c = i0 + lane < nv * kWavesS ? found[i0 + lane] : 0;
-      int up = c;
+  // Indices of the value's tokens, in any order, as far as there is room.
+  int* const list = reinterpret_cast<int*>(bins);
+  constexpr int kRoom = 1024;
+  {
+    const uint32_t both = (uint32_t)(want & 0xFFFF) | (uint32_t)want << 16;
+    ushort2_t least = {0xFFFF, 0xFFFF};
+    auto differ = [&](const u32x4& r, int) {
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int t = __shfl_up(up, d);
-        up += lane >= d ? t : 0;
-      }
-      const uint64_t m = __ballot(before + up > nth);
-      if (m) {
-        const int l = __ffsll((unsigned long long)m) - 1;
-        const int rest = nth - (before + __shfl(up - c, l));
-        // that wave's 512 logits of that vector, eight a lane
-        const int v = (i0 + l) / kWavesS, ww = (i0 + l) % kWavesS;
-        const int64_t at = ((int64_t)v * kThreads + ww * 64 + lane) * 8;
-        uint32_t mask = 0;
+      for (int i = 0; i < 4; ++i)
+        least = __builtin_elementwise_min(least, __builtin_bit_cast(ushort2_t, r[i] ^ both));
+    };
+    bool any = want == 0;
+    if (!any) {
+      LAQ_EACH_VECTOR(differ)
+      any = least[0] == 0 || least[1] == 0;
+    }
+    if (any) {
+      auto note = [&](const u32x4& r, int v) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (at + e < V && key_of(x[at + e]) == want) mask |= 1u << e;
-        const int own = __popc(mask);
-        int sum = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int t = __shfl_up(sum, d);
-          sum += lane >= d ? t : 0;
-        }
-        if (sum - own <= rest && rest < sum) {
-          for (int i = rest - (sum - own); i > 0; --i) mask &= mask - 1;
-          token[row] = (int)(at + __ffs((int)mask) - 1);
-          if (prob) prob[row] = (float)chance;
-        }
-        break;
-      }
-      before += __shfl(up, 63);
+          if (is_wanted(half_of(r[e >> 1], e & 1))) {
+            const int at = atomicAdd(&sh.found, 1);
+            if (at < kRoom) list[at] = (v * kThreads + tid) * 8 + e;
+          }
+      };
+      LAQ_EACH_VECTOR(note)
     }
   }
+  __syncthreads();
+  const int found = sh.found;
+  if (found <= kRoom) {
+    // a thread per token: its rank among them
+    if (tid < found) {
+      const int mine = list[tid];
+      int rank = 0;
+      for (int i = 0; i < found; ++i) rank += list[i] < mine ? 1 : 0;
+      if (rank == nth) {
+        token[row] = mine;
+        if (prob) prob[row] = (float)chance;
+      }
+    }
+    return;
+  }
+  // Many: counts per vector and wave, then that wave's 512 logits.
+  __syncthreads();
+  int* const per_wave = reinterpret_cast<int*>(bins);
+#pragma unroll 1
+  for (int v = 0; v < nv; ++v) {
+    const u32x4 r = to_sortable(fetch(v));
+    int c = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c += __popcll(__ballot(is_wanted(half_of(r[e >> 1], e & 1))));
+    if (lane == 0) per_wave[v * kWavesS + w] = c;
+  }
+  __syncthreads();
+  if (w > 0) return;
+  int before = 0;
+  for (int i0 = 0; i0 < nv * kWavesS; i0 += 64) {
+    const int c = i0 + lane < nv * kWavesS ? per_wave[i0 + lane] : 0;
+    int up = c;
+    double unused = 0.0;
+    wave_scan(unused, up, lane);
+    const uint64_t m = __ballot(before + up > nth);
+    if (m) {
+      const int l = __ffsll((unsigned long long)m) - 1;
+      const int rest = nth - (before + __builtin_amdgcn_readlane(up - c, l));
+      const int v = (i0 + l) / kWavesS, ww = (i0 + l) % kWavesS;
+      const int64_t at = ((int64_t)v * kThreads + ww * 64 + lane) * 8;
+      uint32_t mask = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (at + e < V && is_wanted(half_of(sortable(x[at + e]), 0))) mask |= 1u << e;
+      const int own = __popc(mask);
+      int sum = own;
+      wave_scan(unused, sum, lane);
+      if (sum - own <= rest && rest < sum) {
+        for (int i = rest - (sum - own); i > 0; --i) mask &= mask - 1;
+        token[row] = (int)(at + __ffs((int)mask) - 1);
+        if (prob) prob[row] = (float)chance;
+      }
+      return;
+    }
+    before += __builtin_amdgcn_readlane(up, 63);
+  }
+#undef LAQ_EACH_VECTOR
 }
 
 }  // namespace
