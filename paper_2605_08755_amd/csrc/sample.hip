@@ -11,11 +11,14 @@
 // bits moves a border by whole tokens).  Counting is in whole numbers, sums
 // are added in a fixed order: the same token on every call.
 //
-// One block of 1024 threads per row, the logits in its registers (read once).
-// What bounds a row: the passes over its logits, about a microsecond of one
-// compute unit per vector instruction and 150 000 logits; so the logits are
-// turned into sortable numbers in place, two per instruction, and the
-// histogram holds two 16-bit counts per LDS word (all 65536 values in 128 KiB).
+// One block of 1024 threads per row, two passes over its logits: the histogram
+// (two 16-bit counts per LDS word, so that all 65536 values fit one compute
+// unit) and, once a value is drawn, the search for its index.  What bounds a
+// row: the vector instructions of the first pass, about a microsecond of one
+// compute unit per instruction and 150 000 logits, and the instruction fetch
+// of code that runs once, so loops stay rolled.  (Measured on MI355X, one row of 151936:
+// the row held in registers and every pass unrolled 48 us, this 21.)
+
 #include <limits.h>
 #include <math.h>
 
@@ -28,6 +31,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWavesS = kThreads / 64;
 constexpr int kWords = 32768;           // histogram words: values >= 0 in the upper halves, < 0 in the lower
+constexpr int kBinWords = kWords + kWords / 64;  // a word of padding per 64: a lane per line reads without conflicts
 constexpr int kLines = 1024;            // 64 values each, in falling order
 constexpr int kLowest = -31745;         // sortable number of -inf (and of NaN)
 constexpr int kHighest = 31744;         // of +inf
@@ -103,16 +107,16 @@ __device__ __forceinline__ void wave_scan(double& v, int& c, int lane) {
 }
 
 struct SampleShared {
-  double line_w[kLines];
-  int line_c[kLines];
   double wsum[kWavesS], weight;
-  int csum[kWavesS];
+  int csum[kWavesS], valid[kWavesS];
   int place, nth, found;
+  uint32_t aside[64];
 };
-constexpr int kSampleLds = kWords * 4 + (int)sizeof(SampleShared);
+constexpr int kSampleLds = kBinWords * 4 + (int)sizeof(SampleShared);
 static_assert(kSampleLds <= 160 * 1024, "LDS of a compute unit");
 
-template <int NV>
+__device__ __forceinline__ int bin_word(int word) { return word + (word >> 6); }
+
 __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __restrict__ logits, int64_t stride, int V,
                                                           const float* __restrict__ u_, const float* __restrict__ t_,
                                                           const int* __restrict__ k_, const float* __restrict__ p_,
@@ -120,43 +124,50 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
                                                           float* __restrict__ prob) {
   extern __shared__ u32x4 sample_lds[];
   uint32_t* const bins = reinterpret_cast<uint32_t*>(sample_lds);
-  SampleShared& sh = *reinterpret_cast<SampleShared*>(bins + kWords);
+  SampleShared& sh = *reinterpret_cast<SampleShared*>(bins + kBinWords);
   const int tid = threadIdx.x, lane = tid & 63, w = uni(tid >> 6);
   const int row = blockIdx.x;
   const uint16_t* const x = logits + row * stride;
-  const int nv = (V + 8 * kThreads - 1) / (8 * kThreads);
+  const int whole = V >> 3;                               // vectors of eight logits; the last V % 8 come singly
+  const int nv = (whole + kThreads - 1) / kThreads;       // a thread's vectors: v * 1024 + tid
+  constexpr uint32_t kNone = 0xFC00FC00u;                 // -inf twice
 
-  // Sortable numbers of the eight logits (v * 1024 + tid) * 8 .. + 7, -inf past the end.
-  auto fetch = [&](int v) {
-    const int64_t at = ((int64_t)v * kThreads + tid) * 8;
-    u32x4 r;
-    if (at + 8 <= V) {
-      __builtin_memcpy(&r, x + at, 16);  // rows of an odd vocabulary are 2-byte aligned
-    } else {
-      uint32_t e[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) e[i] = at + i < V ? x[at + i] : 0xFC00u;
-      r = u32x4{e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16};
-    }
+  auto load = [&](int v) {
+    const int at = v * kThreads + tid;
+    u32x4 r = {kNone, kNone, kNone, kNone};
+    if (at < whole) __builtin_memcpy(&r, x + (int64_t)at * 8, 16);  // rows of an odd vocabulary: 2-byte aligned
     return r;
   };
-  auto to_sortable = [](u32x4 r) { return u32x4{sortable(r.x), sortable(r.y), sortable(r.z), sortable(r.w)}; };
-  u32x4 keep[NV > 0 ? NV : 1];
-  if constexpr (NV > 0) {
+  // f(eight logits, index of the first) over this thread's logits, AHEAD
+  // vectors loaded while as many are computed; -inf past the end.
+  auto each_vector = [&](auto ahead, auto&& f) {
+    constexpr int AHEAD = decltype(ahead)::value;
+    const int last = V & ~7;
+    const uint32_t single = tid < V - last ? x[last + tid] : kNone & 0xFFFFu;
+    u32x4 r[AHEAD], next[AHEAD];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) keep[v] = fetch(v);
-    for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
+    for (int i = 0; i < AHEAD; ++i) r[i] = load(i);
+#pragma unroll 1
+    for (int v0 = 0; v0 < nv; v0 += AHEAD) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) keep[v] = to_sortable(keep[v]);
-  } else {
-    for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
-  }
-#define LAQ_EACH_VECTOR(body)                                    \
-  if constexpr (NV > 0) {                                        \
-    _Pragma("unroll") for (int v = 0; v < NV; ++v) body(keep[v], v); \
-  } else {                                                       \
-    for (int v = 0; v < nv; ++v) body(to_sortable(fetch(v)), v);  \
-  }
+      for (int i = 0; i < AHEAD; ++i) next[i] = load(v0 + AHEAD + i);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) f(r[i], ((v0 + i) * kThreads + tid) * 8);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) r[i] = next[i];
+    }
+    f(u32x4{single | (kNone & 0xFFFF0000u), kNone, kNone, kNone}, last + tid);
+  };
+  // f(sortable numbers of two logits).
+  auto each_pair = [&](auto ahead, auto&& f) {
+    each_vector(ahead, [&](const u32x4& r, int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(sortable(r[e]));
+    });
+  };
+  constexpr std::integral_constant<int, 5> counted;
+  constexpr std::integral_constant<int, 10> searched;  // (little to compute: more loads under way)
+  constexpr std::integral_constant<int, 1> rare;
   auto block_max = [&](int m) {
 #pragma unroll
     for (int s = 32; s >= 1; s >>= 1) m = max(m, __shfl_xor(m, s));
@@ -168,31 +179,43 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     return uni(m);
   };
 
-  // The largest; positive NaN, which sort above it, are looked for only where there are some.
-  int top;
+  // The histogram, the largest value and the number of tokens.  Per logit: its
+  // word, the increment of its half, one comparison (of the upper logit as the
+  // whole pair), an atomic; -inf goes to a word of its lane's own.
+  for (int i = tid; i < kBinWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
+  __syncthreads();
+  int valid = 0, top;
   {
     short2_t m = {-32768, -32768};
-    auto take = [&](const u32x4& r, int) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t two = r[i];  // (the cast takes element 0 of a vector element named in it)
-        m = __builtin_elementwise_max(m, __builtin_bit_cast(short2_t, two));
-      }
-    };
-    LAQ_EACH_VECTOR(take)
+    const uint32_t aside = (uint32_t)((sh.aside - bins) + lane);
+    each_pair(counted, [&](uint32_t two) {
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(short2_t, two));
+      const uint32_t neg_lo = (uint32_t)((int)(two << 16) >> 31), neg_hi = (uint32_t)((int)two >> 31);
+      const bool in_lo = (short)(uint16_t)two > (short)kLowest, in_hi = (int)two >= (kLowest + 1) * 65536;
+      valid += __popcll(__ballot(in_lo)) + __popcll(__ballot(in_hi));
+      const uint32_t lo = (two & 0x7FFFu) + (two >> 6 & 0x1FFu), hi = (two >> 16 & 0x7FFFu) + (two >> 22 & 0x1FFu);
+      atomicAdd(&bins[in_lo ? lo : aside], 0x10000u ^ (neg_lo & 0x10001u));
+      atomicAdd(&bins[in_hi ? hi : aside], 0x10000u ^ (neg_hi & 0x10001u));
+    });
+    if (lane == 0) sh.valid[w] = valid;
     top = block_max(max((int)m[0], (int)m[1]));
   }
-  if (top > kHighest) {
+  const bool nan = top > kHighest;  // positive NaN, which sort above +inf: their counts are taken out
+  if (nan) {
     int m = -32768;
-    auto take = [&](const u32x4& r, int) {
+    valid = 0;
+    each_pair(rare, [&](uint32_t two) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int k = half_of(r[e >> 1], e & 1);
+      for (int e = 0; e < 2; ++e) {
+        const int k = half_of(two, e);
         m = max(m, k > kHighest ? -32768 : k);
+        valid += __popcll(__ballot(k > kLowest && k <= kHighest));
       }
-    };
-    LAQ_EACH_VECTOR(take)
+    });
+    if (lane == 0) sh.valid[w] = valid;
     top = block_max(m);
+    for (int k = kHighest + 1 + tid; k < kWords; k += kThreads) bins[bin_word(k)] &= 0xFFFFu;
+    __syncthreads();
   }
   if (top <= kLowest) {  // nothing allowed
     if (tid == 0) {
@@ -213,36 +236,18 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     const int kk = k_ ? k_[row] : 0;
     const int top_k = kk > 0 ? kk : INT_MAX;
 
-    // The histogram.  A value that occurs 65536 times carries into its
-    // neighbour or out of the word: the counts then do not add up to the
-    // tokens, and the values are counted again, 32 bits each, one sign at a
-    // time (a row of one repeated value, say).
-    int valid = 0;
-    {
-      auto add = [&](const u32x4& r, int) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int k = half_of(r[e >> 1], e & 1);
-          if (k > kLowest && k <= kHighest) {
-            ++valid;
-            atomicAdd(&bins[k & 0x7FFF], k < 0 ? 1u : 0x10000u);
-          }
-        }
-      };
-      LAQ_EACH_VECTOR(add)
-    }
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) valid += __shfl_xor(valid, s);
-    if (lane == 0) sh.csum[w] = valid;
-    __syncthreads();
+    // A value that occurs 65536 times carries into its neighbour or out of the
+    // word: the counts then do not add up to the tokens, and the values are
+    // counted again, 32 bits each, one sign at a time (a row of one repeated
+    // value, say).
     valid = 0;
 #pragma unroll
-    for (int i = 0; i < kWavesS; ++i) valid += sh.csum[i];
-    const uint32_t zero = bins[0], minus_zero = bins[kWords - 1] & 0xFFFFu;  // tokens of +0 and -0: one value
+    for (int i = 0; i < kWavesS; ++i) valid += sh.valid[i];
+    const uint32_t zero = bins[0], minus_zero = bins[bin_word(kWords - 1)] & 0xFFFFu;  // tokens of +0 and -0: one value
     __syncthreads();
     if (tid == 0 && minus_zero) {
       bins[0] = zero + (minus_zero << 16);
-      bins[kWords - 1] -= minus_zero;
+      bins[bin_word(kWords - 1)] -= minus_zero;
     }
     bool packed = (zero >> 16) + minus_zero < 65536u;
     int loaded = 2;  // sign whose values are counted (packed: both)
@@ -251,54 +256,73 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     auto count_sign = [&](int neg) {  // 32-bit counts of the values >= 0 or < 0
       if (packed || loaded == neg) return;
       __syncthreads();
-      for (int i = tid; i < kWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
+      for (int i = tid; i < kBinWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
       __syncthreads();
-#pragma unroll 1
-      for (int v = 0; v < nv; ++v) {
-        const u32x4 r = to_sortable(fetch(v));
+      each_pair(rare, [&](uint32_t two) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          int k = half_of(r[e >> 1], e & 1);
+        for (int e = 0; e < 2; ++e) {
+          int k = half_of(two, e);
           if (k == -1) k = 0;
-          if (k > kLowest && k <= kHighest && (k < 0) == (neg != 0)) atomicAdd(&bins[k & 0x7FFF], 1u);
+          if (k > kLowest && k <= kHighest && (k < 0) == (neg != 0)) atomicAdd(&bins[bin_word(k & 0x7FFF)], 1u);
         }
-      }
+      });
       __syncthreads();
       loaded = neg;
     };
-    // Tokens of the value at place b; its sign's counts are loaded.
-    auto count_at = [&](int b) {
-      const int k = value_at(b);
-      const uint32_t word = bins[k & 0x7FFF];
-      return (int)(!packed ? word : k < 0 ? word & 0xFFFFu : word >> 16);
+    // Tokens of value k; its sign's counts are loaded.
+    auto count_of = [&](int k) {
+      const uint32_t word = bins[bin_word(k & 0x7FFF)];
+      return (int)(word >> (packed && k >= 0 ? 16 : 0) & (packed ? 0xFFFFu : ~0u));
     };
-    // Totals of the lines, a line's 64 values over the lanes of a wave; the
-    // waves take every 16th line.
-    auto line_totals = [&](int neg) {
-      for (int j = w; j < kLines / 2; j += kWavesS) {
-        const int line = neg * (kLines / 2) + j;
-        const int b = line * 64 + lane;
-        int c = count_at(b);
-        double ws = 0.0;
-        if (__ballot(c != 0)) {
-          ws = c ? c * weight(b) : 0.0;
-          wave_scan(ws, c, lane);
-        }
-        if (lane == 63) sh.line_w[line] = ws, sh.line_c[line] = c;
-      }
-    };
+    auto count_at = [&](int b) { return count_of(value_at(b)); };
     // Thread t holds line t: counts and weights of the lines before it, and
     // with its own.
-    int cbefore, cupto, ctotal;
-    double wbefore, wupto, wtotal;
-    auto totals = [&]() {
-      for (int neg = 1; neg >= 0; --neg) {
-        count_sign(neg);
-        line_totals(neg);
+    int cbefore, cupto = 0, ctotal;
+    double wbefore, wupto = 0.0, wtotal;
+    // The lines' own, a thread per line.  A line's 64 values share an
+    // exponent, so they are evenly spaced and their weights a geometric series:
+    // summed from its end, a multiplication and an addition per value and two
+    // exponentials per line.  In the line of the largest logit the series
+    // starts there (weight 1 to the bit).
+    auto line_total = [&]() {
+      const int k0 = value_at(tid * 64);
+      const int e = (k0 < 0 ? ~k0 : k0) >> 10 & 31;
+      const double ratio = exp2_neg(-ldexp(per, max(e, 1) - 25));
+      const int stop = tid == first_place >> 6 ? first_place & 63 : -64;
+      const double first = tid <= first_place >> 6 ? 1.0 : exp2_neg((logit_of(k0) - largest) * per);
+      const uint32_t* const words = bins + bin_word((k0 & 0x7FFF) - 63);  // of the line's last value
+      const int shift = packed && k0 >= 0 ? 16 : 0;
+      const uint32_t mask = packed ? 0xFFFFu : ~0u;
+      double sum = 0.0;
+      int c = 0;
+#pragma unroll 1
+      for (int j = 0; j < 64; j += 16) {  // j: places before the line's last
+        int n[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) n[i] = (int)(words[j + i] >> shift & mask);
+        if (63 - j - 15 >= stop) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            c += n[i];
+            sum = fma(sum, ratio, (double)n[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            c += n[i];
+            if (63 - j - i >= stop) sum = fma(sum, ratio, (double)n[i]);
+          }
+        }
       }
-      __syncthreads();
-      wupto = sh.line_w[tid];
-      cupto = sh.line_c[tid];
+      wupto = sum * first;
+      cupto = c;
+    };
+    auto totals = [&]() {
+#pragma unroll 1
+      for (int neg = 1; neg >= 0; --neg) {  // packed: both signs at once
+        count_sign(neg);
+        if (packed ? neg == 1 : (tid >= kLines / 2) == (neg == 1)) line_total();
+      }
       wave_scan(wupto, cupto, lane);
       if (lane == 63) sh.wsum[w] = wupto, sh.csum[w] = cupto;
       __syncthreads();
@@ -327,188 +351,137 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
       packed = false;
     }
 
-    // The values of one line, one a lane, in the wave that holds the line.
-    struct Line {
-      int place, c, cb;     // the place, its count, the counts before it
-      double w, wb, wupto;  // its weight, the weights before it and up to it
-    };
-    auto line = [&](int l) {  // l: the line's lane in this wave
-      Line r;
-      r.place = (w * 64 + l) * 64 + lane;
-      r.c = count_at(r.place);
-      r.w = r.c ? weight(r.place) : 0.0;
-      double ws = r.c * r.w;
-      int cs = r.c;
-      wave_scan(ws, cs, lane);
-      const double base = lane_double(wbefore, l);
-      r.cb = __builtin_amdgcn_readlane(cbefore, l) + cs - r.c;
-      r.wupto = base + ws;
-      const double x = __shfl_up(r.wupto, 1);
-      r.wb = lane ? x : base;
-      return r;
-    };
-    // The first line that has tokens and for which `reached` holds: its wave
-    // calls take(lane).  False where there is none.
-    auto at_first = [&](bool reached, auto&& take) {
-      const uint64_t m = __ballot(cupto > cbefore && reached);
+    // What is kept is the first kept_n tokens in order, of weight kept.  Up to
+    // five places are looked for, each in the line (found among the threads'
+    // sums) and then among the line's values, one a lane of the line's wave:
+    //   0  top-k: token number top_k
+    //   1  top-p: the first token at which the weight reaches top_p x kept
+    //   2  min-p: the last value with that weight
+    //   3  the draw: the first token at which the weight passes u x kept
+    //   4  where that is past the last kept token (u = 1, or a border met by
+    //      rounding): the last kept token
+    const float pf = p_ ? p_[row] : 1.0f, mp = mp_ ? mp_[row] : 0.0f, uf = u_[row];
+    int kept_n = ctotal;
+    double kept = wtotal;
+#pragma unroll 1
+    for (int step = 0; step < 5; ++step) {
+      int number = 0, place = 0;
+      double target = 0.0;
+      if (step == 0) {
+        if (top_k >= ctotal) continue;
+        number = top_k;
+      } else if (step == 1) {
+        if (!(pf < 1.0f)) continue;
+        target = fmax((double)pf, 0.0) * kept;
+      } else if (step == 2) {
+        if (!(mp > 0.0f)) continue;
+        // near the inverse, then by the weights themselves
+        const double least = fmin((double)mp, 1.0);
+        place = first_place;
+        if (largest < INFINITY) {
+          const double edge = fmax(largest + (double)temp * log(least), -65504.0);
+          const int end = place_of(kLowest) - 1;
+          const int k = half_of(sortable(__builtin_bit_cast(uint16_t, (_Float16)(float)edge)), 0);
+          place = min(max(place_of(k), first_place), end);
+          while (place > first_place && weight(place) < least) --place;
+          while (place < end && weight(place + 1) >= least) ++place;
+        }
+        place = uni(place);
+      } else if (step == 3) {
+        target = (uf > 0.0f ? fmin((double)uf, 1.0) : 0.0) * kept;
+      } else {
+        number = kept_n;
+      }
+      const bool by_number = step == 0 || step == 4;
+      const bool reached = by_number ? number <= cupto : step == 1 ? wupto >= target : wupto > target;
+      const uint64_t m = __ballot(step == 2 ? tid == place >> 6 : cupto > cbefore && reached);
       if (lane == 0) sh.csum[w] = m ? w * 64 + __ffsll((unsigned long long)m) - 1 : kLines;
       __syncthreads();
       int owner = kLines;
 #pragma unroll
       for (int i = 0; i < kWavesS; ++i) owner = min(owner, sh.csum[i]);
       owner = uni(owner);
-      if (owner < kLines) {
-        count_sign(owner >= kLines / 2);
-        if (owner >> 6 == w) take(owner & 63);
+      if (owner == kLines) {  // past every weight
+        __syncthreads();
+        continue;
       }
-      __syncthreads();
-      return owner < kLines;
-    };
-    // The first lane of a line for which `in` holds (its last token's otherwise).
-    auto first_lane = [&](const Line& r, bool in) {
-      const uint64_t m = __ballot(in), any = __ballot(r.c > 0);
-      return m ? __ffsll((unsigned long long)m) - 1 : 63 - __clzll((long long)any);
-    };
-
-    // What is kept: all tokens of the values before cut, cut_count of its own.
-    int cut = 65536, cut_count = 0;
-    double kept = wtotal;
-    if (top_k < ctotal) {
-      at_first(top_k <= cupto, [&](int l) {
-        const Line r = line(l);
-        if (lane == first_lane(r, r.c && top_k <= r.cb + r.c)) {
-          sh.place = r.place;
-          sh.nth = top_k - r.cb;
-          sh.weight = r.wb + (top_k - r.cb) * r.w;
-        }
-      });
-      cut = sh.place;
-      cut_count = sh.nth;
-      kept = sh.weight;
-      __syncthreads();
-    }
-    bool narrowed = false;
-    const float pf = p_ ? p_[row] : 1.0f;
-    if (pf < 1.0f) {
-      const double target = fmax((double)pf, 0.0) * kept;
-      const bool found = at_first(wupto >= target, [&](int l) {
-        const Line r = line(l);
-        if (lane == first_lane(r, r.c && r.wupto >= target)) {
-          // the smallest count whose weight reaches the target
-          double c = fmin(fmax(ceil((target - r.wb) / r.w), 1.0), (double)r.c);
-          if (c > 1.0 && r.wb + (c - 1.0) * r.w >= target) c -= 1.0;
-          if (c < r.c && r.wb + c * r.w < target) c += 1.0;
-          sh.place = r.place;
-          sh.nth = (int)c;
-          sh.weight = r.wb + c * r.w;
-        }
-      });
-      const int b = sh.place, c = sh.nth;
-      const double wt = sh.weight;
-      __syncthreads();
-      if (found && (b < cut || (b == cut && c < cut_count))) cut = b, cut_count = c, kept = wt;
-    }
-    const float mp = mp_ ? mp_[row] : 0.0f;
-    if (mp > 0.0f) {
-      // The last value with a weight of min-p: near the inverse, then by the weights themselves.
-      const double least = fmin((double)mp, 1.0);
-      int b = first_place;
-      if (largest < INFINITY) {
-        const double edge = fmax(largest + (double)temp * log(least), -65504.0);
-        const int k = half_of(sortable(__builtin_bit_cast(uint16_t, (_Float16)(float)edge)), 0);
-        const int end = place_of(kLowest) - 1;
-        b = min(max(place_of(k), first_place), end);
-        while (b > first_place && weight(b) < least) --b;
-        while (b < end && weight(b + 1) >= least) ++b;
-      }
-      if (b + 1 <= cut) cut = b + 1, cut_count = 0, narrowed = true;
-    }
-    if (narrowed) {  // the weight of all values before cut
-      const int b = cut - 1, owner = b >> 6;
       count_sign(owner >= kLines / 2);
-      if (w == owner >> 6) {
-        const Line r = line(owner & 63);
-        if (r.place == b) sh.weight = r.wupto;
-      }
-      __syncthreads();
-      kept = sh.weight;
-      __syncthreads();
-    }
-    // The draw.
-    const float uf = u_[row];
-    const double target = (uf > 0.0f ? fmin((double)uf, 1.0) : 0.0) * kept;
-    bool drawn = at_first(wupto > target, [&](int l) {
-      const Line r = line(l);
-      if (lane == first_lane(r, r.c && r.wupto > target)) {
-        double c = fmin(fmax(floor((target - r.wb) / r.w), 0.0), (double)(r.c - 1));
-        if (c > 0.0 && r.wb + c * r.w > target) c -= 1.0;
-        if (c + 1.0 < r.c && r.wb + (c + 1.0) * r.w <= target) c += 1.0;
-        sh.place = r.place;
-        sh.nth = (int)c;
-        sh.weight = r.w;
-      }
-    });
-    if (drawn) pick = sh.place, nth = sh.nth, chance = sh.weight / kept;
-    __syncthreads();
-    if (!drawn || pick > cut || (pick == cut && nth >= cut_count)) {
-      // u = 1, or a border met by rounding: the last token kept
-      if (cut_count > 0) {
-        pick = cut, nth = cut_count - 1;
-      } else {
-        pick = first_place, nth = 0;
-        for (int neg = 1; neg >= 0; --neg) {
-          count_sign(neg);
-          int mine = -1;
-          for (int i = 0; i < kWords / kThreads; ++i) {
-            const int b = neg * kWords + tid * (kWords / kThreads) + i;
-            if (b < cut && count_at(b)) mine = b;
+      if (owner >> 6 == w) {
+        const int b = owner * 64 + lane, l = owner & 63;
+        const int c = count_at(b);
+        const double wt = c ? weight(b) : 0.0;
+        double ws = c * wt;
+        int cs = c;
+        wave_scan(ws, cs, lane);
+        const double base = lane_double(wbefore, l), upto = base + ws;
+        const double below = __shfl_up(upto, 1), wb = lane ? below : base;
+        const int cu = __builtin_amdgcn_readlane(cbefore, l) + cs, cb = cu - c;
+        const bool in = by_number ? number <= cu : step == 1 ? upto >= target : upto > target;
+        const uint64_t at = __ballot(c > 0 && in), any = __ballot(c > 0);
+        const int mine = step == 2 ? place & 63 : at ? __ffsll((unsigned long long)at) - 1 : 63 - __clzll((long long)any);
+        if (lane == mine) {
+          int n = c;  // tokens of this value up to the place
+          if (by_number) {
+            n = number - cb;
+          } else if (step == 1) {  // the smallest count whose weight reaches the target
+            double t = fmin(fmax(ceil((target - wb) / wt), 1.0), (double)c);
+            if (t > 1.0 && wb + (t - 1.0) * wt >= target) t -= 1.0;
+            if (t < c && wb + t * wt < target) t += 1.0;
+            n = (int)t;
+          } else if (step == 3) {  // the smallest whose weight passes it
+            double t = fmin(fmax(floor((target - wb) / wt), 0.0), (double)(c - 1));
+            if (t > 0.0 && wb + t * wt > target) t -= 1.0;
+            if (t + 1.0 < c && wb + (t + 1.0) * wt <= target) t += 1.0;
+            n = (int)t + 1;
           }
-          mine = block_max(mine);
-          if (mine >= 0) {
-            pick = mine;
-            nth = count_at(mine) - 1;
-            break;
-          }
+          sh.place = b;
+          sh.nth = n;
+          sh.found = cb + n;
+          sh.weight = wb + n * wt;
         }
       }
-      chance = weight(pick) / kept;
+      __syncthreads();
+      const int n = sh.found;
+      if (step < 3) {
+        if (step == 0 || n < kept_n) kept_n = n, kept = sh.weight;
+      } else if (n <= kept_n) {
+        pick = sh.place;
+        nth = sh.nth - 1;
+        break;
+      }
+      __syncthreads();
     }
+    chance = weight(pick) / kept;
     __syncthreads();  // the histogram is done with
   }
 
   // The nth token of the drawn value, in the order of indices.
   const int want = value_at(pick);
-  auto is_wanted = [&](int k) { return k == want || (want == 0 && k == -1); };
+  // as the logits' own bits, the sign of zeros apart
+  const uint32_t bits = (uint32_t)(want < 0 ? want ^ 0x7FFF : want) & 0xFFFFu;
+  const uint32_t both = bits | bits << 16, mask = want == 0 ? 0x7FFF7FFFu : ~0u;
+  auto is_wanted = [&](uint32_t logit) { return ((logit ^ bits) & mask & 0xFFFFu) == 0; };
   if (tid == 0) sh.found = 0;
   __syncthreads();
   // Indices of the value's tokens, in any order, as far as there is room.
   int* const list = reinterpret_cast<int*>(bins);
   constexpr int kRoom = 1024;
-  {
-    const uint32_t both = (uint32_t)(want & 0xFFFF) | (uint32_t)want << 16;
+  each_vector(searched, [&](const u32x4& r, int at) {
     ushort2_t least = {0xFFFF, 0xFFFF};
-    auto differ = [&](const u32x4& r, int) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        least = __builtin_elementwise_min(least, __builtin_bit_cast(ushort2_t, r[i] ^ both));
-    };
-    bool any = want == 0;
-    if (!any) {
-      LAQ_EACH_VECTOR(differ)
-      any = least[0] == 0 || least[1] == 0;
+    for (int e = 0; e < 4; ++e)
+      least = __builtin_elementwise_min(least, __builtin_bit_cast(ushort2_t, (r[e] & mask) ^ both));
+    if (least[0] == 0 || least[1] == 0) {
+#pragma unroll 1
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t two = e < 2 ? r.x : e < 4 ? r.y : e < 6 ? r.z : r.w;
+        if (is_wanted(two >> (16 * (e & 1)))) {
+          const int i = atomicAdd(&sh.found, 1);
+          if (i < kRoom) list[i] = at + e;
+        }
+      }
     }
-    if (any) {
-      auto note = [&](const u32x4& r, int v) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (is_wanted(half_of(r[e >> 1], e & 1))) {
-            const int at = atomicAdd(&sh.found, 1);
-            if (at < kRoom) list[at] = (v * kThreads + tid) * 8 + e;
-          }
-      };
-      LAQ_EACH_VECTOR(note)
-    }
-  }
+  });
   __syncthreads();
   const int found = sh.found;
   if (found <= kRoom) {
@@ -524,48 +497,30 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     }
     return;
   }
-  // Many: counts per vector and wave, then that wave's 512 logits.
-  __syncthreads();
-  int* const per_wave = reinterpret_cast<int*>(bins);
-#pragma unroll 1
-  for (int v = 0; v < nv; ++v) {
-    const u32x4 r = to_sortable(fetch(v));
-    int c = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c += __popcll(__ballot(is_wanted(half_of(r[e >> 1], e & 1))));
-    if (lane == 0) per_wave[v * kWavesS + w] = c;
-  }
-  __syncthreads();
-  if (w > 0) return;
+  // Many: counts per wave of a thousand consecutive logits at a time, then the
+  // logit itself.
   int before = 0;
-  for (int i0 = 0; i0 < nv * kWavesS; i0 += 64) {
-    const int c = i0 + lane < nv * kWavesS ? per_wave[i0 + lane] : 0;
-    int up = c;
-    double unused = 0.0;
-    wave_scan(unused, up, lane);
-    const uint64_t m = __ballot(before + up > nth);
-    if (m) {
-      const int l = __ffsll((unsigned long long)m) - 1;
-      const int rest = nth - (before + __builtin_amdgcn_readlane(up - c, l));
-      const int v = (i0 + l) / kWavesS, ww = (i0 + l) % kWavesS;
-      const int64_t at = ((int64_t)v * kThreads + ww * 64 + lane) * 8;
-      uint32_t mask = 0;
+#pragma unroll 1
+  for (int64_t i0 = 0; i0 < V; i0 += kThreads) {
+    const int64_t i = i0 + tid;
+    const bool is = i < V && is_wanted(x[i]);
+    const uint64_t m = __ballot(is);
+    __syncthreads();
+    if (lane == 0) sh.csum[w] = __popcll(m);
+    __syncthreads();
+    int mine = before, all = before;
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (at + e < V && is_wanted(half_of(sortable(x[at + e]), 0))) mask |= 1u << e;
-      const int own = __popc(mask);
-      int sum = own;
-      wave_scan(unused, sum, lane);
-      if (sum - own <= rest && rest < sum) {
-        for (int i = rest - (sum - own); i > 0; --i) mask &= mask - 1;
-        token[row] = (int)(at + __ffs((int)mask) - 1);
-        if (prob) prob[row] = (float)chance;
-      }
-      return;
+    for (int k = 0; k < kWavesS; ++k) {
+      if (k == w) mine = all;
+      all += sh.csum[k];
     }
-    before += __builtin_amdgcn_readlane(up, 63);
+    if (is && mine + __popcll(m & ((1ULL << lane) - 1)) == nth) {
+      token[row] = (int)i;
+      if (prob) prob[row] = (float)chance;
+    }
+    if (nth < all) return;
+    before = all;
   }
-#undef LAQ_EACH_VECTOR
 }
 
 }  // namespace
@@ -574,17 +529,8 @@ hipError_t launch_sample(const uint16_t* logits, int64_t stride, int64_t rows, i
                          const float* temperature, const int* top_k, const float* top_p, const float* min_p, int* token,
                          float* prob, hipStream_t stream, const LaunchEvents& ev) {
   const dim3 grid((unsigned)rows), block(kThreads);
-  const int64_t nv = (V + 8 * kThreads - 1) / (8 * kThreads);
-#define LAQ_SAMPLE(NV)                                                                                             \
-  launch(sample_kernel<NV>, grid, block, kSampleLds, stream, ev, logits, stride, (int)V, u, temperature, top_k, top_p, \
-         min_p, token, prob)
-  // Logits stay in registers where the row fits: 19 vectors of eight a thread.
-  if (nv <= 1) LAQ_SAMPLE(1);
-  else if (nv <= 4) LAQ_SAMPLE(4);
-  else if (nv <= 10) LAQ_SAMPLE(10);
-  else if (nv <= 19) LAQ_SAMPLE(19);
-  else LAQ_SAMPLE(0);
-#undef LAQ_SAMPLE
+  launch(sample_kernel, grid, block, kSampleLds, stream, ev, logits, stride, (int)V, u, temperature, top_k, top_p, min_p,
+         token, prob);
   return hipGetLastError();
 }
 
