@@ -1,4 +1,6 @@
-"""One batch-1 decode step of a Qwen3-shaped decoder on the library's kernels.
+"""Decode steps of a Qwen3-shaped decoder on the library's kernels: one token of
+one sequence (DecodeStep), or rows of several sequences with paged caches
+(BatchStep).
 
 Each layer: residual add + RMSNorm, the fused q|k|v linear (the norm inside
 it when the linear offers laq.add_rmsnorm_linear), per-head q/k
@@ -184,3 +186,100 @@ class DecodeStep:
             return self.out
         self.lm_head(self.out, self.logits)
         return self.logits
+
+
+class BatchStep:
+    """Buffers and call sequence of one step of a batch: T rows of up to B
+    sequences -- one row of each while they decode, several rows of a prompt's
+    chunk -- whose keys and values lie in pages.
+
+    linears, norms, final_norm and lm_head as for DecodeStep, with x and out of
+    T rows (laq.linear takes up to 16).  A gate_up callable with the attribute
+    swiglu = True writes silu(gate) * up itself (laq.linear_swiglu: up to 4
+    rows).  k_pages / v_pages: fp16 [num_pages][kv_heads][page_size][128] per
+    layer (the same pages of every layer belong together: one page table serves
+    them all).  window > 0: a row sees its own and the window - 1 positions
+    before it.
+
+    Before run() the caller writes the step's rows into the step's tensors:
+      x0           fp32 [T][hidden]: the rows' embeddings
+      page_table   int32 [B][pages]: page numbers, -1 where there is none
+      token_start  int32 [B + 1]: sequence b's rows (rows from token_start[B]
+                   on are padding)
+      seq_len      int32 [B]: positions of each sequence, its new rows included
+    run() appends the rows to the caches, attends, and returns the logits [T]
+    [vocab] (the final norm's output when there is no LM head).  run() reads
+    nothing back, so a captured graph of it serves every later step: the tensors
+    are rewritten between replays.
+
+    sample() draws a token for every row from the logits: u fp32 [T] in [0, 1)
+    and the settings temperature, top_k, top_p and min_p (tensors [T], filled
+    with the values that leave the distribution as it is); it returns tokens
+    int32 [T] and probs fp32 [T].  A row whose token nobody wants (a prompt's
+    inner rows, padding) costs its pass and can be ignored."""
+
+    def __init__(self, shape, linears, norms, final_norm, k_pages, v_pages, B, T, pages, device, lm_head=None, window=0):
+        import torch
+        self.s = shape
+        self.linears, self.norms, self.final_norm, self.lm_head = linears, norms, final_norm, lm_head
+        self.k_pages, self.v_pages, self.window = k_pages, v_pages, window
+        D, Hq, Hkv, I = shape["hidden"], shape["heads"], shape["kv_heads"], shape["mlp"]
+        capacity = pages * k_pages[0].shape[2]
+        self.cos_sin = rope_table(capacity, shape["rope_theta"], device)
+        f16, f32, i32 = (dict(dtype=t, device=device) for t in (torch.float16, torch.float32, torch.int32))
+        self.page_table = torch.full((B, pages), -1, **i32)
+        self.token_start = torch.zeros((B + 1,), **i32)
+        self.seq_len = torch.zeros((B,), **i32)
+        self.x0 = torch.zeros((T, D), **f32)
+        self.residual = torch.zeros((T, D), **f32)
+        self.h = torch.empty((T, D), **f16)
+        # (zeros: padding rows of q and attn are never written, and what follows reads them)
+        self.qkv = torch.empty((T, (Hq + 2 * Hkv) * HEAD_DIM), **f16)
+        self.q = torch.zeros((T, Hq, HEAD_DIM), **f16)
+        self.attn = torch.zeros((T, Hq, HEAD_DIM), **f16)
+        self.o = torch.empty((T, D), **f16)
+        self.gu = torch.empty((T, 2 * I), **f16)
+        self.m = torch.empty((T, I), **f16)
+        self.down = torch.empty((T, D), **f16)
+        self.out = torch.empty((T, D), **f16)
+        self.workspace = torch.empty(max(laq.paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity), 16),
+                                     dtype=torch.uint8, device=device)
+        self.logits = self.u = None
+        if lm_head is not None:
+            self.logits = torch.empty((T, shape["vocab"]), **f16)
+            self.u = torch.zeros((T,), **f32)
+            self.temperature, self.top_p = torch.ones((T,), **f32), torch.ones((T,), **f32)
+            self.min_p, self.top_k = torch.zeros((T,), **f32), torch.zeros((T,), **i32)
+            self.tokens, self.probs = torch.zeros((T,), **i32), torch.zeros((T,), **f32)
+
+    def run(self):
+        s = self.s
+        Hq, eps, T = s["heads"], s["eps"], self.x0.shape[0]
+        self.residual.copy_(self.x0)
+        delta = None
+        for l, (f_qkv, f_o, f_gu, f_down) in enumerate(self.linears):
+            w_in, w_post, qn, kn = self.norms[l]
+            laq.add_rmsnorm(self.residual, delta, w_in, eps, out=self.h)
+            f_qkv(self.h, self.qkv)
+            laq.paged_append(self.qkv, qn, kn, self.cos_sin, self.k_pages[l], self.v_pages[l], self.page_table,
+                             self.token_start, self.seq_len, Hq, eps, q_out=self.q)
+            laq.paged_attention(self.q, self.k_pages[l], self.v_pages[l], self.page_table, self.token_start,
+                                self.seq_len, window=self.window, out=self.attn, workspace=self.workspace)
+            f_o(self.attn.view(T, Hq * HEAD_DIM), self.o)
+            laq.add_rmsnorm(self.residual, self.o, w_post, eps, out=self.h)
+            if getattr(f_gu, "swiglu", False):
+                f_gu(self.h, self.m)
+            else:
+                f_gu(self.h, self.gu)
+                laq.silu_mul(self.gu, out=self.m)
+            f_down(self.m, self.down)
+            delta = self.down
+        laq.add_rmsnorm(self.residual, delta, self.final_norm, eps, out=self.out)
+        if self.lm_head is None:
+            return self.out
+        self.lm_head(self.out, self.logits)
+        return self.logits
+
+    def sample(self):
+        return laq.sample(self.logits, self.u, self.temperature, self.top_k, self.top_p, self.min_p, out=self.tokens,
+                          probs=self.probs)

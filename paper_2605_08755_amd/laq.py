@@ -8,6 +8,7 @@ exception is raised.
 import ctypes
 import functools
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "liblaq.so")
@@ -45,11 +46,8 @@ class LinearCall(ctypes.Structure):
                 ("zeros", ctypes.c_void_p), ("y", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int64)]
 
 
-class PagedBatch(ctypes.Structure):
-    """laq_paged_batch of include/laq.h."""
-    _fields_ = ([(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "token_start", "seq_len")] +
-                [(n, ctypes.c_int64) for n in ("num_pages", "page_size", "page_stride", "head_stride", "slot_stride",
-                                               "table_pages", "table_stride", "B", "T")])
+# laq_paged_batch of include/laq.h: five pointers, then nine int64.
+_PAGED_BATCH = struct.Struct("5P9q")
 
 
 _lib = None
@@ -131,12 +129,11 @@ def lib():
         L.laq_mlp_workspace_bytes.restype = I64
         L.laq_add_rmsnorm_mlp_w3g128.argtypes = [P, P, P, F32, P, P, P, P, P, P, P, P, I64, I64, P, I64, P]
         L.laq_add_rmsnorm_mlp_w3g128.restype = ctypes.c_int32
-        PB = ctypes.POINTER(PagedBatch)
-        L.laq_paged_append_f16.argtypes = [PB, P, I64, P, P, P, I64, I64, I64, I64, F32, P, P]
+        L.laq_paged_append_f16.argtypes = [P, P, I64, P, P, P, I64, I64, I64, I64, F32, P, P]
         L.laq_paged_append_f16.restype = ctypes.c_int32
         L.laq_paged_attention_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
         L.laq_paged_attention_workspace_bytes.restype = I64
-        L.laq_paged_attention_f16.argtypes = [PB, P, I64, I64, I64, I64, P, P, I64, P]
+        L.laq_paged_attention_f16.argtypes = [P, P, I64, I64, I64, I64, P, P, I64, P]
         L.laq_paged_attention_f16.restype = ctypes.c_int32
         L.laq_sample_f16.argtypes = [P, I64, I64, I64, P, P, P, P, P, P, P, P]
         L.laq_sample_f16.restype = ctypes.c_int32
@@ -540,35 +537,42 @@ def silu_mul(gate_up, out=None):
 # ---------------------------------------------------------------------------
 # batched serving: paged caches, sampling (head dimension 128)
 # ---------------------------------------------------------------------------
-def _on(device):
-    """Makes `device` the current one for a launch on its stream (a no-op where
-    it already is)."""
-    import contextlib
+_current_device = None
 
+
+def _launch(device, fn, *args):
+    """fn(*args, stream) on the current stream of `device`, which is made the
+    current device for the call where it is not."""
+    global _current_device
     import torch
-    if torch.cuda.current_device() == device.index:
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+    if _current_device is None:
+        _current_device = torch._C._cuda_getDevice
+    if _current_device() == device.index:
+        _check(fn(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(device)))
 
 
 def _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T):
+    """(laq_paged_batch, Hkv, B, positions a table row holds)."""
     import torch
+    dev, shape, strides = k_pages.device, k_pages.shape, k_pages.stride()
     assert k_pages.is_cuda and k_pages.dtype == torch.float16 and v_pages.dtype == torch.float16
-    assert k_pages.dim() == 4 and k_pages.shape[3] == HEAD_DIM and k_pages.stride(3) == 1
-    assert v_pages.shape == k_pages.shape and v_pages.stride() == k_pages.stride()
+    assert len(shape) == 4 and shape[3] == HEAD_DIM and strides[3] == 1
+    assert v_pages.shape == shape and v_pages.stride() == strides
     assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.stride(1) == 1
-    B = seq_len.numel()
+    B, pages = page_table.shape
     assert token_start.dtype == torch.int32 and token_start.is_contiguous() and token_start.numel() == B + 1
-    assert seq_len.dtype == torch.int32 and seq_len.is_contiguous() and page_table.shape[0] == B
-    dev = k_pages.device
+    assert seq_len.dtype == torch.int32 and seq_len.is_contiguous() and seq_len.numel() == B
     assert v_pages.device == dev and page_table.device == dev and token_start.device == dev and seq_len.device == dev
-    num_pages, _, page_size, _ = k_pages.shape
     # a dimension of one element has any stride; the library wants a real one
-    page_stride, head_stride, slot_stride = (s if n > 1 else max(s, HEAD_DIM)
-                                             for s, n in zip(k_pages.stride(), k_pages.shape[:3]))
-    return PagedBatch(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), token_start.data_ptr(),
-                      seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, slot_stride,
-                      page_table.shape[1], page_table.stride(0), B, T)
+    num_pages, Hkv, page_size = shape[:3]
+    page_stride = strides[0] if num_pages > 1 else max(strides[0], HEAD_DIM)
+    head_stride = strides[1] if Hkv > 1 else max(strides[1], HEAD_DIM)
+    return _PAGED_BATCH.pack(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), token_start.data_ptr(),
+                             seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, strides[2],
+                             pages, page_table.stride(0) if B > 1 else pages, B, T), Hkv, B, pages * page_size
 
 
 def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, page_table, token_start, seq_len, Hq,
@@ -585,10 +589,9 @@ def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, p
     None.  cos_sin fp32 [positions][128] (decode.rope_table)."""
     import torch
     T = qkv.shape[0]
-    Hkv = k_pages.shape[1]
     dev = qkv.device
     assert qkv.is_cuda and qkv.dtype == torch.float16 and qkv.dim() == 2 and qkv.stride(1) == 1
-    assert qkv.shape[1] == (Hq + 2 * Hkv) * HEAD_DIM and k_pages.device == dev
+    assert k_pages.device == dev
     assert cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.shape[1] == HEAD_DIM
     assert cos_sin.is_contiguous() and cos_sin.device == dev
     for w in (q_norm_weight, k_norm_weight):
@@ -599,13 +602,12 @@ def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, p
     else:
         assert q_out.dtype == torch.float16 and q_out.shape == (T, Hq, HEAD_DIM) and q_out.is_contiguous()
         assert q_out.device == dev
-    batch = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
-    with _on(dev):
-        _check(lib().laq_paged_append_f16(
-            batch, qkv.data_ptr(), qkv.stride(0) if T > 1 else qkv.shape[1],
+    batch, Hkv, _, _ = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
+    assert qkv.shape[1] == (Hq + 2 * Hkv) * HEAD_DIM
+    _launch(dev, lib().laq_paged_append_f16, batch, qkv.data_ptr(), qkv.stride(0) if T > 1 else qkv.shape[1],
             None if q_norm_weight is None else q_norm_weight.data_ptr(),
             None if k_norm_weight is None else k_norm_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0], Hq, Hkv,
-            HEAD_DIM, float(eps), q_out.data_ptr(), _stream(dev)))
+            HEAD_DIM, float(eps), q_out.data_ptr())
     return q_out
 
 
@@ -628,24 +630,21 @@ def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, windo
     assert q.is_cuda and q.dtype == torch.float16 and q.dim() == 3 and q.shape[2] == HEAD_DIM and q.is_contiguous()
     assert k_pages.device == dev
     T, Hq, _ = q.shape
-    Hkv = k_pages.shape[1]
-    batch = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
+    batch, Hkv, B, capacity = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
     if out is None:
         out = torch.zeros((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
     else:
         assert out.dtype == torch.float16 and out.shape == q.shape and out.is_contiguous() and out.device == dev
     nbytes = 0
     if workspace is None:
-        nbytes = paged_attention_workspace_bytes(batch.B, T, Hq, Hkv, batch.table_pages * batch.page_size)
+        nbytes = paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity)
         if nbytes:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     else:
         assert workspace.device == dev and workspace.is_contiguous()
         nbytes = workspace.numel() * workspace.element_size()
-    with _on(dev):
-        _check(lib().laq_paged_attention_f16(batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, int(window), out.data_ptr(),
-                                             None if workspace is None else workspace.data_ptr(), nbytes,
-                                             _stream(dev)))
+    _launch(dev, lib().laq_paged_attention_f16, batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, int(window), out.data_ptr(),
+            None if workspace is None else workspace.data_ptr(), nbytes)
     return out
 
 
@@ -671,7 +670,5 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=
     for t in (u, temperature, top_k, top_p, min_p, out, probs):
         assert t is None or (t.numel() == rows and t.is_contiguous() and t.device == dev)
         ptr.append(None if t is None else t.data_ptr())
-    with _on(dev):
-        _check(lib().laq_sample_f16(logits.data_ptr(), logits.stride(0) if rows > 1 else V, rows, V, *ptr,
-                                    _stream(dev)))
+    _launch(dev, lib().laq_sample_f16, logits.data_ptr(), logits.stride(0) if rows > 1 else V, rows, V, *ptr)
     return out, probs

@@ -577,3 +577,136 @@ def test_sample_distribution():
     tok, prob = tok.cpu().numpy(), prob.cpu().numpy()
     for t in set(tok.tolist()):
         assert abs((tok == t).sum() - prob[tok == t][0] * n) <= 1.0
+
+
+# ---------------------------------------------------------------------------
+# the operators together, as decode.BatchStep runs them
+# ---------------------------------------------------------------------------
+SHAPE = {"layers": 2, "hidden": 256, "heads": 8, "kv_heads": 2, "mlp": 384, "eps": EPS, "rope_theta": 1e6,
+         "vocab": 1000}
+
+
+def make_step(rng, T, B, ps, pages, window, seen=None):
+    """A BatchStep of quantized linears; `seen` receives (what, layer, input,
+    q, output) of the attention-side linears as they are called."""
+    D, Hq, Hkv, I = SHAPE["hidden"], SHAPE["heads"], SHAPE["kv_heads"], SHAPE["mlp"]
+
+    def linear(N, K, what, l):
+        p = laq.quantize_w3g128(dev(f16(rng, (N, K), 0.05)))
+
+        def f(x, out):
+            laq.linear(x, *p, 3, out=out)
+            if seen is not None:
+                seen.append((what, l, x.clone(), out.clone(), step.q.clone(), step.k_pages[l].clone(),
+                             step.v_pages[l].clone()))
+        return f
+    vec = lambda n: dev((1 + 0.1 * rng.standard_normal(n)).astype(np.float16))  # noqa: E731
+    lins = [(linear((Hq + 2 * Hkv) * 128, D, "qkv", l), linear(D, Hq * 128, "o", l), linear(2 * I, D, "gu", l),
+             linear(D, I, "down", l)) for l in range(2)]
+    norms = [(vec(D), vec(D), vec(128), vec(128)) for _ in range(2)]
+    num = B * pages + 1
+    kp, vp = ([torch.zeros((num, Hkv, ps, 128), dtype=torch.float16, device=DEV) for _ in range(2)] for _ in range(2))
+    head = laq.quantize_w3g128(dev(f16(rng, (SHAPE["vocab"], D), 0.2)))
+    step = decode.BatchStep(SHAPE, lins, norms, vec(D), kp, vp, B, T, pages, DEV,
+                            lm_head=lambda x, out: laq.linear(x, *head, 3, out=out), window=window)
+    step.page_table.copy_(dev(rng.permutation(num)[:B * pages].astype(np.int32).reshape(B, pages)))
+    return step
+
+
+def set_rows(step, tokens, before, rng):
+    step.token_start.copy_(dev(np.concatenate([[0], np.cumsum(tokens)]).astype(np.int32)))
+    step.seq_len.copy_(dev((np.array(tokens) + np.array(before)).astype(np.int32)))
+    step.x0.copy_(dev(rng.standard_normal(tuple(step.x0.shape)).astype(np.float32)))
+
+
+@pytest.mark.parametrize("window", [0, 9])
+def test_batch_step(window):
+    """A prompt's chunk, a second chunk beside a decoding sequence, then
+    decoding with padding rows: every stage against the oracle, from the stage's
+    own inputs on the GPU."""
+    say("batch step", window)
+    rng = np.random.default_rng(70 + window)
+    T, B, ps, pages = 12, 3, 16, 3
+    seen = []
+    step = make_step(rng, T, B, ps, pages, window, seen)
+    Hq, Hkv = SHAPE["heads"], SHAPE["kv_heads"]
+    cs = step.cos_sin.cpu().numpy()
+    for tokens, before in (([12, 0, 0], [0, 0, 0]), ([6, 5, 1], [12, 0, 0]), ([1, 1, 1], [18, 5, 1]),
+                           ([1, 1, 1], [19, 6, 2])):
+        set_rows(step, tokens, before, rng)
+        step.u.copy_(dev(rng.random(T).astype(np.float32)))
+        step.temperature.fill_(0.8)
+        step.top_k.fill_(50)
+        step.top_p.fill_(0.9)
+        del seen[:]
+        old = [(k.cpu().numpy(), v.cpu().numpy()) for k, v in zip(step.k_pages, step.v_pages)]
+        logits = step.run()
+        tok, prob = step.sample()
+        torch.cuda.synchronize()
+        table, start, lens = (t.cpu().numpy() for t in (step.page_table, step.token_start, step.seq_len))
+        mine = sum(tokens)
+        for l in range(2):
+            got = {e[0]: [x.cpu().numpy() for x in e[2:]] for e in seen if e[1] == l}
+            qkv = got["qkv"][1]
+            rq, rk, rv = OS.paged_append(qkv, step.norms[l][2].cpu().numpy(), step.norms[l][3].cpu().numpy(), cs,
+                                         *old[l], table, start, lens, Hq, EPS, np.zeros((T, Hq, 128)))
+            x, _, q, k, v = got["o"]
+            for a, b in ((q[:mine], rq[:mine]), (k, rk)):
+                r = linear_check(a, b)
+                assert r["ok"], r
+            assert np.array_equal(v, rv.astype(np.float16))
+            ref, weight, reach = OS.paged_attention(q, k, v, table, start, lens, window, np.zeros((T, Hq, 128)))
+            attention_check(x.reshape(T, Hq, 128)[:mine], ref[:mine], weight[:mine], reach[:mine], int(lens.max()),
+                            T * (Hq // Hkv) > 16 * B)
+        host = logits.cpu().numpy()
+        for r in range(mine):
+            want, p = OS.sample_row(host[r], float(step.u[r]), temperature=float(np.float32(0.8)), top_k=50,
+                                    top_p=float(np.float32(0.9)))
+            assert int(tok[r]) == want and abs(float(prob[r]) - p) <= 2.0**-23 * p
+
+
+def test_batch_step_in_a_graph():
+    """A decoding loop that feeds each step's tokens into the next, as graph
+    replays and as eager calls: the same tokens, caches and logits."""
+    say("batch step graph")
+    T, B, ps, pages = 4, 4, 16, 4
+    runs = []
+    for graphed in (False, True):
+        rng = np.random.default_rng(90)
+        step = make_step(rng, T, B, ps, pages, 0)
+        table = dev(rng.standard_normal((SHAPE["vocab"], SHAPE["hidden"])).astype(np.float32))
+        one = torch.ones_like(step.seq_len)
+        step.token_start.copy_(torch.arange(B + 1, device=DEV, dtype=torch.int32))
+        step.temperature.copy_(torch.tensor([0.0, 0.7, 1.0, 1.3], device=DEV))
+        step.top_k.fill_(20)
+
+        def one_step():
+            step.seq_len.add_(one)
+            step.run()
+            tok, _ = step.sample()
+            torch.index_select(table, 0, tok, out=step.x0)
+        g = None
+        got = []
+        uniform = rng.random((8, T)).astype(np.float32)
+        step.x0.copy_(table[:T])
+        for i in range(8):
+            step.u.copy_(dev(uniform[i]))
+            if graphed and i == 1:  # the first step, eager, warms up
+                torch.cuda.synchronize()
+                g = torch.cuda.CUDAGraph()
+                saved = step.seq_len.clone(), step.x0.clone()
+                with torch.cuda.graph(g):
+                    one_step()
+                step.seq_len.copy_(saved[0])
+                step.x0.copy_(saved[1])
+            if g is not None:
+                g.replay()
+            else:
+                one_step()
+            torch.cuda.synchronize()
+            got.append((step.tokens.clone(), step.logits.clone()))
+        runs.append((got, [k.clone() for k in step.k_pages]))
+    for (a, la), (b, lb) in zip(runs[0][0], runs[1][0]):
+        assert torch.equal(a, b) and torch.equal(la.view(torch.int16), lb.view(torch.int16))
+    for a, b in zip(runs[0][1], runs[1][1]):
+        assert torch.equal(a, b)
