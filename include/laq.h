@@ -556,7 +556,7 @@ typedef struct laq_paged_batch {
     const int32_t *seq_len;     /* [B] */
     int64_t num_pages;          /* pages of the cache, >= 1 */
     int64_t page_size;          /* positions per page: a power of two, 16..2^20 */
-    int64_t page_stride;        /* elements between pages, a multiple of 8 */
+    int64_t page_stride;        /* elements between pages, a multiple of 8, < 2^31 */
     int64_t head_stride;        /* between key/value heads, a multiple of 8 */
     int64_t slot_stride;        /* between positions, a multiple of 8, <= 2^26 */
     int64_t table_pages;        /* entries of a table row; x page_size <= 2^30 */

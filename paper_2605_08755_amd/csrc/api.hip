@@ -567,8 +567,8 @@ laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int
     return fail(LAQ_ERR_BAD_SHAPE, fn, "table_stride must be at least table_pages");
   if (b->table_stride < 0 || b->table_stride > (1LL << 40)) return fail(LAQ_ERR_BAD_SHAPE, fn, "table_stride must be in 0..2^40");
   if (b->slot_stride < kHeadDimAbi || b->slot_stride > (1 << 26) || b->head_stride < kHeadDimAbi ||
-      b->head_stride > (1LL << 40) || b->page_stride < kHeadDimAbi || b->page_stride > (1LL << 40))
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be at least 128 (slots at most 2^26, heads and pages 2^40)");
+      b->head_stride > (1LL << 40) || b->page_stride < kHeadDimAbi || b->page_stride >= (1LL << 31))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be at least 128 (slots at most 2^26, pages below 2^31, heads at most 2^40)");
   if (b->slot_stride % 8 != 0 || b->head_stride % 8 != 0 || b->page_stride % 8 != 0)
     return fail(LAQ_ERR_MISALIGNED, fn, "strides must be multiples of 8 elements");
   return LAQ_OK;
@@ -590,7 +590,7 @@ laq::PagedBatch internal_batch(const laq_paged_batch& b) {
   p.page_table = b.page_table;
   p.token_start = b.token_start;
   p.seq_len = b.seq_len;
-  p.page_stride = b.page_stride;
+  p.page_bytes = (uint32_t)(b.page_stride * 2);
   p.head_stride = b.head_stride;
   p.table_stride = b.table_stride;
   p.slot_stride = (int)b.slot_stride;

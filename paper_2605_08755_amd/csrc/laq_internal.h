@@ -257,7 +257,8 @@ struct PagedBatch {
   const int* page_table;
   const int* token_start;
   const int* seq_len;
-  int64_t page_stride, head_stride, table_stride;
+  int64_t head_stride, table_stride;
+  uint32_t page_bytes;  // between pages
   int slot_stride, page_shift, num_pages, table_pages, B, T;
 };
 hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,

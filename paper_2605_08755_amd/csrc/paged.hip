@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
   int page = -1;
   if (placed) page = pb.page_table[seq * pb.table_stride + (pos >> pb.page_shift)];
   const bool keep = (unsigned)page < (unsigned)pb.num_pages;
-  const int64_t slot = keep ? page * pb.page_stride + (pos & ((1LL << pb.page_shift) - 1)) * pb.slot_stride : 0;
+  const int64_t slot = keep ? (int64_t)page * (pb.page_bytes / 2) + (pos & ((1LL << pb.page_shift) - 1)) * pb.slot_stride : 0;
 
   const float* const cs = cos_sin + (placed ? pos : 0) * kHeadDim + 8 * i;
   float c[8], s[8];
@@ -334,16 +334,26 @@ __device__ __forceinline__ Span span_of(const Item& it, int j0, int j1, int wind
   return s;
 }
 
-// Sixteen positions from t on (t a multiple of 16, in one page) of one head as
-// a buffer: rows from `end` on, and all rows of a page that is not there, lie
-// past its extent and read as zeros.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows16(const PagedBatch& pb, const uint16_t* base, int g, int page,
-                                                         int t, int end) {
-  const uint32_t there = ((unsigned)page < (unsigned)pb.num_pages) & (t < end);  // (arithmetic, so that no branch is made)
-  const int64_t at = (int64_t)page * pb.page_stride + g * pb.head_stride +
-                     (int64_t)(t & ((1 << pb.page_shift) - 1)) * pb.slot_stride;
-  const uint32_t bytes = (uint32_t)((min(end - t, 16) - 1) * pb.slot_stride + kHeadDim) * 2;
-  return rsrc(base + (at & -(int64_t)there), bytes & -there);
+// Sixteen positions from t on (t a multiple of 16, in one page) of one head, in
+// bytes from the head's first row: rows from `end` on, and all rows of a page
+// that is not there, lie past the extent and read as zeros.  Scalar arithmetic
+// without branches: it stands before every tile's loads (page and slot strides
+// are below 2^32 bytes, so the products are 32 x 32 -> 64 bits).
+struct Rows16 {
+  uint64_t at;
+  uint32_t bytes;
+};
+__device__ __forceinline__ Rows16 rows16(const PagedBatch& pb, int page, int t, int end) {
+  const uint32_t there = ((unsigned)page < (unsigned)pb.num_pages) & (t < end);
+  const uint32_t slot = (uint32_t)t & ((1u << pb.page_shift) - 1);
+  const uint32_t slot_bytes = (uint32_t)pb.slot_stride * 2;
+  Rows16 r;
+  r.at = ((uint64_t)(uint32_t)page * pb.page_bytes + (uint64_t)slot * slot_bytes) & -(uint64_t)there;
+  r.bytes = ((uint32_t)(min(end - t, 16) - 1) * slot_bytes + kHeadDim * 2) & -there;
+  return r;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* head, const Rows16& r) {
+  return rsrc(reinterpret_cast<const char*>(head) + r.at, r.bytes);
 }
 
 // Bits of the halves of x that are infinite or NaN: 0x8000 in each.
@@ -441,6 +451,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
   const uint32_t probs = lds_byte(lds + kWaves * 2 * kKeyBytes + w * 16 * kRowBytes);
   const int p_first = sp.lo + w * kStep;
   const int* const table = pb.page_table + it.b * pb.table_stride;
+  const uint16_t* const khead = pb.k + g * pb.head_stride;
+  const uint16_t* const vhead = pb.v + g * pb.head_stride;
   // Page numbers of the 32 steps from step s on (a multiple of 32).
   auto pages_from = [&](int s) {
     const int t = p_first + (s + (lane >> 1)) * kStride + 16 * (lane & 1);
@@ -456,20 +468,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
     if (s > 0 && (s & 31) == 0) pages = pages_from(s);
     const int pg[2] = {readlane(pages, 2 * (s & 31)), readlane(pages, 2 * (s & 31) + 1)};
     bad[B] = ((unsigned)pg[0] >= (unsigned)pb.num_pages ? 1 : 0) | ((unsigned)pg[1] >= (unsigned)pb.num_pages ? 2 : 0);
+    const Rows16 at[2] = {rows16(pb, pg[0], p, sp.hi), rows16(pb, pg[1], p + 16, sp.hi)};
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int r = 4 * i + j;
-      const __amdgpu_buffer_rsrc_t kr = rows16(pb, pb.k, g, pg[i >> 2], p + 16 * (i >> 2), sp.hi);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(keys + B * kKeyBytes + i * 1024), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rows_of(khead, at[i >> 2]), (lds_void*)(keys + B * kKeyBytes + i * 1024), 16,
                                                (uint32_t)(r & 15) * pb.slot_stride * 2 + 16 * (n ^ (r & 15)), 0, 0, kStreamed);
     }
     __builtin_amdgcn_sched_barrier(0);  // the keys' wait below counts the values' loads as the later ones
     // values of step k = 4 kk + i: positions 16 kk + 4 j + i
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-      const __amdgpu_buffer_rsrc_t vr = rows16(pb, pb.v, g, pg[k >> 2], p + 16 * (k >> 2), sp.hi);
-      vv[B][k] =
-          __builtin_amdgcn_raw_buffer_load_b128(vr, (uint32_t)(4 * j + (k & 3)) * pb.slot_stride * 2 + 16 * n, 0,
+      vv[B][k] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(vhead, at[k >> 2]), (uint32_t)(4 * j + (k & 3)) * pb.slot_stride * 2 + 16 * n, 0,
                                                 kStreamed);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -710,6 +720,8 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
   for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const half8_t*>(q + qrow * kHeadDim + 16 * s + 8 * h);
 
   const int* const table = pb.page_table + it.b * pb.table_stride;
+  const uint16_t* const khead = pb.k + g * pb.head_stride;
+  const uint16_t* const vhead = pb.v + g * pb.head_stride;
   auto pages_from = [&](int t0) {  // page numbers of the 64 groups of 16 positions from t0 on
     const int t = t0 + 16 * lane;
     return t < sp.hi ? table[t >> pb.page_shift] : -1;
@@ -728,8 +740,9 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
     for (int i = 0; i < 4; ++i) {
       const int page = readlane(pages, (t0 - pages_at) / 16 + i);
       bad |= (unsigned)page >= (unsigned)pb.num_pages ? 1 << i : 0;
-      kreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows16(pb, pb.k, g, page, t0 + 16 * i, sp.hi), src_at, 0, 0);
-      vreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows16(pb, pb.v, g, page, t0 + 16 * i, sp.hi), src_at, 0, 0);
+      const Rows16 at = rows16(pb, page, t0 + 16 * i, sp.hi);
+      kreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(khead, at), src_at, 0, 0);
+      vreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(vhead, at), src_at, 0, 0);
     }
   };
   auto is_masked = [&](int t0, int bad_groups) {
