@@ -1093,14 +1093,21 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
     e2.stop = ev.stop;
   }
   const Out o{out, ws, (int)Hq, (int)p.records};
-  const dim3 grid((unsigned)(p.items * Hkv)), join((unsigned)(p.split_tiles * Hkv),
-                                                              p.large ? kLargeRows / 16 : std::min<int64_t>(kSmallRows, pb.T * R));
+  const dim3 grid((unsigned)(p.items * Hkv));
+  // A block joins one row; 16 rows where the tiles (most of them not split) would make many blocks.
+  constexpr int64_t kFewTiles = 32;
+  const bool many = p.large && p.split_tiles * Hkv > kFewTiles;
+  const int64_t most_rows = std::min<int64_t>(p.large ? kLargeRows : kSmallRows, pb.T * R);
+  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? (most_rows + 15) / 16 : most_rows));
   if (p.large) {
     launch(paged_attention_rows128_kernel, grid, dim3(256), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv, (int)window,
            o);
-    if (p.split_tiles > 0)
-      launch((paged_attention_join_kernel<kLargeRows, 1>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,
-             o);
+    if (p.split_tiles > 0 && p.split_tiles * Hkv <= kFewTiles)
+      launch((paged_attention_join_kernel<kLargeRows, 4>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv,
+             (int)window, o);
+    else if (p.split_tiles > 0)
+      launch((paged_attention_join_kernel<kLargeRows, 1>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv,
+             (int)window, o);
   } else {
     launch(paged_attention_rows16_kernel, grid, dim3(64 * kWaves), kSmallLds, stream, e1, pb, q, (int)R, (int)Hkv,
            (int)window, o);
