@@ -587,8 +587,8 @@ laq_status laq_paged_append_f16(const laq_paged_batch *batch, const void *qkv, i
 
 /* laq_paged_attention_workspace_bytes -- workspace (bytes) with which
  * laq_paged_attention_f16 runs a batch of B sequences and T rows whatever
- * their lengths, capacity = table_pages * page_size; at most 68 MB.  0 when the call needs
- * none, and for invalid sizes. */
+ * their lengths, capacity = table_pages * page_size; at most 140 MB.  0 when
+ * the call needs none, and for invalid sizes. */
 int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
 
 /* laq_paged_attention_f16 -- causal attention of every row of a batch over

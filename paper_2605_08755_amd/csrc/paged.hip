@@ -650,7 +650,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
       }
     } else {
       const int r = r0 + h;
-      const _Float16 y = (_Float16)(den > 0.0f ? num / den : 0.0f);
+      const _Float16 y = (_Float16)(den == 0.0f ? 0.0f : num / den);
       o_.out[((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + d] = __builtin_bit_cast(uint16_t, y);
     }
   }
@@ -930,7 +930,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
     }
     return;
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t* const dst = o_.out + qrow * kHeadDim;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
@@ -1028,7 +1028,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   for (int k = 0; k < kRows; ++k) {
     if (row + k >= rows) break;
     const int r = r0 + row + k;
-    const float inv = den[k] > 0.0f ? 1.0f / den[k] : 0.0f;
+    const float inv = den[k] == 0.0f ? 0.0f : 1.0f / den[k];
     *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
         half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
   }
@@ -1047,7 +1047,8 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   p.large = BM == kLargeRows;
   const int64_t tiles = (T * R + std::min(B, T) * (BM - 1)) / BM;
   const int64_t per_head = (kItems<BM> + Hkv - 1) / Hkv;
-  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit;
+  // (with kItems heads and more a head's share of the items is one: no sequence is split)
+  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit && Hkv < kItems<BM>;
   p.items = tiles + (split ? per_head : 0);
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);

@@ -325,6 +325,30 @@ def test_attention_unseen_values(tokens, before, window):
                 assert np.array_equal(out[r, 2:, 1::3].view(np.uint16), clean[r, 2:, 1::3].view(np.uint16))
 
 
+@pytest.mark.parametrize("tokens,before", [([1, 1], [700, 60]), ([70, 40], [90, 40]), ([2, 1], [30, 0])])
+def test_attention_not_finite_inputs(tokens, before):
+    """A NaN query head gives NaN and leaves the other heads and rows as they
+    were; so does a NaN key for the rows and heads that see it."""
+    say("attention not finite", tokens)
+    rng = np.random.default_rng(22)
+    Hq, Hkv, ps = 4, 2, 16
+    bt = Batch(rng, tokens, before, ps, Hkv)
+    q, clean = run_attention(rng, bt, Hq)
+    bad = q.copy()
+    bad[1, 2, 7] = np.nan
+    out = laq.paged_attention(dev(bad), *bt.device()).cpu().numpy()
+    assert np.isnan(out[1, 2]).all()
+    out[1, 2] = clean[1, 2]
+    assert np.array_equal(out.view(np.uint16), clean.view(np.uint16))
+    bt.k[bt.table[0, 0], 1, 3, 9] = np.nan  # position 3 of the first sequence, heads 2 and 3
+    out = laq.paged_attention(dev(q), *bt.device()).cpu().numpy()
+    for r, b, pos in OS.rows(bt.start, bt.lens):
+        if b == 0 and pos >= 3:
+            assert np.isnan(out[r, 2:]).all()
+            out[r, 2:] = clean[r, 2:]
+    assert np.array_equal(out.view(np.uint16), clean.view(np.uint16))
+
+
 @pytest.mark.parametrize("tokens", [[1, 1, 2], [40, 30, 9]])
 def test_attention_rows_that_see_nothing(tokens):
     """No page of the sequence is there, the sequence has fewer positions than
@@ -539,6 +563,31 @@ def test_sample_equal_logits():
     rng = np.random.default_rng(3)
     few = rng.integers(-3, 3, (8, 20000)).astype(np.float16)  # six values
     sample_check(few, u, top_k=[5, 100, 4000, 0, 19999, 7, 0, 12], top_p=[0.9, 1, 0.5, 0.7, 1, 0.1, 0.999, 1])
+
+
+def test_sample_repeated_values():
+    """Values that occur 65536 times and more: alone, beside the value that
+    shares their word of the histogram, among NaN, as both zeros."""
+    say("sample repeated values")
+    V = 140001
+    rng = np.random.default_rng(12)
+    x = (rng.standard_normal((8, V)) * 2).astype(np.float16)
+    # the sortable numbers of a and b differ by 2^15: one word counts both
+    a = np.float16(1.5)
+    b = np.array([(int(a.view(np.uint16)) | 0x8000) ^ 0x7FFF], dtype=np.uint16).view(np.float16)[0]
+    assert b < 0
+    x[0] = a
+    x[1, :70000], x[1, 70000:] = a, b
+    x[2, ::2], x[2, 1::2] = b, a
+    x[3, :66000] = b
+    x[4, :65536] = a
+    x[5, :70000] = np.nan
+    x[6, ::2], x[6, 1::2] = 0.0, -0.0
+    x[7, :65535] = a
+    u = np.array([0.0, 0.3, 0.999, 0.5, 0.7, 0.2, 0.9999, 0.45], dtype=np.float32)
+    for kw in ({}, {"top_k": [70001, 70001, 100000, 65536, 0, 5, 139999, 1]}, {"top_p": [0.6] * 8},
+               {"temperature": [0.3] * 8, "min_p": [0.01] * 8}):
+        sample_check(x, u, **kw)
 
 
 def test_sample_masked_rows():
