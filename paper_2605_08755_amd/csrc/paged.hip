@@ -104,7 +104,9 @@ __device__ __forceinline__ int wave_sum(int v) {
 // lanes a head: lane i holds dimensions 8i .. 8i + 7 and their rotation partners 64
 // further, so a head's two 128-byte halves are loaded and stored whole and the
 // norm needs one sum over eight lanes.  What bounds it: the bytes of the rows
-// in and out; the row's table line is read once per wave.
+// in and out (measured on MI355X, 16384 rows, 32:8 heads: 82 us, 4.9 TB/s,
+// a large copy moves 5.0); few rows are a launch and three dependent reads
+// (16 rows: 3.6 us).  The row's table line is read once per wave.
 // The row's sequence is found by counting the sequences that end at or before
 // it, 64 per step, while the row's first loads are in flight.
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const uint16_t* __restrict__ qkv,
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
 // (row r = token r / R, query head r % R of the head's R) of one sequence, and
 // a range of its positions.  A sequence's positions are split into ranges of
 // `chunk` units of 64 positions; the chunk is chosen on the device from the
-// batch's own lengths, so that all items together are about kItems<BM> per
+// batch's own lengths, so that all items together are about kItems per
 // launch: a long sequence among short ones, or a single one, still occupies
 // the chip, and a sequence that fits one range is written without a second
 // pass.  Every block derives the same numbers from the same arrays; the grid
@@ -219,10 +221,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
 // most 2 x / chunk where it is split, and chunk >= (sum of tiles x units) Hkv / kItems.
 constexpr int kUnit = 64;
 constexpr int kSmallRows = 16, kLargeRows = 128;
+// Blocks that run at once, two a compute unit.  (Measured on MI355X with 256 and
+// 1024: 16 decoding sequences 44 us -> 54 and 44, a chunk beside 15 of them 80
+// -> 104 and 83, three long sequences 160 -> 149 and 159.)
+constexpr int kItems = 512;
+// Units: a shorter range costs more in records than it gains.  (Measured on
+// MI355X: one token at 300 positions 7.4 us with 2, 9.5 with 4; a chunk of 16
+// rows at 6000, 18 us with 4, 18 with 3, 22 with 2.)
 template <int BM>
-constexpr int kItems = BM == kSmallRows ? 512 : 512;
-template <int BM>
-constexpr int kMinChunk = BM == kSmallRows ? 2 : 4;  // units: a shorter range costs more in records than it gains
+constexpr int kMinChunk = BM == kSmallRows ? 2 : 4;
 
 // One sequence, seen from one lane.
 struct Seq {
@@ -270,13 +277,13 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, 
   it.found = false;
   // The smallest chunk by that bound, then up to a third larger until the items
   // are no more than the blocks that run at once (a few more would run alone).
-  const double share = total * Hkv * (1.0 / kItems<BM>);
+  const double share = total * Hkv * (1.0 / kItems);
   const int least = uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
   it.chunk = least;
   if (pb.B <= 64) {
     for (int i = 0; i < 4; ++i) {
       const int c = least + least * i / 8 + (i > 0);
-      if (wave_sum(q.tiles * ((q.units + c - 1) / c)) * Hkv <= kItems<BM>) {
+      if (wave_sum(q.tiles * ((q.units + c - 1) / c)) * Hkv <= kItems) {
         it.chunk = c;
         break;
       }
@@ -385,7 +392,10 @@ struct Out {
 // straight into registers as the operand of the fp32 16x16x4 instruction, so
 // the probabilities stay in 32 bits.  Two blocks per compute unit: one's
 // search for its item, first loads and last joining lie under the other's
-// stream.  The page numbers of 32 steps sit in one register of a wave (lane l:
+// stream.  (Measured on MI355X: sequences of 131072, 77777 and 901 positions,
+// 64:8 heads, 140 us, 6.1 TB/s; 16 of up to 8192, 32:8 heads, 37 us, of which
+// about 8 are the search, the first loads and the joining of the waves; one of
+// 300, 7.4 us.)  The page numbers of 32 steps sit in one register of a wave (lane l:
 // half l & 1 of step l >> 1) and become scalar buffer descriptors.
 constexpr int kWaves = 4;
 constexpr int kStep = 32;
@@ -674,6 +684,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // than 2^7: so they stay below 2^15 and full precision reaches down to 2^-22
 // of the largest, and the value sums are rarely rescaled.  The denominator is
 // the fp32 sum of the unrounded ones.
+//
+// What bounds it: LDS bandwidth.  A wave's 32 rows need a tile's keys and
+// values from LDS whole, 40 KiB per wave and tile with the staging; a compute
+// unit's eight waves take 320 KiB for 8 x 32 matrix instructions.  (Measured
+// on MI355X: two prompts of 8192 and 4001 rows, 32:8 heads, 870 us, 780
+// TFLOP/s; a library's fp16 8192^3 product reaches 1150.  A tile takes a wave
+// about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
+// exponentials, 850 the value sums, 1100 issuing the next tile's loads and
+// stores.  Not faster: the two waves of a SIMD kept a phase apart, 890; the
+// operands of a tile's scores requested at once, 1040.)
 //
 // Tiles of keys and values go memory -> registers -> LDS, two buffers, so that
 // a tile's loads are in flight while the one before is computed and a block
@@ -1046,9 +1066,9 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   AttentionPlan p;
   p.large = BM == kLargeRows;
   const int64_t tiles = (T * R + std::min(B, T) * (BM - 1)) / BM;
-  const int64_t per_head = (kItems<BM> + Hkv - 1) / Hkv;
+  const int64_t per_head = (kItems + Hkv - 1) / Hkv;
   // (with kItems heads and more a head's share of the items is one: no sequence is split)
-  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit && Hkv < kItems<BM>;
+  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit && Hkv < kItems;
   p.items = tiles + (split ? per_head : 0);
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
@@ -1057,7 +1077,10 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   return p;
 }
 
-// Up to 16 rows per sequence on average: decoding.
+// Up to 16 rows per sequence on average go to the 16-row kernel.  (Measured on
+// MI355X, 16-row -> 128-row kernel at twice and four times that: 32:8 heads, one
+// sequence of 6000, 20 -> 17 and 25 -> 19 us; eight of 2000, 35 -> 28 and 54 ->
+// 33; 64:8, four of 8000, 50 -> 44 and 79 -> 47; but one of 500 rows 12 -> 16.5.)
 AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
   if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity);
   return plan_of<kLargeRows>(B, T, R, Hkv, capacity);

@@ -14,10 +14,13 @@
 // One block of 1024 threads per row, two passes over its logits: the histogram
 // (two 16-bit counts per LDS word, so that all 65536 values fit one compute
 // unit) and, once a value is drawn, the search for its index.  What bounds a
-// row: the vector instructions of the first pass, about a microsecond of one
-// compute unit per instruction and 150 000 logits, and the instruction fetch
-// of code that runs once, so loops stay rolled.  (Measured on MI355X, one row of 151936:
-// the row held in registers and every pass unrolled 48 us, this 21.)
+// row: the vector instructions and LDS additions of the first pass (16 of its
+// 32 us at 151936 logits), and the instruction fetch of code that runs once,
+// so loops stay rolled.  (Measured on MI355X, one row of 151936: the row held
+// in registers and every pass unrolled 48 us, rolled and read twice 32.)  A
+// row does not split over compute units: up to 256 rows cost little more than
+// one (64 rows of 151936: 36 us; 256 of 32003: 25), and a decode step has one
+// sampling call per token beside its some hundred other launches.
 
 #include <limits.h>
 #include <math.h>
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     });
   };
   constexpr std::integral_constant<int, 5> counted;
-  constexpr std::integral_constant<int, 10> searched;  // (little to compute: more loads under way)
+  constexpr std::integral_constant<int, 10> searched;  // (little to compute: more loads on their way)
   constexpr std::integral_constant<int, 1> rare;
   auto block_max = [&](int m) {
 #pragma unroll
