@@ -537,42 +537,62 @@ def silu_mul(gate_up, out=None):
 # ---------------------------------------------------------------------------
 # batched serving: paged caches, sampling (head dimension 128)
 # ---------------------------------------------------------------------------
-_current_device = None
+# A small call's host time is what it costs (kernels of 3 to 8 us), and most of
+# that is questions to ten tensors: devices as integers, each shape and stride
+# asked once, torch's names looked up once.  (Measured, eager calls one after another:
+# append of 16 rows 8.5 -> 7.5 us a call, attention of one token 11.4 -> 10.3.)
+class _Torch:
+    """torch's names that a call needs, filled in at the first one."""
+    f16 = f32 = i32 = u8 = empty = zeros = current = stream = guard = None
 
 
-def _launch(device, fn, *args):
-    """fn(*args, stream) on the current stream of `device`, which is made the
-    current device for the call where it is not."""
-    global _current_device
-    import torch
-    if _current_device is None:
-        _current_device = torch._C._cuda_getDevice
-    if _current_device() == device.index:
-        _check(fn(*args, _stream(device)))
+def _torch():
+    if _Torch.f16 is None:
+        import torch
+        _Torch.f32, _Torch.i32, _Torch.u8 = torch.float32, torch.int32, torch.uint8
+        _Torch.empty, _Torch.zeros = torch.empty, torch.zeros
+        _Torch.current, _Torch.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        _Torch.guard = torch.cuda.device
+        _Torch.f16 = torch.float16
+    return _Torch
+
+
+def _launch(dev, fn, *args):
+    """fn(*args, stream) on the current stream of device number `dev`, which is
+    made the current device for the call where it is not."""
+    t = _Torch
+    if t.current() == dev:
+        status = fn(*args, t.stream(dev))
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)))
+        with t.guard(dev):
+            status = fn(*args, t.stream(dev))
+    if status != LAQ_OK:
+        _check(status)
 
 
-def _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T):
-    """(laq_paged_batch, Hkv, B, positions a table row holds)."""
-    import torch
-    dev, shape, strides = k_pages.device, k_pages.shape, k_pages.stride()
-    assert k_pages.is_cuda and k_pages.dtype == torch.float16 and v_pages.dtype == torch.float16
-    assert len(shape) == 4 and shape[3] == HEAD_DIM and strides[3] == 1
+def _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T):
+    """(laq_paged_batch, Hkv, B, positions a table row holds) of tensors on device number `dev`."""
+    t = _Torch
+    num_pages, Hkv, page_size, d = shape = k_pages.shape
+    strides = k_pages.stride()
+    assert d == HEAD_DIM and k_pages.dtype is t.f16 and v_pages.dtype is t.f16
     assert v_pages.shape == shape and v_pages.stride() == strides
-    assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.stride(1) == 1
+    page_stride, head_stride, slot_stride, one = strides
     B, pages = page_table.shape
-    assert token_start.dtype == torch.int32 and token_start.is_contiguous() and token_start.numel() == B + 1
-    assert seq_len.dtype == torch.int32 and seq_len.is_contiguous() and seq_len.numel() == B
-    assert v_pages.device == dev and page_table.device == dev and token_start.device == dev and seq_len.device == dev
+    table_stride, unit = page_table.stride()
+    assert one == 1 and unit == 1 and page_table.dtype is t.i32 and token_start.dtype is t.i32
+    assert seq_len.dtype is t.i32 and token_start.shape == (B + 1,) and seq_len.shape == (B,)
+    assert token_start.is_contiguous() and seq_len.is_contiguous()
+    assert (k_pages.get_device() == v_pages.get_device() == page_table.get_device() == token_start.get_device() ==
+            seq_len.get_device() == dev >= 0)
     # a dimension of one element has any stride; the library wants a real one
-    num_pages, Hkv, page_size = shape[:3]
-    page_stride = strides[0] if num_pages > 1 else max(strides[0], HEAD_DIM)
-    head_stride = strides[1] if Hkv > 1 else max(strides[1], HEAD_DIM)
+    if num_pages == 1:
+        page_stride = max(page_stride, HEAD_DIM)
+    if Hkv == 1:
+        head_stride = max(head_stride, HEAD_DIM)
     return _PAGED_BATCH.pack(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), token_start.data_ptr(),
-                             seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, strides[2],
-                             pages, page_table.stride(0) if B > 1 else pages, B, T), Hkv, B, pages * page_size
+                             seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, slot_stride, pages,
+                             table_stride if B > 1 else pages, B, T), Hkv, B, pages * page_size
 
 
 def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, page_table, token_start, seq_len, Hq,
@@ -587,27 +607,27 @@ def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, p
     seq_len int32 [B] (the new rows included), as laq_paged_batch of
     include/laq.h describes them.  q_norm_weight / k_norm_weight fp16 [128] or
     None.  cos_sin fp32 [positions][128] (decode.rope_table)."""
-    import torch
-    T = qkv.shape[0]
-    dev = qkv.device
-    assert qkv.is_cuda and qkv.dtype == torch.float16 and qkv.dim() == 2 and qkv.stride(1) == 1
-    assert k_pages.device == dev
-    assert cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.shape[1] == HEAD_DIM
-    assert cos_sin.is_contiguous() and cos_sin.device == dev
+    t = _torch()
+    dev = qkv.get_device()
+    T, width = qkv.shape
+    row_stride, one = qkv.stride()
+    batch, Hkv, _, _ = _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T)
+    assert qkv.dtype is t.f16 and one == 1 and width == (Hq + 2 * Hkv) * HEAD_DIM
+    positions, d = cos_sin.shape
+    assert cos_sin.dtype is t.f32 and d == HEAD_DIM and cos_sin.is_contiguous() and cos_sin.get_device() == dev
+    norms = []
     for w in (q_norm_weight, k_norm_weight):
         if w is not None:
-            assert w.dtype == torch.float16 and w.numel() == HEAD_DIM and w.is_contiguous() and w.device == dev
+            assert w.dtype is t.f16 and w.numel() == HEAD_DIM and w.is_contiguous() and w.get_device() == dev
+            w = w.data_ptr()
+        norms.append(w)
     if q_out is None:
-        q_out = torch.zeros((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+        q_out = t.zeros((T, Hq, HEAD_DIM), dtype=t.f16, device=qkv.device)
     else:
-        assert q_out.dtype == torch.float16 and q_out.shape == (T, Hq, HEAD_DIM) and q_out.is_contiguous()
-        assert q_out.device == dev
-    batch, Hkv, _, _ = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
-    assert qkv.shape[1] == (Hq + 2 * Hkv) * HEAD_DIM
-    _launch(dev, lib().laq_paged_append_f16, batch, qkv.data_ptr(), qkv.stride(0) if T > 1 else qkv.shape[1],
-            None if q_norm_weight is None else q_norm_weight.data_ptr(),
-            None if k_norm_weight is None else k_norm_weight.data_ptr(), cos_sin.data_ptr(), cos_sin.shape[0], Hq, Hkv,
-            HEAD_DIM, float(eps), q_out.data_ptr())
+        assert q_out.dtype is t.f16 and q_out.shape == (T, Hq, HEAD_DIM) and q_out.is_contiguous()
+        assert q_out.get_device() == dev
+    _launch(dev, lib().laq_paged_append_f16, batch, qkv.data_ptr(), row_stride if T > 1 else width, norms[0], norms[1],
+            cos_sin.data_ptr(), positions, Hq, Hkv, HEAD_DIM, eps, q_out.data_ptr())
     return q_out
 
 
@@ -625,25 +645,23 @@ def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, windo
     The cache and the batch as for paged_append.  workspace: uint8, at least
     paged_attention_workspace_bytes; taken from torch's allocator on the
     current stream when not given."""
-    import torch
-    dev = q.device
-    assert q.is_cuda and q.dtype == torch.float16 and q.dim() == 3 and q.shape[2] == HEAD_DIM and q.is_contiguous()
-    assert k_pages.device == dev
-    T, Hq, _ = q.shape
-    batch, Hkv, B, capacity = _paged_batch(k_pages, v_pages, page_table, token_start, seq_len, T)
+    t = _torch()
+    dev = q.get_device()
+    T, Hq, d = shape = q.shape
+    assert q.dtype is t.f16 and d == HEAD_DIM and q.is_contiguous()
+    batch, Hkv, B, capacity = _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T)
     if out is None:
-        out = torch.zeros((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+        out = t.zeros(shape, dtype=t.f16, device=q.device)
     else:
-        assert out.dtype == torch.float16 and out.shape == q.shape and out.is_contiguous() and out.device == dev
-    nbytes = 0
+        assert out.dtype is t.f16 and out.shape == shape and out.is_contiguous() and out.get_device() == dev
     if workspace is None:
         nbytes = paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity)
         if nbytes:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            workspace = t.empty(nbytes, dtype=t.u8, device=q.device)
     else:
-        assert workspace.device == dev and workspace.is_contiguous()
+        assert workspace.get_device() == dev and workspace.is_contiguous()
         nbytes = workspace.numel() * workspace.element_size()
-    _launch(dev, lib().laq_paged_attention_f16, batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, int(window), out.data_ptr(),
+    _launch(dev, lib().laq_paged_attention_f16, batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, window, out.data_ptr(),
             None if workspace is None else workspace.data_ptr(), nbytes)
     return out
 
@@ -653,22 +671,21 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=
     the uniform numbers u (fp32 [rows]) -> (tokens int32 [rows], probabilities
     fp32 [rows] among what was kept).  temperature, top_p, min_p fp32 [rows],
     top_k int32 [rows], or None; laq_sample_f16 of include/laq.h defines them."""
-    import torch
-    assert logits.is_cuda and logits.dtype == torch.float16 and logits.dim() == 2 and logits.stride(1) == 1
+    t = _torch()
+    dev = logits.get_device()
     rows, V = logits.shape
-    dev = logits.device
-    assert u.dtype == torch.float32
-    assert top_k is None or top_k.dtype == torch.int32
+    row_stride, one = logits.stride()
+    assert dev >= 0 and logits.dtype is t.f16 and (one == 1 or V == 1)
     if out is None:
-        out = torch.empty((rows,), dtype=torch.int32, device=dev)
+        out = t.empty((rows,), dtype=t.i32, device=logits.device)
     if probs is None:
-        probs = torch.empty((rows,), dtype=torch.float32, device=dev)
-    assert out.dtype == torch.int32
-    for t in (temperature, top_p, min_p, probs):
-        assert t is None or t.dtype == torch.float32
+        probs = t.empty((rows,), dtype=t.f32, device=logits.device)
     ptr = []
-    for t in (u, temperature, top_k, top_p, min_p, out, probs):
-        assert t is None or (t.numel() == rows and t.is_contiguous() and t.device == dev)
-        ptr.append(None if t is None else t.data_ptr())
-    _launch(dev, lib().laq_sample_f16, logits.data_ptr(), logits.stride(0) if rows > 1 else V, rows, V, *ptr)
+    for x, dtype in ((u, t.f32), (temperature, t.f32), (top_k, t.i32), (top_p, t.f32), (min_p, t.f32), (out, t.i32),
+                     (probs, t.f32)):
+        if x is not None:
+            assert x.dtype is dtype and x.numel() == rows and x.is_contiguous() and x.get_device() == dev
+            x = x.data_ptr()
+        ptr.append(x)
+    _launch(dev, lib().laq_sample_f16, logits.data_ptr(), row_stride if rows > 1 else V, rows, V, *ptr)
     return out, probs
