@@ -14,12 +14,13 @@
 // One block of 1024 threads per row, two passes over its logits: the histogram
 // (two 16-bit counts per LDS word, so that all 65536 values fit one compute
 // unit) and, once a value is drawn, the search for its index.  What bounds a
-// row: the vector instructions and LDS additions of the first pass (16 of its
-// 32 us at 151936 logits), and the instruction fetch of code that runs once,
-// so loops stay rolled.  (Measured on MI355X, one row of 151936: the row held
-// in registers and every pass unrolled 48 us, rolled and read twice 32.)  A
+// row: the LDS additions of the first pass (14 of its 31 us at 151936 logits,
+// one addition of a wave about every 13 cycles), and the instruction fetch of
+// code that runs once, so loops stay rolled.  (Measured on MI355X, one row of
+// 151936: the row held in registers and every pass unrolled 48 us, rolled and
+// read twice 33, with words and increments of two logits at a time 31.)  A
 // row does not split over compute units: up to 256 rows cost little more than
-// one (64 rows of 151936: 36 us; 256 of 32003: 25), and a decode step has one
+// one (64 rows of 151936: 35 us; 256 of 32003: 26), and a decode step has one
 // sampling call per token beside its some hundred other launches.
 
 #include <limits.h>
@@ -41,6 +42,7 @@ constexpr int kHighest = 31744;         // of +inf
 
 typedef short short2_t __attribute__((ext_vector_type(2)));
 typedef unsigned short ushort2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) uint32_t lds_word;
 
 __device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -182,23 +184,36 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const uint16_t* __rest
     return uni(m);
   };
 
-  // The histogram, the largest value and the number of tokens.  Per logit: its
-  // word, the increment of its half, one comparison (of the upper logit as the
-  // whole pair), an atomic; -inf goes to a word of its lane's own.
+  // The histogram, the largest value and the number of tokens.  Words and signs
+  // are formed for two logits at once; then per logit a 16-bit dot product
+  // gives the address, a byte permutation the increment of its half, and one
+  // comparison (of the upper logit as the whole pair) sends -inf to a word of
+  // its lane's own.  (A separate path for vectors without -inf: 1 us less per
+  // row of 151936, 1.4 us more where most logits are -inf; additions left out
+  // instead of sent aside: 1 us more.)
   for (int i = tid; i < kBinWords / 4; i += kThreads) reinterpret_cast<u32x4*>(bins)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
   int valid = 0, top;
   {
     short2_t m = {-32768, -32768};
-    const uint32_t aside = (uint32_t)((sh.aside - bins) + lane);
+    const uint32_t base = (uint32_t)(uintptr_t)(lds_word*)bins;
+    const uint32_t aside = base + (uint32_t)((sh.aside - bins) + lane) * 4;
+    auto bump = [&](uint32_t at, uint32_t what) {
+      __hip_atomic_fetch_add((lds_word*)at, what, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
     each_pair(counted, [&](uint32_t two) {
       m = __builtin_elementwise_max(m, __builtin_bit_cast(short2_t, two));
-      const uint32_t neg_lo = (uint32_t)((int)(two << 16) >> 31), neg_hi = (uint32_t)((int)two >> 31);
+      const ushort2_t word = __builtin_bit_cast(ushort2_t, two & 0x7FFF7FFFu);
+      const ushort2_t at = word + (word >> 6);  // bin_word()
+      const uint32_t neg = __builtin_bit_cast(uint32_t, __builtin_bit_cast(short2_t, two) >> 15);
+      // bytes of 0 and 1: (value < 0, value >= 0) of the lower logit, then of the upper
+      const uint32_t which = (neg & 0x01010101u) ^ 0x01000100u;
+      const uint32_t lo = __builtin_amdgcn_udot2(at, ushort2_t{4, 0}, base, false);
+      const uint32_t hi = __builtin_amdgcn_udot2(at, ushort2_t{0, 4}, base, false);
       const bool in_lo = (short)(uint16_t)two > (short)kLowest, in_hi = (int)two >= (kLowest + 1) * 65536;
       valid += __popcll(__ballot(in_lo)) + __popcll(__ballot(in_hi));
-      const uint32_t lo = (two & 0x7FFFu) + (two >> 6 & 0x1FFu), hi = (two >> 16 & 0x7FFFu) + (two >> 22 & 0x1FFu);
-      atomicAdd(&bins[in_lo ? lo : aside], 0x10000u ^ (neg_lo & 0x10001u));
-      atomicAdd(&bins[in_hi ? hi : aside], 0x10000u ^ (neg_hi & 0x10001u));
+      bump(in_lo ? lo : aside, __builtin_amdgcn_perm(0u, which, 0x0C010C00u));
+      bump(in_hi ? hi : aside, __builtin_amdgcn_perm(0u, which, 0x0C030C02u));
     });
     if (lane == 0) sh.valid[w] = valid;
     top = block_max(max((int)m[0], (int)m[1]));
