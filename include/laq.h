@@ -602,7 +602,7 @@ int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, in
  * Probabilities of batches with more than 16 / (Hq / Hkv) rows a sequence on
  * average are rounded to fp16 (half a step, 2^-11 of each) before they weigh
  * the values; sums and denominators are fp32.
- * One or two kernels: items of at most 128 query rows and a range of
+ * One or two kernels: items of at most 256 query rows and a range of
  * positions, and where a sequence's positions are split, the joining of its
  * ranges in position order.  The split follows the lengths on the device.
  *   workspace  [scratch] device memory, 16-byte aligned, any contents, at

@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
 // since a sequence of x units has ceil(x / chunk) < x / chunk + 1 ranges, at
 // most 2 x / chunk where it is split, and chunk >= (sum of tiles x units) Hkv / kItems.
 constexpr int kUnit = 64;
-constexpr int kSmallRows = 16, kLargeRows = 128;
+constexpr int kSmallRows = 16, kLargeRows = 256;
 // Blocks that run at once, two a compute unit.  (Measured on MI355X with 256 and
 // 1024: 16 decoding sequences 44 us -> 54 and 44, a chunk beside 15 of them 80
 // -> 104 and 83, three long sequences 160 -> 149 and 159.)
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // attention of prompts' chunks: the matrix cores bound it
 // ---------------------------------------------------------------------------
 
-// A block of four waves holds 128 query rows of one item, 32 a wave, and walks
+// A block of eight waves holds 256 query rows of one item, 32 a wave, and walks
 // the positions in tiles of 64.  Scores are formed transposed, keys (rows) x
 // queries (columns), so that a lane holds 32 scores of one query: the running
 // maximum and the denominator need one exchange between the two halves of the
@@ -686,14 +686,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // the fp32 sum of the unrounded ones.
 //
 // What bounds it: LDS bandwidth.  A wave's 32 rows need a tile's keys and
-// values from LDS whole, 40 KiB per wave and tile with the staging; a compute
-// unit's eight waves take 320 KiB for 8 x 32 matrix instructions.  (Measured
-// on MI355X: two prompts of 8192 and 4001 rows, 32:8 heads, 870 us, 780
-// TFLOP/s; a library's fp16 8192^3 product reaches 1150.  A tile takes a wave
+// values from LDS whole, 32 KiB a wave and tile, and the staging writes 32 KiB
+// a block: a compute unit's eight waves take 288 KiB for 8 x 32 matrix
+// instructions (as two blocks of 128 rows, 320 KiB and twice the staging
+// instructions: prompts 945 us, a chunk beside 15 decoding rows 80).  (Measured
+// on MI355X, kernel alone, without the joining: two prompts of 8192 and 4001
+// rows, 32:8 heads, 860 us back to back, 790 on a rested chip, 860 TFLOP/s; a
+// library's fp16 8192^3 product reaches 1150.  With 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
 // exponentials, 850 the value sums, 1100 issuing the next tile's loads and
-// stores.  Not faster: the two waves of a SIMD kept a phase apart, 890; the
-// operands of a tile's scores requested at once, 1040.)
+// stores.  Not faster: the two waves of a SIMD kept a phase apart, the operands
+// of a tile's scores requested at once.)
 //
 // Tiles of keys and values go memory -> registers -> LDS, two buffers, so that
 // a tile's loads are in flight while the one before is computed and a block
@@ -701,14 +704,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // and of value row r at p ^ 4 (r & 3): the operand reads touch each bank once.
 constexpr int kTile = 64;
 constexpr int kTileBytes = kTile * kHeadDim * 2;
+constexpr int kLargeThreads = 512;
 constexpr int kLargeLds = 4 * kTileBytes + 64;
 constexpr float kProbLog2 = 8.0f, kLagLog2 = 7.0f;
 
-__global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBatch pb, const uint16_t* __restrict__ q,
-                                                                         int R, int Hkv, int window, Out o_) {
+__global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kernel(PagedBatch pb,
+                                                                                   const uint16_t* __restrict__ q,
+                                                                                   int R, int Hkv, int window,
+                                                                                   Out o_) {
   extern __shared__ u32x4 large_lds[];
   char* const lds = reinterpret_cast<char*>(large_lds);
-  int* const flags = reinterpret_cast<int*>(lds + 4 * kTileBytes);  // [2]: tile whose values are not all finite
+  int* const flags = reinterpret_cast<int*>(lds + 4 * kTileBytes);  // [4]: tile (& 3) whose values are not all finite
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int w = uniform(tid >> 6);
@@ -742,47 +748,79 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
   const int* const table = pb.page_table + it.b * pb.table_stride;
   const uint16_t* const khead = pb.k + g * pb.head_stride;
   const uint16_t* const vhead = pb.v + g * pb.head_stride;
-  auto pages_from = [&](int t0) {  // page numbers of the 64 groups of 16 positions from t0 on
-    const int t = t0 + 16 * lane;
-    return t < sp.hi ? table[t >> pb.page_shift] : -1;
+  // Where the groups of 16 positions lie, 64 groups (16 tiles) at a time: a
+  // lane computes a group's byte offset from the head's first row, and the
+  // mask says which pages are there; a tile's loads then cost a few scalar
+  // instructions.  Two sets are held: rows are loaded two tiles before they
+  // are computed.
+  constexpr int kSet = 16;  // tiles
+  uint32_t set_lo = 0, set_hi = 0, old_lo = 0, old_hi = 0;
+  uint64_t set_there = 0, old_there = 0;
+  int set_first = 0;  // its first tile; the set before covers the kSet tiles before that
+  auto next_set = [&](int t) {
+    old_lo = set_lo, old_hi = set_hi, old_there = set_there;
+    const int at = sp.lo + t * kTile + 16 * lane;
+    const int page = at < sp.hi ? table[at >> pb.page_shift] : -1;
+    const bool there = (unsigned)page < (unsigned)pb.num_pages;
+    const uint64_t off = (uint64_t)(uint32_t)page * pb.page_bytes +
+                         (uint64_t)((uint32_t)at & ((1u << pb.page_shift) - 1)) * (uint32_t)(pb.slot_stride * 2);
+    set_lo = there ? (uint32_t)off : 0;
+    set_hi = there ? (uint32_t)(off >> 32) : 0;
+    set_there = __ballot(there);
+    set_first = t;
   };
-  int pages = pages_from(sp.lo), pages_at = sp.lo;
 
-  // Staging: thread (row tid / 16 of each group of 16, piece tid % 16).
+  // Staging: thread (row tid / 16 of each half of the tile, piece tid % 16);
+  // a wave's rows of a half lie in one group of 16.
   const int sr = tid >> 4, spc = tid & 15;
-  const uint32_t src_at = (uint32_t)sr * pb.slot_stride * 2 + 16 * spc;
-  u32x4 kreg[4], vreg[4];
-  int bad = 0;  // groups of the staged tile whose page is not there
-  auto load_tile = [&](int t0) {
-    if (t0 - pages_at >= 64 * 16) pages = pages_from(t0), pages_at = t0;
-    bad = 0;
+  const uint32_t src_at = (uint32_t)(sr & 15) * pb.slot_stride * 2 + 16 * spc;
+  u32x4 kreg[2], vreg[2];
+  // Groups of tile t whose page is not there, for the tiles of the two sets.
+  auto bad_of = [&](int t) {
+    const int i = (t - set_first) & (kSet - 1);
+    return (int)(~(t >= set_first ? set_there : old_there) >> 4 * i) & 15;
+  };
+  auto load_rows = [&](u32x4(&r)[2], const uint16_t* head, int t) {
+    const int i0 = (t - set_first) & (kSet - 1);
+    const bool now = t >= set_first;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int page = readlane(pages, (t0 - pages_at) / 16 + i);
-      bad |= (unsigned)page >= (unsigned)pb.num_pages ? 1 << i : 0;
-      const Rows16 at = rows16(pb, page, t0 + 16 * i, sp.hi);
-      kreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(khead, at), src_at, 0, 0);
-      vreg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(vhead, at), src_at, 0, 0);
+    for (int i = 0; i < 2; ++i) {
+      const int gr = 2 * i + (w >> 2), l = 4 * i0 + gr;
+      const uint32_t lo = readlane((int)(now ? set_lo : old_lo), l), hi = readlane((int)(now ? set_hi : old_hi), l);
+      const uint32_t there = (uint32_t)((now ? set_there : old_there) >> l) & 1;
+      const int left = sp.hi - (sp.lo + t * kTile + 16 * gr);  // (a page that is there has a row)
+      Rows16 at;
+      at.at = (uint64_t)hi << 32 | lo;
+      at.bytes = ((uint32_t)(min(left, 16) - 1) * (uint32_t)(pb.slot_stride * 2) + kHeadDim * 2) & -there;
+      r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_of(head, at), src_at, 0, 0);
     }
   };
-  auto is_masked = [&](int t0, int bad_groups) {
-    return (bad_groups != 0) | (t0 < sp.all_lo) | (t0 + kTile > sp.all_hi) | (t0 + kTile > sp.hi);
+  auto load_keys = [&](int t) {
+    if (t - set_first >= kSet) next_set(t);
+    load_rows(kreg, khead, t);
   };
-  auto store_tile = [&](int B, int t0) {
-    char* const kd = lds + B * 2 * kTileBytes;
-    char* const vd = kd + kTileBytes;
+  auto load_values = [&](int t) { load_rows(vreg, vhead, t); };
+  // Tiles that every row of the block sees whole: first .. last - 1.
+  const int whole_first = (max(sp.all_lo - sp.lo, 0) + kTile - 1) / kTile;
+  const int whole_last = max(min(sp.all_hi, sp.hi) - sp.lo, 0) / kTile;
+  auto is_masked = [&](int t) { return (bad_of(t) != 0) | (t < whole_first) | (t >= whole_last); };
+  auto store_keys = [&](int t) {
+    char* const d = lds + (t & 1) * 2 * kTileBytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 16 * i + sr;
-      *reinterpret_cast<u32x4*>(kd + r * 256 + 16 * (spc ^ (r & 15))) = kreg[i];
-      *reinterpret_cast<u32x4*>(vd + r * 256 + 16 * (spc ^ (4 * (r & 3)))) = vreg[i];
-    }
-    if (is_masked(t0, bad)) {
-      uint32_t nf = 0;
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<u32x4*>(d + (32 * i + sr) * 256 + 16 * (spc ^ (sr & 15))) = kreg[i];
+  };
+  // Values that are infinite or NaN stay out of masked tiles: 0 times one is NaN.
+  auto store_values = [&](int t) {
+    if (is_masked(t)) {
+      if (not_finite(vreg[0]) | not_finite(vreg[1])) flags[t & 3] = t;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) nf |= not_finite(vreg[i]);
-      if (nf) flags[B] = t0;
+      for (int i = 0; i < 2; ++i) vreg[i] = finite_or_zero(vreg[i]);
     }
+    char* const d = lds + (t & 1) * 2 * kTileBytes + kTileBytes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      *reinterpret_cast<u32x4*>(d + (32 * i + sr) * 256 + 16 * (spc ^ (4 * (sr & 3)))) = vreg[i];
   };
 
   float ref = kNoMax, l = 0.0f;
@@ -792,44 +830,44 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
 
-  auto compute = [&](auto mc, int B, int t0, int bad_groups) {
-    constexpr bool MASKED = decltype(mc)::value;
-    // (the two forms share no code: what the compiler moved out of both would be held in registers beyond 256)
-    if constexpr (MASKED) asm volatile("; masked" ::: "memory");
-    else asm volatile("; whole" ::: "memory");
+  // Scores of a tile: keys from buffer B.
+  auto scores = [&](float16_t(&s)[2], int B) {
     const char* const kd = lds + B * 2 * kTileBytes;
-    const char* const vd = kd + kTileBytes;
-    float16_t s[2];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks) {
         const half8_t a = *reinterpret_cast<const half8_t*>(kd + (32 * kt + n) * 256 + 16 * ((2 * ks + h) ^ (n & 15)));
         s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, qf[ks], s[kt], 0, 0, 0);
       }
-    }
-    if constexpr (MASKED) {
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int at = t0 + 32 * kt + 8 * (r >> 2) + 4 * h + (r & 3);
-          const bool there = !(bad_groups >> (2 * kt + (r >> 3)) & 1) & (at < sp.hi);
-          s[kt][r] = (there & (at >= see_lo) & (at < see_hi)) ? s[kt][r] : -INFINITY;
-        }
-    }
-    float mx = s[0][0];
+  };
+  auto mask = [&](float16_t(&s)[2], int t0, int bad_groups) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][r]);
-    {
-      auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx), __builtin_bit_cast(uint32_t, mx),
-                                                false, false);
-      mx = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
+      for (int r = 0; r < 16; ++r) {
+        const int at = t0 + 32 * kt + 8 * (r >> 2) + 4 * h + (r & 3);
+        const bool there = !(bad_groups >> (2 * kt + (r >> 3)) & 1) & (at < sp.hi);
+        s[kt][r] = (there & (at >= see_lo) & (at < see_hi)) ? s[kt][r] : -INFINITY;
+      }
+  };
+  // The reference follows the scores that are used next; sums so far are rescaled.
+  auto follow = [&](const float16_t(&s)[2]) {
+    float m4[4];  // four chains
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m4[i] = fmaxf(s[0][i], s[1][i]);
+#pragma unroll
+      for (int r = 4; r < 16; r += 4) m4[i] = fmaxf(m4[i], fmaxf(s[0][r + i], s[1][r + i]));
     }
+    float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+    auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx), __builtin_bit_cast(uint32_t, mx), false,
+                                              false);
+    mx = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
     if (__ballot(mx > ref + kLagLog2)) {
       const float mn = mx > ref + kLagLog2 ? mx : ref;  // each query by itself: no row depends on its neighbours
       const float alpha = __builtin_amdgcn_exp2f(ref - mn);
@@ -840,91 +878,106 @@ __global__ __launch_bounds__(256, 2) void paged_attention_rows128_kernel(PagedBa
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
     }
+  };
+  auto probabilities = [&](half8_t(&pf)[4], const float16_t(&s)[2]) {
     const float bias = kProbLog2 - ref;
-    half8_t pf[4];
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kt][r], kScaleLog2, bias));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kt][r + 1], kScaleLog2, bias));
-        l += p0 + p1;
-        const half2_t pk = __builtin_convertvector((float2_t{p0, p1}), half2_t);
-        pf[2 * kt + (r >> 3)][r & 7] = pk[0];
-        pf[2 * kt + (r >> 3)][(r & 7) + 1] = pk[1];
-      }
-    // values: 16 lanes read 4 positions x 16 dimensions and receive a column each
-    const int gl = lane & 15;
-    const int vrow = 4 * h + (gl >> 2);
-    const int vcol = 16 * ((lane >> 4) & 1) + 4 * (gl & 3);  // dimension within 32
-    bool nf = false;
-    if constexpr (MASKED) nf = uniform(flags[B]) == t0;
+      for (int r = 0; r < 16; r += 4) {
+        float p[4];
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
+        for (int i = 0; i < 4; ++i) p[i] = fmaf(s[kt][r + i], kScaleLog2, bias);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += p[i];
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const half2_t pk = __builtin_convertvector((float2_t{p[i], p[i + 1]}), half2_t);
+          pf[2 * kt + (r >> 3)][(r & 7) + i] = pk[0];
+          pf[2 * kt + (r >> 3)][(r & 7) + i + 1] = pk[1];
+        }
+      }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  // Value sums: 16 lanes read 4 positions x 16 dimensions and receive a column each.
+  const int vrow = 4 * h + (lane & 15) / 4;
+  const int vcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);  // dimension within 32
+  auto value_sums = [&](const half8_t(&pf)[4], int B) {
+    typedef short short4_t __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) short4_t lds_short4;
+    const char* const vd = lds + B * 2 * kTileBytes + kTileBytes;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
-        typedef short short4_t __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) short4_t lds_short4;
         const int piece = (32 * d + vcol) >> 3;
-        const int ra = 16 * ks + vrow;  // vrow + 8: the same bits 0 and 1
-        const char* const a = vd + ra * 256 + 16 * (piece ^ (4 * (ra & 3))) + 2 * (vcol & 7);
+        const char* const a = vd + (16 * ks + vrow) * 256 + 16 * (piece ^ (4 * (vrow & 3))) + 2 * (vcol & 7);
         const short4_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a));
         const short4_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a + 8 * 256));
-        u32x4 v = __builtin_bit_cast(u32x4, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
-        if constexpr (MASKED)
-          if (nf) v = finite_or_zero(v);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, v), pf[ks], o[d], 0, 0, 0);
+        const half8_t v = __builtin_bit_cast(half8_t, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[ks], o[d], 0, 0, 0);
       }
-    }
-    if constexpr (MASKED) {
-      // Values that are infinite or NaN were left out of the product (0 times
-      // one is NaN): the rows that see one receive it here, whatever its weight.
-      if (nf) {
-        typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            const int piece = 4 * d + (r >> 2);
+  };
+  // The rows that see a value that was left out receive it here, from memory,
+  // whatever its weight (the result is infinite or NaN).
+  auto add_not_finite = [&](int t) {
+    typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
 #pragma unroll 1
-            for (int t = 0; t < kTile; ++t) {
-              const int at = t0 + t;
-              const bool sees =
-                  (at < sp.hi) & !(bad_groups >> (t >> 4) & 1) & (at >= see_lo) & (at < see_hi);
-              const half4_t x = *reinterpret_cast<const half4_t*>(vd + t * 256 + 16 * (piece ^ (4 * (t & 3))) + 8 * h);
+    for (int i = 0; i < kTile; ++i) {
+      const int at = sp.lo + t * kTile + i;
+      if (at >= sp.hi) break;
+      const int page = table[at >> pb.page_shift];
+      if ((unsigned)page >= (unsigned)pb.num_pages) continue;
+      const uint16_t* const row = vhead + (int64_t)page * (pb.page_bytes / 2) +
+                                  (int64_t)(at & ((1 << pb.page_shift) - 1)) * pb.slot_stride;
+      const bool sees = (at >= see_lo) & (at < see_hi);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float add = fabsf((float)x[e]) < INFINITY ? 0.0f : (float)x[e];
-                o[d][r + e] += sees ? add : 0.0f;
-              }
-            }
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const half4_t x = *reinterpret_cast<const half4_t*>(row + 32 * d + 2 * r + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float add = fabsf((float)x[e]) < INFINITY ? 0.0f : (float)x[e];
+            o[d][r + e] += sees ? add : 0.0f;
           }
-      }
+        }
     }
   };
 
-  if (tid < 2) flags[tid] = -1;
-  __syncthreads();
-  if (sp.lo < sp.hi) {
-    load_tile(sp.lo);
-    int bad_now = bad;
-    store_tile(0, sp.lo);
-    int B = 0;
-    if (sp.lo + kTile < sp.hi) load_tile(sp.lo + kTile);
+  const int tiles = sp.hi > sp.lo ? (sp.hi - sp.lo + kTile - 1) / kTile : 0;
+  // Tiles of which some row of the wave sees something.
+  const int want_first = max(wave_lo - sp.lo, 0) / kTile;
+  const int want_last = min(tiles, (max(wave_hi - sp.lo, 0) + kTile - 1) / kTile);
+  auto wanted = [&](int t) { return (t >= want_first) & (t < want_last); };
+  float16_t s[2];
+  half8_t pf[4];
+  if (tid < 4) flags[tid] = -1;
+  if (tiles > 0) {
+    next_set(0);
+    load_keys(0);
+    load_values(0);
     __syncthreads();
-    for (int t0 = sp.lo; t0 < sp.hi; t0 += kTile) {
-      const int bad_next = bad;
-      if (t0 + kTile < sp.hi) store_tile(B ^ 1, t0 + kTile);
-      if (t0 + 2 * kTile < sp.hi) load_tile(t0 + 2 * kTile);
-      if (t0 < wave_hi && t0 + kTile > wave_lo) {
-        if (is_masked(t0, bad_now))
-          compute(std::true_type{}, B, t0, bad_now);
-        else
-          compute(std::false_type{}, B, t0, 0);
+    store_keys(0);
+    store_values(0);
+    if (tiles > 1) load_keys(1), load_values(1);
+    __syncthreads();
+#pragma unroll 1
+    for (int t = 0; t < tiles; ++t) {
+      if (t + 1 < tiles) store_keys(t + 1), store_values(t + 1);
+      if (t + 2 < tiles) load_keys(t + 2), load_values(t + 2);
+      if (wanted(t)) {
+        scores(s, t & 1);
+        if (is_masked(t)) mask(s, sp.lo + t * kTile, bad_of(t));
+        follow(s);
+        probabilities(pf, s);
+        value_sums(pf, t & 1);
+        if (uniform(flags[t & 3]) == t) add_not_finite(t);
       }
       __syncthreads();
-      B ^= 1;
-      bad_now = bad_next;
     }
   }
   // the two halves of the wave hold different positions' parts of the denominator
@@ -1072,7 +1125,7 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   p.items = tiles + (split ? per_head : 0);
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
-  p.records = split ? std::min(2 * per_head, tiles * most) : 0;
+  p.records = split ? std::min(2 * kItems / Hkv, tiles * most) : 0;
   p.floats = p.records * Hkv * BM * (kHeadDim + 2);
   return p;
 }
@@ -1124,8 +1177,8 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
   const int64_t most_rows = std::min<int64_t>(p.large ? kLargeRows : kSmallRows, pb.T * R);
   const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? (most_rows + 15) / 16 : most_rows));
   if (p.large) {
-    launch(paged_attention_rows128_kernel, grid, dim3(256), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv, (int)window,
-           o);
+    launch(paged_attention_rows256_kernel, grid, dim3(kLargeThreads), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv,
+           (int)window, o);
     if (p.split_tiles > 0 && p.split_tiles * Hkv <= kFewTiles)
       launch((paged_attention_join_kernel<kLargeRows, 4>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv,
              (int)window, o);
