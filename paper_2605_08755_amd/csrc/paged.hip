@@ -1020,8 +1020,11 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
 // by 2^(their maximum - the largest of all); a lane holds two dimensions.
 // WAVES == 4: a block per row, its waves take every fourth record and meet in
 // LDS (decoding: few rows, many ranges).  WAVES == 1: a wave per four rows,
-// 16 rows a block (a chunk's rows have few ranges each, and most blocks of the
-// grid find nothing to do: they cost their search).
+// 16 rows a block at a time (a chunk's rows have few ranges each).  Most blocks
+// of the grid can find nothing to do and cost their search, so there are about
+// kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
+// prompts whose tiles are not split, 16.4 -> 4.9 us; a chunk beside 15 decoding
+// rows, 14.5 -> 15.1, of the bytes of its records; twice the blocks, 8.7 and 17.)
 template <int BM, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
@@ -1035,75 +1038,78 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
-  const int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4;
-  if (row >= rows) return;  // WAVES == 4: the whole block
   const int first = WAVES == 4 ? w : 0;
   const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
-  const float *stat[kRows], *sums[kRows];
-  float2_t x[kRows][kB], st[kRows][kB], num[kRows];
-  float M[kRows], den[kRows];
-#pragma unroll
-  for (int k = 0; k < kRows; ++k) {
-    const int r = min(row + k, rows - 1);
-    stat[k] = base + BM * kHeadDim + 2 * r;
-    sums[k] = base + r * kHeadDim + 2 * lane;
-    num[k] = float2_t{0.0f, 0.0f};
-    M[k] = kNoMax, den[k] = 0.0f;
-  }
-  auto load = [&](int s0) {
-#pragma unroll
-    for (int k = 0; k < kRows; ++k)
-#pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        const int64_t s = min(s0 + WAVES * i, it.splits - 1);
-        st[k][i] = *reinterpret_cast<const float2_t*>(stat[k] + s * kRec);
-        x[k][i] = *reinterpret_cast<const float2_t*>(sums[k] + s * kRec);
-      }
-  };
-  load(first);  // before the statistics: up to WAVES * kB ranges cost one memory round trip
-  auto over_rows = [](float v, auto&& op) {  // of a value per 16-lane row
-    const int u = __builtin_bit_cast(int, v);
-    auto f = [](int x) { return __builtin_bit_cast(float, x); };
-    return op(op(f(readlane(u, 0)), f(readlane(u, 16))), op(f(readlane(u, 32)), f(readlane(u, 48))));
-  };
-  for (int s0 = 0; s0 < it.splits; s0 += 64) {
+  // WAVES == 4: a row, the same for the whole block; else every gridDim.y-th group of 16
+#pragma unroll 1
+  for (int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4; row < rows; row += 16 * gridDim.y) {
+    const float *stat[kRows], *sums[kRows];
+    float2_t x[kRows][kB], st[kRows][kB], num[kRows];
+    float M[kRows], den[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      const int s = s0 + lane;
-      const float2_t y = *reinterpret_cast<const float2_t*>(stat[k] + (int64_t)min(s, it.splits - 1) * kRec);
-      const float top = fmaxf(M[k], over_rows(row_max(y[0]), [](float a, float b) { return fmaxf(a, b); }));
-      const float sum = over_rows(row_sum(s < it.splits ? __builtin_amdgcn_exp2f(y[0] - top) * y[1] : 0.0f),
-                                  [](float a, float b) { return a + b; });
-      den[k] = fmaf(den[k], __builtin_amdgcn_exp2f(M[k] - top), sum);
-      M[k] = top;
+      const int r = min(row + k, rows - 1);
+      stat[k] = base + BM * kHeadDim + 2 * r;
+      sums[k] = base + r * kHeadDim + 2 * lane;
+      num[k] = float2_t{0.0f, 0.0f};
+      M[k] = kNoMax, den[k] = 0.0f;
     }
-  }
-  for (int s0 = first; s0 < it.splits; s0 += WAVES * kB) {
-    if (s0 > first) load(s0);
+    auto load = [&](int s0) {
 #pragma unroll
-    for (int k = 0; k < kRows; ++k)
+      for (int k = 0; k < kRows; ++k)
 #pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[k][i][0] - M[k]) : 0.0f;
-        num[k][0] = fmaf(e, x[k][i][0], num[k][0]);
-        num[k][1] = fmaf(e, x[k][i][1], num[k][1]);
+        for (int i = 0; i < kB; ++i) {
+          const int64_t s = min(s0 + WAVES * i, it.splits - 1);
+          st[k][i] = *reinterpret_cast<const float2_t*>(stat[k] + s * kRec);
+          x[k][i] = *reinterpret_cast<const float2_t*>(sums[k] + s * kRec);
+        }
+    };
+    load(first);  // before the statistics: up to WAVES * kB ranges cost one memory round trip
+    auto over_rows = [](float v, auto&& op) {  // of a value per 16-lane row
+      const int u = __builtin_bit_cast(int, v);
+      auto f = [](int x) { return __builtin_bit_cast(float, x); };
+      return op(op(f(readlane(u, 0)), f(readlane(u, 16))), op(f(readlane(u, 32)), f(readlane(u, 48))));
+    };
+    for (int s0 = 0; s0 < it.splits; s0 += 64) {
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        const int s = s0 + lane;
+        const float2_t y = *reinterpret_cast<const float2_t*>(stat[k] + (int64_t)min(s, it.splits - 1) * kRec);
+        const float top = fmaxf(M[k], over_rows(row_max(y[0]), [](float a, float b) { return fmaxf(a, b); }));
+        const float sum = over_rows(row_sum(s < it.splits ? __builtin_amdgcn_exp2f(y[0] - top) * y[1] : 0.0f),
+                                    [](float a, float b) { return a + b; });
+        den[k] = fmaf(den[k], __builtin_amdgcn_exp2f(M[k] - top), sum);
+        M[k] = top;
       }
-  }
-  if constexpr (WAVES == 4) {
-    part[w][lane] = num[0];
-    __syncthreads();
-    if (w > 0) return;
-    num[0] = part[0][lane];
+    }
+    for (int s0 = first; s0 < it.splits; s0 += WAVES * kB) {
+      if (s0 > first) load(s0);
 #pragma unroll
-    for (int i = 1; i < 4; ++i) num[0] += part[i][lane];
-  }
+      for (int k = 0; k < kRows; ++k)
 #pragma unroll
-  for (int k = 0; k < kRows; ++k) {
-    if (row + k >= rows) break;
-    const int r = r0 + row + k;
-    const float inv = den[k] == 0.0f ? 0.0f : 1.0f / den[k];
-    *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
-        half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
+        for (int i = 0; i < kB; ++i) {
+          const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[k][i][0] - M[k]) : 0.0f;
+          num[k][0] = fmaf(e, x[k][i][0], num[k][0]);
+          num[k][1] = fmaf(e, x[k][i][1], num[k][1]);
+        }
+    }
+    if constexpr (WAVES == 4) {
+      part[w][lane] = num[0];
+      __syncthreads();
+      if (w > 0) return;
+      num[0] = part[0][lane];
+#pragma unroll
+      for (int i = 1; i < 4; ++i) num[0] += part[i][lane];
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      if (row + k >= rows) break;
+      const int r = r0 + row + k;
+      const float inv = den[k] == 0.0f ? 0.0f : 1.0f / den[k];
+      *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
+          half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
+    }
+    if constexpr (WAVES == 4) return;
   }
 }
 
@@ -1172,10 +1178,11 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
   const Out o{out, ws, (int)Hq, (int)p.records};
   const dim3 grid((unsigned)(p.items * Hkv));
   // A block joins one row; 16 rows where the tiles (most of them not split) would make many blocks.
-  constexpr int64_t kFewTiles = 32;
+  constexpr int64_t kFewTiles = 32, kJoinBlocks = 2048;
   const bool many = p.large && p.split_tiles * Hkv > kFewTiles;
   const int64_t most_rows = std::min<int64_t>(p.large ? kLargeRows : kSmallRows, pb.T * R);
-  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? (most_rows + 15) / 16 : most_rows));
+  const int64_t by_16 = std::min((most_rows + 15) / 16, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
+  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_16 : most_rows));
   if (p.large) {
     launch(paged_attention_rows256_kernel, grid, dim3(kLargeThreads), kLargeLds, stream, e1, pb, q, (int)R, (int)Hkv,
            (int)window, o);
