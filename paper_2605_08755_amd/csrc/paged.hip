@@ -1088,9 +1088,10 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
       for (int k = 0; k < kRows; ++k)
 #pragma unroll
         for (int i = 0; i < kB; ++i) {
-          const float e = s0 + WAVES * i < it.splits ? __builtin_amdgcn_exp2f(st[k][i][0] - M[k]) : 0.0f;
-          num[k][0] = fmaf(e, x[k][i][0], num[k][0]);
-          num[k][1] = fmaf(e, x[k][i][1], num[k][1]);
+          const bool in = s0 + WAVES * i < it.splits;  // else the last record again: its sums may be infinite
+          const float e = in ? __builtin_amdgcn_exp2f(st[k][i][0] - M[k]) : 0.0f;
+          num[k][0] = fmaf(e, in ? x[k][i][0] : 0.0f, num[k][0]);
+          num[k][1] = fmaf(e, in ? x[k][i][1] : 0.0f, num[k][1]);
         }
     }
     if constexpr (WAVES == 4) {

@@ -381,6 +381,35 @@ def test_attention_missing_pages_inside():
         run_attention(rng, bt, Hq)
 
 
+@pytest.mark.parametrize("tokens,before,Hq,Hkv,ps,window", [
+    ([255, 1, 0, 3], [1500, 300, 0, 1000], 1, 1, 16, 0),  # one row fewer than a block of 256 holds
+    ([257, 2], [1800, 1023], 1, 1, 16, 0),                # and one more
+    ([300, 5], [2300, 1100], 2, 1, 64, 1100),
+    ([5] * 40 + [300] + [5] * 30, [20] * 40 + [1500] + [100] * 30, 4, 2, 16, 0),  # few joining blocks a tile
+])
+def test_attention_chunks_over_many_tiles(tokens, before, Hq, Hkv, ps, window):
+    """Chunks of several blocks of rows over more positions than one set of
+    page offsets covers (1024), pages missing around its ends, and infinities
+    among the values that some rows of a block do not see."""
+    say("attention many tiles", tokens[:4], Hq, Hkv, window)
+    rng = np.random.default_rng(len(tokens) + Hq + ps)
+    bt = Batch(rng, tokens, before, ps, Hkv)
+    long = int(np.argmax(bt.lens))
+    for at in (1000, 1023, 1024, 2040, 2064):
+        if at < bt.lens[long]:
+            bt.table[long, at // ps] = -1 if at != 1024 else bt.P
+    q, clean = run_attention(rng, bt, Hq, window)
+    at = int(bt.lens[long]) - 2  # the last two rows see it
+    bt.v[bt.table[long, at // ps], 0, at % ps, ::5] = -np.inf
+    out = laq.paged_attention(dev(q), *bt.device(), window=window).cpu().numpy()
+    R = Hq // Hkv
+    for r, b, pos in OS.rows(bt.start, bt.lens):
+        if b == long and pos >= at:
+            assert (out[r, :R, ::5] == -np.inf).all()
+            out[r, :R, ::5] = clean[r, :R, ::5]
+    assert np.array_equal(out.view(np.uint16), clean.view(np.uint16))
+
+
 def test_attention_far_pages():
     """Pages past 2^31 elements of the cache; the other pages are never read."""
     say("attention far pages")
