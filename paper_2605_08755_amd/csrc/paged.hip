@@ -221,13 +221,14 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
 // most 2 x / chunk where it is split, and chunk >= (sum of tiles x units) Hkv / kItems.
 constexpr int kUnit = 64;
 constexpr int kSmallRows = 16, kLargeRows = 256;
-// Blocks that run at once, two a compute unit.  (Measured on MI355X with 256 and
-// 1024: 16 decoding sequences 44 us -> 54 and 44, a chunk beside 15 of them 80
-// -> 104 and 83, three long sequences 160 -> 149 and 159.)
+// Blocks of 16 rows that run at once, two a compute unit; twice the blocks of
+// 256.  (Measured on MI355X with 256 and 1024: 16 decoding sequences 44 us -> 54
+// and 44, three long ones 160 -> 149 and 159, a chunk beside 15 decoding rows 70
+// -> 84 and 78, without the joining.)
 constexpr int kItems = 512;
 // Units: a shorter range costs more in records than it gains.  (Measured on
 // MI355X: one token at 300 positions 7.4 us with 2, 9.5 with 4; a chunk of 16
-// rows at 6000, 18 us with 4, 18 with 3, 22 with 2.)
+// rows at 6000, 16.3 us with 4, 17.4 with 3, 22 with 2.)
 template <int BM>
 constexpr int kMinChunk = BM == kSmallRows ? 2 : 4;
 
@@ -691,7 +692,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // instructions (as two blocks of 128 rows, 320 KiB and twice the staging
 // instructions: prompts 945 us, a chunk beside 15 decoding rows 80).  (Measured
 // on MI355X, kernel alone, without the joining: two prompts of 8192 and 4001
-// rows, 32:8 heads, 860 us back to back, 790 on a rested chip, 860 TFLOP/s; a
+// rows, 32:8 heads, 860 us back to back, 790 the shortest, 860 TFLOP/s; a
 // library's fp16 8192^3 product reaches 1150.  With 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
 // exponentials, 850 the value sums, 1100 issuing the next tile's loads and
@@ -1024,7 +1025,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
 // of the grid can find nothing to do and cost their search, so there are about
 // kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
 // prompts whose tiles are not split, 16.4 -> 4.9 us; a chunk beside 15 decoding
-// rows, 14.5 -> 15.1, of the bytes of its records; twice the blocks, 8.7 and 17.)
+// rows, 14.5 -> 15.5, of the bytes of its records; twice the blocks, 8.7 and 17.)
 template <int BM, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
@@ -1138,9 +1139,9 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
 }
 
 // Up to 16 rows per sequence on average go to the 16-row kernel.  (Measured on
-// MI355X, 16-row -> 128-row kernel at twice and four times that: 32:8 heads, one
-// sequence of 6000, 20 -> 17 and 25 -> 19 us; eight of 2000, 35 -> 28 and 54 ->
-// 33; 64:8, four of 8000, 50 -> 44 and 79 -> 47; but one of 500 rows 12 -> 16.5.)
+// MI355X, 16-row -> 256-row kernel at twice and four times that: 32:8 heads, one
+// sequence of 6000, 20 -> 14.5 and 25 -> 16 us; eight of 2000, 35 -> 29 and 52 ->
+// 34; 64:8, four of 8000, 47 -> 43 and 75 -> 51; but one of 500, 12 -> 15.)
 AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
   if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity);
   return plan_of<kLargeRows>(B, T, R, Hkv, capacity);
