@@ -562,7 +562,7 @@ typedef struct laq_paged_batch {
     int64_t table_pages;        /* entries of a table row; x page_size <= 2^30 */
     int64_t table_stride;       /* elements between table rows, >= table_pages */
     int64_t B;                  /* sequences, 0..2^20 */
-    int64_t T;                  /* rows, padding included; T * Hq <= 2^30 */
+    int64_t T;                  /* rows, padding included; below 2^26, T * Hq <= 2^30 */
 } laq_paged_batch;
 
 /* laq_paged_append_f16 -- laq_qk_norm_rope_f16 for every row of a batch: row

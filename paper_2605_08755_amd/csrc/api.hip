@@ -556,8 +556,9 @@ laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int
   if (head_dim != kHeadDimAbi) return fail(LAQ_ERR_BAD_SHAPE, fn, "head_dim must be 128");
   if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096)
     return fail(LAQ_ERR_BAD_SHAPE, fn, "Hq must be a positive multiple of Hkv, at most 4096");
-  if (b->B < 0 || b->B > (1 << 20) || b->T < 0 || b->T > (1LL << 30) || b->T * Hq > (1LL << 30))
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= B <= 2^20 and 0 <= T, T * Hq <= 2^30");
+  // (a wave per row: 2^26 rows would be 2^32 threads, more than one launch may have)
+  if (b->B < 0 || b->B > (1 << 20) || b->T < 0 || b->T >= (1LL << 26) || b->T * Hq > (1LL << 30))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= B <= 2^20, 0 <= T < 2^26 and T * Hq <= 2^30");
   if (b->page_size < 16 || b->page_size > (1 << 20) || (b->page_size & (b->page_size - 1)) != 0)
     return fail(LAQ_ERR_BAD_SHAPE, fn, "page_size must be a power of two from 16 to 2^20");
   if (b->num_pages < 1 || b->num_pages > 0x7FFFFFFFLL) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= num_pages < 2^31");
@@ -655,7 +656,7 @@ laq_status laq_paged_attention_f16(const laq_paged_batch* batch, const void* q, 
   if (need > 0 && !workspace) return fail(LAQ_ERR_NULL_POINTER, fn, "null workspace");
   if (workspace_bytes < need)
     return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below laq_paged_attention_workspace_bytes");
-  if (laq::paged_attention_grid(batch->B, batch->T, Hq, Hkv, capacity) > 0x7FFFFFFFLL)
+  if (laq::paged_attention_threads(batch->B, batch->T, Hq, Hkv, capacity) > 0xFFFFFFFFLL)
     return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
     return fail(LAQ_ERR_MISALIGNED, fn, "q, out and workspace must be 16-byte aligned");

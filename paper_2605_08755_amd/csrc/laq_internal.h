@@ -264,10 +264,10 @@ struct PagedBatch {
 hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
                                const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv,
                                float eps, uint16_t* q_out, hipStream_t stream, const LaunchEvents& ev);
-// Workspace bytes and blocks of the attention, for any lengths within the
+// Workspace bytes and threads of the attention, for any lengths within the
 // table's capacity (positions a sequence can have).
 int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
-int64_t paged_attention_grid(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+int64_t paged_attention_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
 hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,
                                   uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev);
 hipError_t launch_sample(const uint16_t* logits, int64_t stride, int64_t rows, int64_t V, const float* u,

@@ -1164,8 +1164,9 @@ int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv,
   return attention_plan(B, T, Hq / Hkv, Hkv, capacity).floats * (int64_t)sizeof(float);
 }
 
-int64_t paged_attention_grid(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
-  return attention_plan(B, T, Hq / Hkv, Hkv, capacity).items * Hkv;
+int64_t paged_attention_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  const AttentionPlan p = attention_plan(B, T, Hq / Hkv, Hkv, capacity);
+  return p.items * Hkv * (p.large ? kLargeThreads : 64 * kWaves);
 }
 
 hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,

@@ -112,6 +112,15 @@ def test_attention_refusals(L):
         assert attention(L, **{f: FAKE + o}) == laq.LAQ_ERR_MISALIGNED
 
 
+def test_launch_size_refusals(L):
+    """What would take 2^32 threads or more is refused, not left to the launch."""
+    for call in (append, attention):
+        assert call(L, Hq=1, Hkv=1, T=1 << 26) == laq.LAQ_ERR_BAD_SHAPE
+    for Hq, Hkv, B, T in ((1024, 1024, 1 << 20, 1 << 20), (16, 16, 1 << 20, (1 << 26) - 1)):
+        assert attention(L, Hq=Hq, Hkv=Hkv, B=B, T=T) == laq.LAQ_ERR_BAD_SHAPE
+        assert b"too many rows" in L.laq_last_error()
+
+
 def test_attention_workspace_query(L):
     f = L.laq_paged_attention_workspace_bytes
     for args in ((0, 1, 8, 8, 100), (1, 0, 8, 8, 100), (1, 1, 0, 8, 100), (1, 1, 8, 3, 100), (1, 1, 8, 8, 0),
