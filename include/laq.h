@@ -640,7 +640,7 @@ laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, 
  *   token [out] int32 [rows].  prob [out] fp32 [rows], or NULL.
  * rows == 0: nothing is done.
  * Errors: NULL_POINTER (logits, u, token); BAD_SHAPE (V outside 1..2^24, rows
- * < 0 or >= 2^31, logits_stride below V or above 2^32); MISALIGNED (logits
+ * < 0 or >= 2^22, logits_stride below V or above 2^32); MISALIGNED (logits
  * 2-byte, the others 4-byte). */
 laq_status laq_sample_f16(const void *logits, int64_t logits_stride, int64_t rows, int64_t V, const float *u,
                           const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,

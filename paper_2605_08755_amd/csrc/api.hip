@@ -671,7 +671,8 @@ laq_status laq_sample_f16(const void* logits, int64_t logits_stride, int64_t row
                           int32_t* token, float* prob, void* stream) {
   const char* fn = "laq_sample_f16";
   const laq::LaunchEvents ev = take_events();
-  if (rows < 0 || rows > 0x7FFFFFFFLL) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= rows < 2^31");
+  // (1024 threads a row: 2^22 rows would be 2^32 threads, more than one launch may have)
+  if (rows < 0 || rows >= (1LL << 22)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= rows < 2^22");
   if (V < 1 || V > (1 << 24)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= V <= 2^24");
   if (logits_stride < V && rows > 1) return fail(LAQ_ERR_BAD_SHAPE, fn, "logits_stride must be at least V");
   if (logits_stride < 0 || logits_stride > (1LL << 32)) return fail(LAQ_ERR_BAD_SHAPE, fn, "logits_stride must be in 0..2^32");

@@ -119,6 +119,7 @@ def test_launch_size_refusals(L):
     for Hq, Hkv, B, T in ((1024, 1024, 1 << 20, 1 << 20), (16, 16, 1 << 20, (1 << 26) - 1)):
         assert attention(L, Hq=Hq, Hkv=Hkv, B=B, T=T) == laq.LAQ_ERR_BAD_SHAPE
         assert b"too many rows" in L.laq_last_error()
+    assert sample(L, rows=1 << 22) == laq.LAQ_ERR_BAD_SHAPE
 
 
 def test_attention_workspace_query(L):
