@@ -507,6 +507,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
   // are in flight (compile-time, so that the waits for this step's values,
   // which the compiler counts, leave them in flight).
   auto step = [&](auto bc, auto mc, int p) {
+#pragma clang fp contract(off)  // a scaled score is rounded before the maximum, rounded alike, is subtracted
     constexpr int B = decltype(bc)::value;
     constexpr bool MORE = decltype(mc)::value;
     __builtin_amdgcn_sched_barrier(0);
@@ -708,6 +709,7 @@ constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kLargeThreads = 512;
 constexpr int kLargeLds = 4 * kTileBytes + 64;
 constexpr float kProbLog2 = 8.0f, kLagLog2 = 7.0f;
+constexpr float kFarLog2 = 65536.0f;
 
 __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kernel(PagedBatch pb,
                                                                                    const uint16_t* __restrict__ q,
@@ -856,8 +858,16 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
         s[kt][r] = (there & (at >= see_lo) & (at < see_hi)) ? s[kt][r] : -INFINITY;
       }
   };
-  // The reference follows the scores that are used next; sums so far are rescaled.
-  auto follow = [&](const float16_t(&s)[2]) {
+  // The reference follows the scores that are used next; sums so far are
+  // rescaled.  A probability's exponent is then scale x s + bias, fused.  Past
+  // |ref| = kFarLog2 a score's scaled value is rounded before ref is subtracted
+  // from it: fused, the difference keeps the rounding of ref alone, up to half a
+  // step of it (2^12 at the largest scores of fp16 inputs, where ref is 2^36:
+  // probabilities would be infinite).  Rounded alike, the largest score is ref.
+  uint64_t far_rows = 0;  // lanes of which that is so
+  float bias, scale;
+  auto follow = [&](float16_t(&s)[2]) {
+#pragma clang fp contract(off)
     float m4[4];  // four chains
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -869,8 +879,11 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
     auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx), __builtin_bit_cast(uint32_t, mx), false,
                                               false);
     mx = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
-    if (__ballot(mx > ref + kLagLog2)) {
-      const float mn = mx > ref + kLagLog2 ? mx : ref;  // each query by itself: no row depends on its neighbours
+    // (the difference, which is exact where they are near: ref + 7 may be rounded to ref + 8)
+    const bool ahead = mx - ref > kLagLog2;
+    scale = kScaleLog2;
+    if (__ballot(ahead) | far_rows) {
+      const float mn = ahead ? mx : ref;  // each query by itself: no row depends on its neighbours
       const float alpha = __builtin_amdgcn_exp2f(ref - mn);
       ref = mn;
       l *= alpha;
@@ -878,10 +891,22 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      const bool far = fabsf(ref) > kFarLog2 && ref != kNoMax;
+      far_rows = __ballot(far);
+      if (far_rows) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float scaled = s[kt][r] * kScaleLog2;
+            s[kt][r] = far ? scaled - ref : s[kt][r];
+          }
+        scale = far ? 1.0f : kScaleLog2;
+      }
     }
+    bias = kProbLog2 - (scale == 1.0f ? 0.0f : ref);
   };
   auto probabilities = [&](half8_t(&pf)[4], const float16_t(&s)[2]) {
-    const float bias = kProbLog2 - ref;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
@@ -889,7 +914,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
       for (int r = 0; r < 16; r += 4) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = fmaf(s[kt][r + i], kScaleLog2, bias);
+        for (int i = 0; i < 4; ++i) p[i] = fmaf(s[kt][r + i], scale, bias);
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = __builtin_amdgcn_exp2f(p[i]);
 #pragma unroll

@@ -1,0 +1,96 @@
+"""Batched serving on the GPU where its arithmetic is at its edges, against the
+float64 oracle (oracle/serving.py)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as OS
+from paper_2605_08755_amd import laq
+from test_gpu_serving import Batch, dev, f16, say
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+
+
+def attend(q, bt, window=0):
+    out = laq.paged_attention(dev(q), *bt.device(), window=window)
+    torch.cuda.synchronize()
+    return out.cpu().numpy()
+
+
+def rows_of(bt, sequences):
+    return [r for r, b, _ in OS.rows(bt.start, bt.lens) if b in sequences]
+
+
+@pytest.mark.parametrize("tokens,before", [([40], [90]), ([1, 2], [300, 70]), ([300, 1], [50, 700]), ([20], [5000]),
+                                           ([200], [3000])])
+@pytest.mark.parametrize("size", [400.0, 4000.0, 10000.0, 20000.0])
+def test_attention_huge_scores(tokens, before, size):
+    """Finite queries and keys whose scores pass 2^24, where 32 bits no longer
+    hold whole numbers: the largest score takes all, and equal keys share it.
+
+    A row is compared where the next lower score is further from the largest
+    than both can be off (136 x 2^-24 of the sum of magnitudes each) plus 50,
+    e^-50 being nothing beside one fp16 step.  Weights of equal scores are equal,
+    so a row's output is the mean of at most three values: two roundings of
+    2^-11 and sums of a few terms."""
+    say("huge scores", tokens, size)
+    rng = np.random.default_rng(int(size) + sum(tokens))
+    Hq, Hkv, ps = 4, 2, 16
+    bt = Batch(rng, tokens, before, ps, Hkv)
+    grow = lambda a: np.clip(a.astype(np.float32) * size, -65504, 65504).astype(np.float16)  # noqa: E731
+    bt.k = np.where(np.isnan(bt.k), bt.k, grow(np.nan_to_num(bt.k)))
+    at = lambda b, t: (bt.table[b, t // ps], slice(None), t % ps)  # noqa: E731
+    for b, n in enumerate(bt.lens):  # equal keys, near and far
+        for t, s in ((1, 0), (n // 2, 0), (n - 1 - tokens[b], 7)):
+            bt.k[at(b, t)] = bt.k[at(b, s)]
+    q = grow(f16(rng, (bt.T, Hq, 128)))
+    got = attend(q, bt).astype(np.float64)
+    assert np.isfinite(got[rows_of(bt, range(len(tokens)))]).all()
+    compared = 0
+    for r, b, pos in OS.rows(bt.start, bt.lens):
+        t = np.arange(pos + 1)
+        for h in range(Hq):
+            K, V = (c[bt.table[b, t // ps], h // 2, t % ps].astype(np.float64) for c in (bt.k, bt.v))
+            x = q[r, h].astype(np.float64)
+            s = K @ x / 128**0.5
+            reach = (np.abs(K) @ np.abs(x)).max() / 128**0.5
+            top = s >= s.max() - 1e-9 * reach  # the same products, whatever their order
+            rest = s[~top].max() if (~top).any() else -np.inf
+            if s.max() - rest < 2 * 136 * 2.0**-24 * reach + 50 or top.sum() > 3:
+                continue
+            compared += 1
+            want, weight = V[top].mean(0), np.abs(V[top]).mean(0)
+            assert (np.abs(got[r, h] - want) <= 2.0**-11 * np.abs(want) + (2.0**-11 + 2.0**-20) * weight + 2.0**-25).all()
+    assert compared > sum(tokens)
+
+
+@pytest.mark.parametrize("tokens,before", [([40], [90]), ([300, 1], [50, 700]), ([30], [4000]), ([1, 1], [60, 1500])])
+def test_attention_huge_scores_near_each_other(tokens, before):
+    """Scores from 2^20 to 2^37 of which a row sees some that lie a few steps of
+    32 bits apart, growing or in any order.  All values are 1, so that outputs
+    are 1 whatever the weights: each probability's rounding is 2^-11 of it, the
+    output's 2^-11, and sums over L positions 2 L x 2^-24."""
+    say("huge scores near each other", tokens)
+    rng = np.random.default_rng(sum(tokens) + sum(before))
+    bt = Batch(rng, tokens, before, 16, 1)
+    L = int(bt.lens.max())
+    bt.v = np.where(np.isnan(bt.v), bt.v, np.float16(1))
+    for e in range(20, 38):
+        for order in ("growing", "any"):
+            a = np.float16(2.0**((e - 6) / 2))  # 64 products of a x a: about 2^e
+            q = np.zeros((bt.T, 2, 128), dtype=np.float16)
+            q[..., :64], q[:, 0, 64], q[:, 1, 65] = a, 2.0**max(e - 24, 0), 2.0**max(e - 24, 0)
+            k = np.zeros((bt.P, 1, 16, 128), dtype=np.float16)
+            k[..., :64] = a
+            for b, n in enumerate(bt.lens):
+                steps = rng.integers(-64, 64, (n, 2)).astype(np.float16)
+                if order == "growing":
+                    steps.sort(axis=0)
+                for t in range(n):
+                    k[bt.table[b, t // 16], 0, t % 16, 64:66] = steps[t]
+            k[~np.broadcast_to(bt.used[:, None], k.shape[:3])] = np.nan
+            out = laq.paged_attention(dev(q), bt.cache(k), *bt.device()[1:])
+            torch.cuda.synchronize()
+            got = out.cpu().numpy()[rows_of(bt, range(len(tokens)))].astype(np.float64)
+            assert (np.abs(got - 1) <= 2.0**-11 + 2.0**-11 + 2 * L * 2.0**-24).all(), (e, order, got.min(), got.max())
