@@ -599,9 +599,11 @@ int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, in
  * is there; zeros when there are none.  q and out fp16 [T][Hq][128].
  * Whatever positions that a row does not see hold (infinities and NaN too)
  * does not change that row.
- * Probabilities of batches with more than 16 / (Hq / Hkv) rows a sequence on
- * average are rounded to fp16 (half a step, 2^-11 of each) before they weigh
- * the values; sums and denominators are fp32.
+ * A sequence with at most 16 / (Hq / Hkv) rows keeps its probabilities in fp32
+ * whatever else the batch holds; those of longer chunks are rounded to fp16
+ * (half a step, 2^-11 of each) before they weigh the values where T / B is
+ * above that number (rows of no sequence and waiting sequences count: sizes
+ * choose the kernel).  Sums and denominators are fp32.
  * One or two kernels: items of at most 256 query rows and a range of
  * positions, and where a sequence's positions are split, the joining of its
  * ranges in position order.  The split follows the lengths on the device.

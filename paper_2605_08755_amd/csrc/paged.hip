@@ -400,14 +400,14 @@ struct Out {
 // half l & 1 of step l >> 1) and become scalar buffer descriptors.
 constexpr int kWaves = 4;
 constexpr int kStep = 32;
-constexpr int kStride = kWaves * kStep;
 constexpr int kRowBytes = (kStep + 4) * 4;         // a row of probabilities (4 words of padding)
 constexpr int kKeyBytes = kStep * kHeadDim * 2;    // a step's keys
 // Keys and values pass once: loads that do not keep their lines (measured on
 // MI355X, three sequences of 131072, 77777 and 901 positions, 64:8 heads: 167 ->
 // 151 us; 16 sequences of up to 8192, 32:8: 44 -> 39).
 constexpr int kStreamed = 2;
-constexpr int kSmallLds = kWaves * (2 * kKeyBytes + 16 * kRowBytes);
+template <int WAVES>
+constexpr int kSmallLds = WAVES * (2 * kKeyBytes + 16 * kRowBytes);
 
 __device__ __forceinline__ void lds_read4(u32x4 (&f)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
   asm volatile(
@@ -424,18 +424,15 @@ __device__ __forceinline__ void lds_put(uint32_t addr, float v) {
   asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory");
 }
 
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(PagedBatch pb,
-                                                                             const uint16_t* __restrict__ q, int R,
-                                                                             int Hkv, int window, Out o_) {
+// An item of up to 16 rows, by a block of WAVES waves; REC: rows that a record has room for.
+template <int WAVES, int REC>
+__device__ __forceinline__ void rows16_item(const PagedBatch& pb, const uint16_t* __restrict__ q, int R, int window,
+                                            const Out& o_, const Item& it, int g, char* lds) {
   typedef __attribute__((address_space(3))) void lds_void;
-  extern __shared__ u32x4 small_lds[];
-  char* const lds = reinterpret_cast<char*>(small_lds);
+  constexpr int kStride = WAVES * kStep;
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int n = lane & 15, j = lane >> 4;
-  const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kSmallRows, false>(pb, at_item, R, Hkv, window, lane);
-  if (!it.found) return;
   const int rows = min(it.n * R - it.tile * kSmallRows, kSmallRows);
   const int r0 = it.tile * kSmallRows;
   const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
@@ -459,7 +456,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
   }
 
   char* const keys = lds + w * 2 * kKeyBytes;
-  const uint32_t probs = lds_byte(lds + kWaves * 2 * kKeyBytes + w * 16 * kRowBytes);
+  const uint32_t probs = lds_byte(lds + WAVES * 2 * kKeyBytes + w * 16 * kRowBytes);
   const int p_first = sp.lo + w * kStep;
   const int* const table = pb.page_table + it.b * pb.table_stride;
   const uint16_t* const khead = pb.k + g * pb.head_stride;
@@ -624,8 +621,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
   // The waves' results, in wave order: 128 value sums per (wave, row) over the
   // keys' place, maxima and denominators over the probabilities'.
   __syncthreads();
-  float* const osum = reinterpret_cast<float*>(lds);                              // [4][16][128]
-  float* const stat = reinterpret_cast<float*>(lds + kWaves * 2 * kKeyBytes);     // [4][16][2]
+  float* const osum = reinterpret_cast<float*>(lds);                              // [WAVES][16][128]
+  float* const stat = reinterpret_cast<float*>(lds + WAVES * 2 * kKeyBytes);     // [WAVES][16][2]
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     const int h = 4 * j + r;
@@ -641,15 +638,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
   __syncthreads();
   const int rec = it.rec + it.split;
   if (it.splits > 1 && rec >= o_.rec_bound) return;  // token_start out of order
-  float* const wp = o_.ws + ((int64_t)g * o_.rec_bound + rec) * (kSmallRows * (kHeadDim + 2));
-  for (int idx = threadIdx.x; idx < rows * kHeadDim; idx += 64 * kWaves) {
+  float* const wp = o_.ws + ((int64_t)g * o_.rec_bound + rec) * (REC * (kHeadDim + 2));
+  for (int idx = threadIdx.x; idx < rows * kHeadDim; idx += 64 * WAVES) {
     const int h = idx / kHeadDim, d = idx % kHeadDim;
     float M = kNoMax;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, stat[(i * 16 + h) * 2]);
+    for (int i = 0; i < WAVES; ++i) M = fmaxf(M, stat[(i * 16 + h) * 2]);
     float den = 0.0f, num = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
       const float e = __builtin_amdgcn_exp2f(stat[(i * 16 + h) * 2] - M);
       den = fmaf(e, stat[(i * 16 + h) * 2 + 1], den);
       num = fmaf(e, osum[(i * 16 + h) * kHeadDim + d], num);
@@ -657,8 +654,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
     if (it.splits > 1) {
       wp[idx] = num;
       if (d == 0) {
-        wp[kSmallRows * kHeadDim + 2 * h] = M;
-        wp[kSmallRows * kHeadDim + 2 * h + 1] = den;
+        wp[REC * kHeadDim + 2 * h] = M;
+        wp[REC * kHeadDim + 2 * h + 1] = den;
       }
     } else {
       const int r = r0 + h;
@@ -666,6 +663,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
       o_.out[((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + d] = __builtin_bit_cast(uint16_t, y);
     }
   }
+}
+
+__global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(PagedBatch pb,
+                                                                             const uint16_t* __restrict__ q, int R,
+                                                                             int Hkv, int window, Out o_) {
+  extern __shared__ u32x4 small_lds[];
+  const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
+  const Item it = find_item<kSmallRows, false>(pb, at_item, R, Hkv, window, threadIdx.x & 63);
+  if (!it.found) return;
+  rows16_item<kWaves, kSmallRows>(pb, q, R, window, o_, it, g, reinterpret_cast<char*>(small_lds));
 }
 
 // ---------------------------------------------------------------------------
@@ -686,6 +693,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // than 2^7: so they stay below 2^15 and full precision reaches down to 2^-22
 // of the largest, and the value sums are rarely rescaled.  The denominator is
 // the fp32 sum of the unrounded ones.
+// A sequence of up to 16 rows (decoding rows beside a chunk, or of a batch with
+// much padding) would fill half a wave's rows: the block takes its items as the
+// 16-row kernel does, with probabilities in 32 bits and eight waves along the
+// positions.  Its records have the place of 256 rows.  (Measured on MI355X: a
+// chunk beside 15 decoding rows 77.8 -> 78.2 us; two waves more for the
+// probabilities' remainders instead, 84.8.)
 //
 // What bounds it: LDS bandwidth.  A wave's 32 rows need a tile's keys and
 // values from LDS whole, 32 KiB a wave and tile, and the staging writes 32 KiB
@@ -707,7 +720,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 constexpr int kTile = 64;
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kLargeThreads = 512;
-constexpr int kLargeLds = 4 * kTileBytes + 64;
+constexpr int kLargeLds = std::max(4 * kTileBytes + 64, kSmallLds<kLargeThreads / 64>);
 constexpr float kProbLog2 = 8.0f, kLagLog2 = 7.0f;
 constexpr float kFarLog2 = 65536.0f;
 
@@ -725,6 +738,10 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
   const Item it = find_item<kLargeRows, false>(pb, at_item, R, Hkv, window, lane);
   if (!it.found) return;
+  if (it.n * R <= kSmallRows) {
+    rows16_item<kLargeThreads / 64, kLargeRows>(pb, q, R, window, o_, it, g, lds);
+    return;
+  }
   const int r0 = it.tile * kLargeRows;
   const int rows = min(it.n * R - r0, kLargeRows);
   const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
@@ -1221,7 +1238,7 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
       launch((paged_attention_join_kernel<kLargeRows, 1>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv,
              (int)window, o);
   } else {
-    launch(paged_attention_rows16_kernel, grid, dim3(64 * kWaves), kSmallLds, stream, e1, pb, q, (int)R, (int)Hkv,
+    launch(paged_attention_rows16_kernel, grid, dim3(64 * kWaves), kSmallLds<kWaves>, stream, e1, pb, q, (int)R, (int)Hkv,
            (int)window, o);
     if (p.split_tiles > 0)
       launch((paged_attention_join_kernel<kSmallRows, 4>), join, dim3(256), 0, stream, e2, pb, (int)R, (int)Hkv, (int)window,

@@ -22,6 +22,48 @@ def rows_of(bt, sequences):
     return [r for r, b, _ in OS.rows(bt.start, bt.lens) if b in sequences]
 
 
+@pytest.mark.parametrize("tokens,before,Hq,Hkv,kw", [
+    ([40, 1], [900, 50], 1, 1, {}),
+    ([1, 1, 150, 1, 2], [33, 60, 20, 47, 40], 8, 2, {}),   # decoding rows beside a chunk
+    ([70, 1, 1], [0, 47, 61], 5, 1, {}),
+    ([1, 1], [50, 61], 8, 2, {"pad": 60}),                 # decoding rows of a batch with padding
+    ([1], [53], 4, 1, {"pad": 30, "first": 9}),
+    ([4], [44], 4, 1, {"pad": 1}),                         # 16 query rows
+    ([100, 1, 4], [300, 700, 640], 4, 1, {}),              # split over ranges of positions
+])
+def test_attention_of_few_rows_keeps_32_bits(tokens, before, Hq, Hkv, kw):
+    """Sequences of up to 16 query rows a key/value head, whatever stands
+    beside them: the probabilities are not rounded to 16 bits.
+
+    Scores are small sums of four products and values are +1 and -1, as many of
+    the one as of the other, so that outputs are near 0 and their own fp16
+    rounding is small.  The bound, relative to the weights' sum of |v| = 1:
+    scores are fp32 sums (their errors as in tests/test_gpu_serving.py, 136 x
+    2^-24 of the sum of magnitudes, in a weight and in the denominator), L x
+    2^-24 in the value sums and in the denominator, and the rounding of the
+    output, 2^-11 of it.  A rounding of each probability to 16 bits would be
+    2^-11 of it."""
+    say("few rows", tokens, Hq, kw)
+    rng = np.random.default_rng(sum(tokens) + sum(before) + Hq)
+    bt = Batch(rng, tokens, before, 16, Hkv, **kw)
+    for b, n in enumerate(bt.lens):
+        for g in range(Hkv):
+            signs = np.array([rng.permutation(np.resize([1.0, -1.0], n)) for _ in range(128)])
+            for t in range(n):
+                bt.v[bt.table[b, t // 16], g, t % 16] = signs[:, t]
+    q = np.zeros((bt.T, Hq, 128), dtype=np.float16)
+    q[..., 5::32] = f16(rng, (bt.T, Hq, 4), 0.5)
+    got = attend(q, bt).astype(np.float64)
+    ref, weight, reach = OS.paged_attention(q, bt.k, bt.v, bt.table, bt.start, bt.lens, 0, np.zeros_like(got))
+    mine = rows_of(bt, [b for b, n in enumerate(tokens) if n * (Hq // Hkv) <= 16])
+    assert len(mine) >= 1 and np.allclose(weight[mine], 1)
+    seen = {r: pos + 1 for r, _, pos in OS.rows(bt.start, bt.lens)}
+    L = np.array([seen[r] for r in mine])[:, None, None]
+    tol = 2.0**-11 * np.abs(ref[mine]) + 2 * 136 * 2.0**-24 * reach[mine][..., None] + 2 * L * 2.0**-24 + 2.0**-25
+    err = np.abs(got[mine] - ref[mine])
+    assert (err <= tol).all(), float((err / tol).max())
+
+
 @pytest.mark.parametrize("tokens,before", [([40], [90]), ([1, 2], [300, 70]), ([300, 1], [50, 700]), ([20], [5000]),
                                            ([200], [3000])])
 @pytest.mark.parametrize("size", [400.0, 4000.0, 10000.0, 20000.0])
