@@ -578,7 +578,7 @@ typedef struct laq_paged_batch {
  * nothing.  Two rows of a call must not name the same place in the pages.
  * B == 0 or T == 0: nothing is done.
  * Errors: NULL_POINTER; BAD_SHAPE (sizes above, head_dim != 128, Hq not a
- * multiple of Hkv, Hq > 4096, bad eps); MISALIGNED (fp16 arrays 16-byte,
+ * multiple of Hkv, Hq > 4096, bad eps, T > 2^26 - 4); MISALIGNED (fp16 arrays 16-byte,
  * cos_sin and the batch's arrays 4-byte, strides). */
 laq_status laq_paged_append_f16(const laq_paged_batch *batch, const void *qkv, int64_t qkv_stride,
                                 const void *q_norm_weight, const void *k_norm_weight, const float *cos_sin,
@@ -613,8 +613,8 @@ int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, in
  *              Calls in flight need separate workspaces.
  * B == 0 or T == 0: nothing is done.
  * Errors: NULL_POINTER; BAD_SHAPE (sizes above, head_dim != 128, Hq not a
- * multiple of Hkv, Hq > 4096, window outside 0..2^30, workspace too small);
- * MISALIGNED. */
+ * multiple of Hkv, Hq > 4096, window outside 0..2^30, workspace too small,
+ * rows that would take 2^32 threads and more); MISALIGNED. */
 laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, int64_t Hq, int64_t Hkv,
                                    int64_t head_dim, int64_t window, void *out, void *workspace,
                                    int64_t workspace_bytes, void *stream);

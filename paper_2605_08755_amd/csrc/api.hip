@@ -556,7 +556,7 @@ laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int
   if (head_dim != kHeadDimAbi) return fail(LAQ_ERR_BAD_SHAPE, fn, "head_dim must be 128");
   if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096)
     return fail(LAQ_ERR_BAD_SHAPE, fn, "Hq must be a positive multiple of Hkv, at most 4096");
-  // (a wave per row: 2^26 rows would be 2^32 threads, more than one launch may have)
+  // (the threads of a launch, 2^32 - 1 at most, are checked by the calls themselves)
   if (b->B < 0 || b->B > (1 << 20) || b->T < 0 || b->T >= (1LL << 26) || b->T * Hq > (1LL << 30))
     return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= B <= 2^20, 0 <= T < 2^26 and T * Hq <= 2^30");
   if (b->page_size < 16 || b->page_size > (1 << 20) || (b->page_size & (b->page_size - 1)) != 0)
@@ -623,6 +623,8 @@ laq_status laq_paged_append_f16(const laq_paged_batch* batch, const void* qkv, i
   if (batch->B == 0 || batch->T == 0) return ok();
   if (!qkv || !cos_sin || !q_out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
   if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
+  if (laq::paged_append_threads(batch->T, Hq, Hkv) > 0xFFFFFFFFLL)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
   if (!aligned(qkv, 16) || !aligned(q_norm_weight, 16) || !aligned(k_norm_weight, 16) || !aligned(cos_sin, 4) ||
       !aligned(q_out, 16))
     return fail(LAQ_ERR_MISALIGNED, fn, "cos_sin must be 4-byte, fp16 arrays 16-byte aligned");

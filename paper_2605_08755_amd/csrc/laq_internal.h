@@ -261,6 +261,8 @@ struct PagedBatch {
   uint32_t page_bytes;  // between pages
   int slot_stride, page_shift, num_pages, table_pages, B, T;
 };
+// Threads of the append's launch.
+int64_t paged_append_threads(int64_t T, int64_t Hq, int64_t Hkv);
 hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
                                const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv,
                                float eps, uint16_t* q_out, hipStream_t stream, const LaunchEvents& ev);

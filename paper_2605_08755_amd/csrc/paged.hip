@@ -1191,14 +1191,23 @@ AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64
 
 }  // namespace
 
+namespace {
+// Waves of a row of the append: one where rows alone fill the chip, else one per group of eight heads.
+int64_t append_waves(int64_t T, int64_t Hq, int64_t Hkv) {
+  return std::max<int64_t>(1, std::min<int64_t>((Hq + 2 * Hkv + 7) / 8, kResidentWaves / T));
+}
+}  // namespace
+
+int64_t paged_append_threads(int64_t T, int64_t Hq, int64_t Hkv) {
+  return (T * append_waves(T, Hq, Hkv) + 3) / 4 * 256;
+}
+
 hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
                                const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv,
                                float eps, uint16_t* q_out, hipStream_t stream, const LaunchEvents& ev) {
-  // A wave per row where rows alone fill the chip, else a wave per group of eight heads.
-  const int64_t groups = (Hq + 2 * Hkv + 7) / 8;
-  const int64_t per = std::max<int64_t>(1, std::min<int64_t>(groups, kResidentWaves / pb.T));
-  launch(paged_append_kernel, dim3((unsigned)((pb.T * per + 3) / 4)), dim3(256), 0, stream, ev, pb, qkv, qkv_stride, qw,
-         kw, cos_sin, (int)std::min<int64_t>(rope_rows, 0x7FFFFFFF), (int)Hq, (int)Hkv, eps, q_out, (int)per);
+  launch(paged_append_kernel, dim3((unsigned)(paged_append_threads(pb.T, Hq, Hkv) / 256)), dim3(256), 0, stream, ev, pb,
+         qkv, qkv_stride, qw, kw, cos_sin, (int)std::min<int64_t>(rope_rows, 0x7FFFFFFF), (int)Hq, (int)Hkv, eps, q_out,
+         (int)append_waves(pb.T, Hq, Hkv));
   return hipGetLastError();
 }
 
