@@ -107,8 +107,9 @@ __device__ __forceinline__ int wave_sum(int v) {
 // in and out (measured on MI355X, 16384 rows, 32:8 heads: 82 us, 4.9 TB/s,
 // a large copy moves 5.0); few rows are a launch and three dependent reads
 // (16 rows: 3.6 us).  The row's table line is read once per wave.
-// The row's sequence is found by counting the sequences that end at or before
-// it, 64 per step, while the row's first loads are in flight.
+// The row's sequence is found while its first loads are in flight: among the
+// sequences' ends, which do not decrease, by 64 of them a step (up to 64
+// sequences one step, 2^20 four).
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const uint16_t* __restrict__ qkv,
                                                            int64_t qkv_stride, const uint16_t* __restrict__ qw,
                                                            const uint16_t* __restrict__ kw,
@@ -134,10 +135,13 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedBatch pb, const 
   u32x4 a, b;
   load(first, a, b);
 
-  int seq = 0;
-  for (int b0 = 0; b0 < pb.B; b0 += 64) {
-    const bool before = b0 + lane < pb.B && pb.token_start[b0 + lane + 1] <= row;
-    seq += __popcll(__ballot(before));
+  int seq = 0;  // sequences that end at or before the row
+  for (int left = pb.B; left > 0;) {
+    const int step = (left + 63) >> 6, last = (lane + 1) * step - 1;  // a lane's step sequences end with the last's end
+    const bool before = last < left && pb.token_start[seq + last + 1] <= row;
+    const int whole = __popcll(__ballot(before)) * step;
+    seq += whole;
+    left = min(step - 1, left - whole);
   }
   seq = uniform(seq);
   if (seq >= pb.B) return;  // behind the last sequence

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from oracle import serving as OS
-from paper_2605_08755_amd import laq
+from oracle.compare import linear_check
+from paper_2605_08755_amd import decode, laq
 from test_gpu_serving import Batch, dev, f16, say
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +137,78 @@ def test_attention_huge_scores_near_each_other(tokens, before):
             torch.cuda.synchronize()
             got = out.cpu().numpy()[rows_of(bt, range(len(tokens)))].astype(np.float64)
             assert (np.abs(got - 1) <= 2.0**-11 + 2.0**-11 + 2 * L * 2.0**-24).all(), (e, order, got.min(), got.max())
+
+
+# ---------------------------------------------------------------------------
+# many sequences
+# ---------------------------------------------------------------------------
+def many(rng, B, T, Hq, Hkv, ps=16):
+    """T rows spread over B sequences (most waiting where T < B), pages of one
+    row's sequences only: (table, start, lens) and arrays of the caches."""
+    owner = np.sort(rng.integers(0, B, T))
+    start = np.concatenate([[0], np.cumsum(np.bincount(owner, minlength=B))]).astype(np.int32)
+    tokens = np.diff(start)
+    lens = (tokens + rng.integers(0, 3 * ps - tokens.max(), B)).astype(np.int32)
+    width = 3
+    pages = np.where(tokens > 0, -(-lens // ps), 0)
+    table = np.full((B, width), -1, dtype=np.int32)
+    order = rng.permutation(int(pages.sum())).astype(np.int32)
+    column = np.arange(width) < pages[:, None]
+    table[column] = order
+    k, v = (f16(rng, (len(order), Hkv, ps, 128)) for _ in range(2))
+    return table, start, lens, k, v
+
+
+@pytest.mark.parametrize("B,T", [(63, 40), (64, 200), (65, 65), (129, 500), (4095, 1000), (4097, 3000), (70000, 900),
+                                 (1 << 20, 300)])
+def test_append_many_sequences(B, T):
+    """Rows of sequences anywhere among many, most of which wait."""
+    say("append many", B, T)
+    rng = np.random.default_rng(B + T)
+    Hq, Hkv = 2, 1
+    table, start, lens, k, v = many(rng, B, T, Hq, Hkv)
+    qkv = f16(rng, (T, (Hq + 2 * Hkv) * 128))
+    cs = decode.rope_table(64, 1e6, DEV)
+    kd, vd = dev(k), dev(v)
+    q = laq.paged_append(dev(qkv), None, None, cs, kd, vd, dev(table), dev(start), dev(lens), Hq, 1e-6)
+    torch.cuda.synchronize()
+    ref = OS.paged_append(qkv, None, None, cs.cpu().numpy(), k, v, table, start, lens, Hq, 1e-6, np.zeros((T, Hq, 128)))
+    for a, b in zip((q, kd, vd), ref):
+        r = linear_check(a.cpu().numpy(), b)
+        assert r["ok"], r
+
+
+def best_time(f, calls=3):
+    """Shortest of some calls, in ms."""
+    times = []
+    for _ in range(calls + 1):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b))
+    return min(times[1:])
+
+
+def decoding(B, Hq=2, Hkv=1):
+    """B decoding sequences of 16 positions."""
+    return (torch.zeros((B, Hkv, 16, 128), dtype=torch.float16, device=DEV),
+            torch.zeros((B, Hkv, 16, 128), dtype=torch.float16, device=DEV),
+            torch.arange(B, dtype=torch.int32, device=DEV)[:, None], torch.arange(B + 1, dtype=torch.int32, device=DEV),
+            torch.full((B,), 16, dtype=torch.int32, device=DEV))
+
+
+def test_append_time_grows_with_the_rows():
+    """16 times the sequences take 16 times as long at most, as their bytes do,
+    with as much again for the timing: each row's search of its sequence does
+    not grow with their number (it took 256 times as long then)."""
+    say("append time")
+    times = []
+    for B in (8192, 131072):
+        k, v, table, start, lens = decoding(B)
+        qkv = torch.zeros((B, 4 * 128), dtype=torch.float16, device=DEV)
+        q = torch.zeros((B, 2, 128), dtype=torch.float16, device=DEV)
+        cs = decode.rope_table(16, 1e6, DEV)
+        times.append(best_time(lambda: laq.paged_append(qkv, None, None, cs, k, v, table, start, lens, 2, 1e-6, q_out=q)))
+    assert times[1] < 32 * times[0], times
