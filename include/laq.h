@@ -604,9 +604,10 @@ int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, in
  * (half a step, 2^-11 of each) before they weigh the values where T / B is
  * above that number (rows of no sequence and waiting sequences count: sizes
  * choose the kernel).  Sums and denominators are fp32.
- * One or two kernels: items of at most 256 query rows and a range of
- * positions, and where a sequence's positions are split, the joining of its
- * ranges in position order.  The split follows the lengths on the device.
+ * One to three kernels: from 65 sequences a plan of the batch, then items of
+ * at most 256 query rows and a range of positions, and where a sequence's
+ * positions can be split, the joining of its ranges in position order.  The
+ * split follows the lengths on the device.
  *   workspace  [scratch] device memory, 16-byte aligned, any contents, at
  *              least laq_paged_attention_workspace_bytes(B, T, Hq, Hkv,
  *              table_pages * page_size) bytes; may be NULL when that is 0.

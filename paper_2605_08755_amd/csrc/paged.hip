@@ -268,24 +268,94 @@ struct Item {
   int rec;  // first record of the tile's ranges
 };
 
+// The smallest chunk by that bound, of all sequences' tiles x units.
+template <int BM>
+__device__ __forceinline__ int least_chunk(double total, int Hkv) {
+  const double share = total * Hkv * (1.0 / kItems);
+  return uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
+}
+
+// Batches of more than 64 sequences have a plan in the workspace, which a kernel
+// of one block makes first, so that a block's search does not pass over all of
+// them, whose time grew with their square.  Whole numbers: the chunk; then per
+// group of 64 sequences the items before it, then likewise the records, then the
+// split tiles.  (Measured on MI355X, decoding sequences of 128 and of 1024
+// positions, 32:8 heads, each block passing over all -> the plan: 65, 14.4 -> 17.6
+// and 81 -> 76 us; 256, 46 -> 40 and 206 -> 182; 4096, 3.6 -> 0.55 and 5.9 -> 2.7 ms.)
+constexpr int kGroup = 64;
+__host__ __device__ constexpr int64_t plan_groups(int64_t B) { return B > kGroup ? (B + kGroup - 1) / kGroup : 0; }
+
+constexpr int kPlanWaves = 16;
+template <int BM>
+__global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(PagedBatch pb, int R, int Hkv,
+                                                                               int window, int* __restrict__ plan) {
+  __shared__ double totals[kPlanWaves];
+  __shared__ int sums[kPlanWaves][3];
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+  const int groups = (int)plan_groups(pb.B);
+  double total = 0.0;
+  for (int g = w; g < groups; g += kPlanWaves) {
+    const Seq q = load_seq<BM>(pb, g * kGroup + lane, R, window);
+    total += wave_sum_exact((double)q.tiles * q.units);
+  }
+  if (lane == 0) totals[w] = total;
+  __syncthreads();
+  total = 0.0;
+  for (int i = 0; i < kPlanWaves; ++i) total += totals[i];
+  const int chunk = least_chunk<BM>(total, Hkv);
+  if (threadIdx.x == 0) plan[0] = chunk;
+  int* const before = plan + 1;
+  int upto[3] = {0, 0, 0};
+  for (int g0 = 0; g0 < groups; g0 += kPlanWaves) {
+    const int g = g0 + w;
+    const Seq q = load_seq<BM>(pb, min(g, groups) * kGroup + lane, R, window);  // (none past the last group)
+    const int splits = (q.units + chunk - 1) / chunk;
+    const int items = wave_sum(q.tiles * splits), split = wave_sum(splits > 1 ? q.tiles : 0),
+              recs = wave_sum(splits > 1 ? q.tiles * splits : 0);
+    if (lane == 0) sums[w][0] = items, sums[w][1] = recs, sums[w][2] = split;
+    __syncthreads();
+    for (int i = 0; i < 3; ++i) {
+      int at = upto[i];
+      for (int k = 0; k < w; ++k) at += sums[k][i];
+      if (lane == 0 && g < groups) before[i * groups + g] = at;
+      for (int k = 0; k < kPlanWaves; ++k) upto[i] += sums[k][i];
+    }
+    __syncthreads();
+  }
+}
+
 // Item `idx` of a key/value head (SPLIT: the idx-th split tile).
 template <int BM, bool SPLIT>
-__device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, int Hkv, int window, int lane) {
-  double total = 0.0;
-  Seq q = load_seq<BM>(pb, lane, R, window);
-  total = wave_sum_exact((double)q.tiles * q.units);
-  for (int b0 = 64; b0 < pb.B; b0 += 64) {
-    const Seq x = load_seq<BM>(pb, b0 + lane, R, window);
-    total += wave_sum_exact((double)x.tiles * x.units);
-  }
+__device__ __forceinline__ Item find_item(const PagedBatch& pb, const int* __restrict__ plan, int idx, int R, int Hkv,
+                                          int window, int lane) {
   Item it;
   it.found = false;
-  // The smallest chunk by that bound, then up to a third larger until the items
-  // are no more than the blocks that run at once (a few more would run alone).
-  const double share = total * Hkv * (1.0 / kItems);
-  const int least = uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
-  it.chunk = least;
-  if (pb.B <= 64) {
+  int items = 0, recs = 0, b0 = 0;
+  Seq q;
+  if (pb.B > kGroup) {
+    // the last group with no more items before it than idx, 64 groups a step
+    const int groups = (int)plan_groups(pb.B);
+    const int* const before = plan + 1;
+    const int* const first = before + (SPLIT ? 2 * groups : 0);
+    int g = 0;
+    for (int left = groups; left > 1;) {
+      const int step = (left + 63) >> 6, at = lane * step;
+      const int n = max(__popcll(__ballot(at < left && first[g + min(at, left - 1)] <= idx)), 1) - 1;
+      g += n * step;
+      left = min(step, left - n * step);
+    }
+    g = uniform(g);
+    b0 = g * kGroup;
+    it.chunk = uniform(plan[0]);
+    items = uniform(first[g]);
+    recs = uniform(before[groups + g]);
+    q = load_seq<BM>(pb, b0 + lane, R, window);
+  } else {
+    q = load_seq<BM>(pb, lane, R, window);
+    // That chunk, then up to 3/8 and one unit larger until the items are no more
+    // than the blocks that run at once (a few more would run alone).
+    const int least = least_chunk<BM>(wave_sum_exact((double)q.tiles * q.units), Hkv);
+    it.chunk = least;
     for (int i = 0; i < 4; ++i) {
       const int c = least + least * i / 8 + (i > 0);
       if (wave_sum(q.tiles * ((q.units + c - 1) / c)) * Hkv <= kItems) {
@@ -295,37 +365,29 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, int idx, int R, 
     }
     it.chunk = uniform(it.chunk);
   }
-  int items = 0, recs = 0;
-  for (int b0 = 0; b0 < pb.B; b0 += 64) {
-    if (b0 > 0) q = load_seq<BM>(pb, b0 + lane, R, window);
-    const int splits = (q.units + it.chunk - 1) / it.chunk;
-    const int rec = splits > 1 ? q.tiles * splits : 0;
-    const int own = SPLIT ? (splits > 1 ? q.tiles : 0) : q.tiles * splits;
-    const int upto = items + wave_scan(own, lane);
-    const int rupto = recs + wave_scan(rec, lane);
-    const uint64_t past = __ballot(upto > idx);
-    if (past) {
-      const int l = __ffsll((unsigned long long)past) - 1;
-      it.found = true;
-      it.b = b0 + l;
-      it.s0 = readlane(q.s0, l);
-      it.n = readlane(q.n, l);
-      it.pos0 = readlane(q.pos0, l);
-      it.end = readlane(q.end, l);
-      it.lo = readlane(q.lo, l);
-      it.splits = readlane(splits, l);
-      const int i = idx - readlane(upto - own, l);
-      // the last tiles of a prompt see the most positions: they go first
-      // (divisions of uniform values are vector instructions: their results are made uniform again)
-      const int back = SPLIT ? i : uniform(i / it.splits);
-      it.tile = readlane(q.tiles, l) - 1 - back;
-      it.split = SPLIT ? 0 : i - back * it.splits;
-      it.rec = readlane(rupto - rec, l) + it.tile * it.splits;
-      return it;
-    }
-    items = readlane(upto, 63);
-    recs = readlane(rupto, 63);
-  }
+  const int splits = (q.units + it.chunk - 1) / it.chunk;
+  const int rec = splits > 1 ? q.tiles * splits : 0;
+  const int own = SPLIT ? (splits > 1 ? q.tiles : 0) : q.tiles * splits;
+  const int upto = items + wave_scan(own, lane);
+  const int rupto = recs + wave_scan(rec, lane);
+  const uint64_t past = __ballot(upto > idx);
+  if (!past) return it;
+  const int l = __ffsll((unsigned long long)past) - 1;
+  it.found = true;
+  it.b = b0 + l;
+  it.s0 = readlane(q.s0, l);
+  it.n = readlane(q.n, l);
+  it.pos0 = readlane(q.pos0, l);
+  it.end = readlane(q.end, l);
+  it.lo = readlane(q.lo, l);
+  it.splits = readlane(splits, l);
+  const int i = idx - readlane(upto - own, l);
+  // the last tiles of a prompt see the most positions: they go first
+  // (divisions of uniform values are vector instructions: their results are made uniform again)
+  const int back = SPLIT ? i : uniform(i / it.splits);
+  it.tile = readlane(q.tiles, l) - 1 - back;
+  it.split = SPLIT ? 0 : i - back * it.splits;
+  it.rec = readlane(rupto - rec, l) + it.tile * it.splits;
   return it;
 }
 
@@ -378,10 +440,11 @@ __device__ __forceinline__ uint32_t not_finite(u32x4 x) {
   return not_finite(x.x) | not_finite(x.y) | not_finite(x.z) | not_finite(x.w);
 }
 
-// Results of one item: rows of partial sums (split) or of outputs.
+// Results of one item: rows of partial sums (split) or of outputs.  And the plan.
 struct Out {
   uint16_t* out;
   float* ws;
+  const int* plan;
   int Hq, rec_bound;
 };
 
@@ -674,7 +737,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
                                                                              int Hkv, int window, Out o_) {
   extern __shared__ u32x4 small_lds[];
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kSmallRows, false>(pb, at_item, R, Hkv, window, threadIdx.x & 63);
+  const Item it = find_item<kSmallRows, false>(pb, o_.plan, at_item, R, Hkv, window, threadIdx.x & 63);
   if (!it.found) return;
   rows16_item<kWaves, kSmallRows>(pb, q, R, window, o_, it, g, reinterpret_cast<char*>(small_lds));
 }
@@ -740,7 +803,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   const int w = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kLargeRows, false>(pb, at_item, R, Hkv, window, lane);
+  const Item it = find_item<kLargeRows, false>(pb, o_.plan, at_item, R, Hkv, window, lane);
   if (!it.found) return;
   if (it.n * R <= kSmallRows) {
     rows16_item<kLargeThreads / 64, kLargeRows>(pb, q, R, window, o_, it, g, lds);
@@ -1081,7 +1144,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<BM, true>(pb, at_item, R, Hkv, window, lane);
+  const Item it = find_item<BM, true>(pb, o_.plan, at_item, R, Hkv, window, lane);
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
@@ -1165,7 +1228,8 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
 struct AttentionPlan {
   bool large;
   int64_t items, split_tiles, records;  // per key/value head
-  int64_t floats;                       // workspace
+  int64_t floats;                       // workspace: the records, then the plan
+  int64_t plan_at;
 };
 
 template <int BM>
@@ -1180,7 +1244,8 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
   p.records = split ? std::min(2 * kItems / Hkv, tiles * most) : 0;
-  p.floats = p.records * Hkv * BM * (kHeadDim + 2);
+  p.plan_at = p.records * Hkv * BM * (kHeadDim + 2);
+  p.floats = p.plan_at + (B > kGroup ? 1 + 3 * plan_groups(B) : 0);
   return p;
 }
 
@@ -1228,12 +1293,19 @@ hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64
                                   uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev) {
   const int64_t R = Hq / Hkv;
   const AttentionPlan p = attention_plan(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift);
-  LaunchEvents e1 = ev, e2;
-  if (p.split_tiles > 0) {  // the measurement hook spans both kernels
+  LaunchEvents e0, e1 = ev, e2;
+  if (p.split_tiles > 0) {  // the measurement hook spans all kernels
     e1.stop = nullptr;
     e2.stop = ev.stop;
   }
-  const Out o{out, ws, (int)Hq, (int)p.records};
+  int* const plan = reinterpret_cast<int*>(ws + p.plan_at);
+  if (pb.B > kGroup) {
+    e0.start = e1.start;
+    e1.start = nullptr;
+    auto* const kernel = p.large ? paged_attention_plan_kernel<kLargeRows> : paged_attention_plan_kernel<kSmallRows>;
+    launch(kernel, dim3(1), dim3(64 * kPlanWaves), 0, stream, e0, pb, (int)R, (int)Hkv, (int)window, plan);
+  }
+  const Out o{out, ws, plan, (int)Hq, (int)p.records};
   const dim3 grid((unsigned)(p.items * Hkv));
   // A block joins one row; 16 rows where the tiles (most of them not split) would make many blocks.
   constexpr int64_t kFewTiles = 32, kJoinBlocks = 2048;

@@ -7,7 +7,7 @@ import torch
 from oracle import serving as OS
 from oracle.compare import linear_check
 from paper_2605_08755_amd import decode, laq
-from test_gpu_serving import Batch, dev, f16, say
+from test_gpu_serving import Batch, attention_check, dev, f16, say
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
@@ -178,6 +178,80 @@ def test_append_many_sequences(B, T):
         assert r["ok"], r
 
 
+def check(got, q, bt_arrays, window, fp16_probs):
+    table, start, lens, k, v = bt_arrays
+    ref, weight, reach = OS.paged_attention(q, k, v, table, start, lens, window, np.zeros(q.shape))
+    attention_check(got, ref, weight, reach, int(lens.max()), fp16_probs)
+
+
+@pytest.mark.parametrize("B,T,Hq,window", [(64, 60, 4, 0), (65, 65, 4, 0), (129, 600, 4, 0), (129, 600, 2, 9),
+                                           (200, 3000, 2, 0), (4096, 700, 2, 0), (4097, 2000, 1, 0),
+                                           (70000, 900, 2, 20), (1 << 20, 300, 2, 0)])
+def test_attention_many_sequences(B, T, Hq, window):
+    """Rows of sequences anywhere among many, most of which wait."""
+    say("attention many", B, T, Hq, window)
+    rng = np.random.default_rng(B + T + Hq)
+    table, start, lens, k, v = many(rng, B, T, Hq, 1)
+    q = f16(rng, (T, Hq, 128))
+    out = laq.paged_attention(dev(q), dev(k), dev(v), dev(table), dev(start), dev(lens), window=window)
+    torch.cuda.synchronize()
+    check(out.cpu().numpy(), q, (table, start, lens, k, v), window, T * Hq > 16 * B)
+
+
+@pytest.mark.parametrize("tokens,Hq,Hkv", [
+    ([1] * 200, 4, 2),
+    ([1] * 70 + [200] + [0] * 60 + [90, 3], 8, 1),        # chunks in the second and third group
+    ([2] * 64 + [0] * 64 + [33, 1] * 32 + [140], 8, 2),
+])
+def test_attention_many_sequences_split(tokens, Hq, Hkv):
+    """Long sequences, split over ranges, in every group of a batch."""
+    say("attention many split", len(tokens), sum(tokens))
+    rng = np.random.default_rng(len(tokens))
+    before = [int(x) for x in rng.integers(0, 60, len(tokens))]
+    for b in range(5, len(tokens), 61):
+        before[b] = 1500 + b
+    bt = Batch(rng, tokens, before, 16, Hkv)
+    q = f16(rng, (bt.T, Hq, 128))
+    got = attend(q, bt)
+    check(got, q, (bt.table, bt.start, bt.lens, bt.k, bt.v), 0, bt.T * (Hq // Hkv) > 16 * len(tokens))
+    again = attend(q, bt)
+    assert np.array_equal(got.view(np.uint16), again.view(np.uint16))
+
+
+def test_attention_many_sequences_in_a_graph():
+    """The plan of a batch of more than 64 sequences follows the arrays that the
+    host changes between replays; what the workspace held before does not matter."""
+    say("attention many graph")
+    rng = np.random.default_rng(41)
+    Hq, Hkv, B, width = 4, 2, 100, 60
+    k, v = (dev(f16(rng, (B * width, Hkv, 16, 128))) for _ in range(2))
+    table = dev(rng.permutation(B * width).astype(np.int32).reshape(B, width))
+    start = dev(np.arange(B + 1, dtype=np.int32))
+    lens = torch.ones((B,), dtype=torch.int32, device=DEV)
+    q = torch.zeros((B, Hq, 128), dtype=torch.float16, device=DEV)
+    out, again = torch.zeros_like(q), torch.zeros_like(q)
+    nbytes = laq.paged_attention_workspace_bytes(B, B, Hq, Hkv, width * 16)
+    ws, ws2 = (torch.full((nbytes,), x, dtype=torch.uint8, device=DEV) for x in (255, 0))
+    laq.paged_attention(q, k, v, table, start, lens, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        laq.paged_attention(q, k, v, table, start, lens, out=out, workspace=ws)
+    for i in range(4):
+        new = rng.integers(1, 20 + 300 * i, B).astype(np.int32).clip(max=width * 16)
+        lens.copy_(dev(new))
+        first = np.sort(rng.integers(0, B, B - 1)) if i % 2 else np.arange(1, B)
+        start.copy_(dev(np.concatenate([[0], first, [B]]).astype(np.int32)))
+        q.copy_(dev(f16(rng, q.shape)))
+        ws.fill_(255 - i)
+        graph.replay()
+        laq.paged_attention(q, k, v, table, start, lens, out=again, workspace=ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), again.view(torch.int16)), i
+        arrays = tuple(x.cpu().numpy() for x in (table, start, lens, k, v))
+        check(out.cpu().numpy(), q.cpu().numpy(), arrays, 0, False)
+
+
 def best_time(f, calls=3):
     """Shortest of some calls, in ms."""
     times = []
@@ -211,4 +285,17 @@ def test_append_time_grows_with_the_rows():
         q = torch.zeros((B, 2, 128), dtype=torch.float16, device=DEV)
         cs = decode.rope_table(16, 1e6, DEV)
         times.append(best_time(lambda: laq.paged_append(qkv, None, None, cs, k, v, table, start, lens, 2, 1e-6, q_out=q)))
+    assert times[1] < 32 * times[0], times
+
+
+def test_attention_time_grows_with_the_sequences():
+    """As for the append: the items' search of their sequences does not grow
+    with the square of the batch."""
+    say("attention time")
+    times = []
+    for B in (2048, 32768):
+        k, v, table, start, lens = decoding(B)
+        q = torch.zeros((B, 2, 128), dtype=torch.float16, device=DEV)
+        out = torch.zeros_like(q)
+        times.append(best_time(lambda: laq.paged_attention(q, k, v, table, start, lens, out=out)))
     assert times[1] < 32 * times[0], times
