@@ -576,20 +576,23 @@ def _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T):
     num_pages, Hkv, page_size, d = shape = k_pages.shape
     strides = k_pages.stride()
     assert d == HEAD_DIM and k_pages.dtype is t.f16 and v_pages.dtype is t.f16
-    assert v_pages.shape == shape and v_pages.stride() == strides
+    assert v_pages.shape == shape
+    # (a dimension of one element has any stride, here and below)
+    v_strides = v_pages.stride()
+    assert v_strides == strides or all(n == 1 or a == b for n, a, b in zip(shape, strides, v_strides))
     page_stride, head_stride, slot_stride, one = strides
     B, pages = page_table.shape
     table_stride, unit = page_table.stride()
-    assert one == 1 and unit == 1 and page_table.dtype is t.i32 and token_start.dtype is t.i32
+    assert one == 1 and (unit == 1 or pages == 1) and page_table.dtype is t.i32 and token_start.dtype is t.i32
     assert seq_len.dtype is t.i32 and token_start.shape == (B + 1,) and seq_len.shape == (B,)
     assert token_start.is_contiguous() and seq_len.is_contiguous()
     assert (k_pages.get_device() == v_pages.get_device() == page_table.get_device() == token_start.get_device() ==
             seq_len.get_device() == dev >= 0)
-    # a dimension of one element has any stride; the library wants a real one
+    # the library wants a real one, which is not used
     if num_pages == 1:
-        page_stride = max(page_stride, HEAD_DIM)
+        page_stride = HEAD_DIM
     if Hkv == 1:
-        head_stride = max(head_stride, HEAD_DIM)
+        head_stride = HEAD_DIM
     return _PAGED_BATCH.pack(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), token_start.data_ptr(),
                              seq_len.data_ptr(), num_pages, page_size, page_stride, head_stride, slot_stride, pages,
                              table_stride if B > 1 else pages, B, T), Hkv, B, pages * page_size

@@ -299,3 +299,38 @@ def test_attention_time_grows_with_the_sequences():
         out = torch.zeros_like(q)
         times.append(best_time(lambda: laq.paged_attention(q, k, v, table, start, lens, out=out)))
     assert times[1] < 32 * times[0], times
+
+
+# ---------------------------------------------------------------------------
+# layouts
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("tokens", [[1, 2], [40, 1]])
+def test_strides_of_dimensions_of_one_element(tokens):
+    """One page, one key/value head, one table column, of any strides: they do
+    not matter, and neither do those of keys and values have to be equal there."""
+    say("dimensions of one", tokens)
+    rng = np.random.default_rng(3)
+    Hq = 2
+    start = dev(np.concatenate([[0], np.cumsum(tokens)]).astype(np.int32))
+    lens = dev(np.array(tokens, dtype=np.int32) + 3)
+    T = sum(tokens)
+    x = f16(rng, (2, 2, 64, 128))
+    k = dev(x[0])[:, None]                                          # strides of one head: 8192
+    v = dev(x[1])[:, :, None].transpose(1, 2)                       # and 128
+    assert k.stride() != v.stride()
+    column = dev(np.array([[1, 0]], dtype=np.int32)).t()            # [2][1], element stride 2
+    assert column.stride() == (1, 2)
+    q, qkv = f16(rng, (T, Hq, 128)), f16(rng, (T, (Hq + 2) * 128))
+    cs = decode.rope_table(64, 1e6, DEV)
+    plain = [dev(x[0][:, None]), dev(x[1][:, None]), dev(np.array([[1], [0]], dtype=np.int32)), start, lens]
+    odd = [k, v, column, start, lens]
+    outs = [laq.paged_append(dev(qkv), None, None, cs, *a, Hq, 1e-6) for a in (plain, odd)]
+    outs += [laq.paged_attention(dev(q), *a) for a in (plain, odd)]
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[2], outs[3])
+    assert torch.equal(k, plain[0]) and torch.equal(v, plain[1])
+    # one page whose stride is no multiple of 8
+    one = torch.zeros((1, 1, 64, 128), dtype=torch.float16, device=DEV).as_strided((1, 1, 64, 128), (8195, 4, 128, 1))
+    same = torch.zeros((1, 1, 64, 128), dtype=torch.float16, device=DEV)
+    args = (dev(np.array([[0], [0]], dtype=np.int32)), start, lens)
+    assert torch.equal(laq.paged_attention(dev(q), one, one, *args), laq.paged_attention(dev(q), same, same, *args))
