@@ -7,7 +7,10 @@ import torch
 from oracle import serving as OS
 from oracle.compare import linear_check
 from paper_2605_08755_amd import decode, laq
-from test_gpu_serving import Batch, attention_check, dev, f16, say
+from test_gpu_serving import Batch, attention_check, dev, f16, sample_check, say
+from test_gpu_serving import test_attention_not_finite_inputs as not_finite_inputs
+from test_gpu_serving import test_attention_rows_that_see_nothing as rows_that_see_nothing
+from test_gpu_serving import test_attention_unseen_values as unseen_values
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
@@ -334,3 +337,75 @@ def test_strides_of_dimensions_of_one_element(tokens):
     same = torch.zeros((1, 1, 64, 128), dtype=torch.float16, device=DEV)
     args = (dev(np.array([[0], [0]], dtype=np.int32)), start, lens)
     assert torch.equal(laq.paged_attention(dev(q), one, one, *args), laq.paged_attention(dev(q), same, same, *args))
+
+
+# ---------------------------------------------------------------------------
+# few rows beside a chunk: the checks of decoding batches, in the kernel of chunks
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("tokens,before,window", [([1, 60], [100, 60], 0), ([4, 60], [90, 40], 48), ([8, 60], [700, 40], 0)])
+def test_unseen_values_beside_a_chunk(tokens, before, window):
+    unseen_values(tokens, before, window)
+
+
+@pytest.mark.parametrize("tokens,before", [([2, 60], [700, 60]), ([3, 40], [30, 0])])
+def test_not_finite_inputs_beside_a_chunk(tokens, before):
+    not_finite_inputs(tokens, before)
+
+
+def test_rows_that_see_nothing_beside_a_chunk():
+    rows_that_see_nothing([4, 60, 3])
+    rows_that_see_nothing([60, 2, 3])
+
+
+def test_two_streams_at_once():
+    """Calls in flight on two streams, workspaces taken from the allocator."""
+    say("two streams")
+    rng = np.random.default_rng(77)
+    batches = [Batch(rng, *x, 16, 2) for x in (([1, 1, 2], [3000, 900, 40]), ([200, 1], [1500, 2500]))]
+    qs = [f16(rng, (bt.T, 8, 128)) for bt in batches]
+    alone = [attend(q, bt) for q, bt in zip(qs, batches)]
+    args = [(dev(q), *bt.device()) for q, bt in zip(qs, batches)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in batches]
+    got = [[], []]
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(laq.paged_attention(*args[i]))
+    torch.cuda.synchronize()
+    for ref, outs in zip(alone, got):
+        for out in outs:
+            assert np.array_equal(out.cpu().numpy().view(np.uint16), ref.view(np.uint16))
+
+
+# ---------------------------------------------------------------------------
+# sampling: borders of its passes over a row
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("V", [7, 8, 9, 15, 16, 17, 8192, 8199, 40952, 40960, 40961, 49152, 81920, 81927, 122880])
+def test_sample_borders_of_vectors(V):
+    """Vectors of 8 logits, 8192 a pass of the block, 5 and 10 of them loaded
+    ahead: the last token, the last of a vector and the first are drawn too."""
+    say("sample borders", V)
+    rng = np.random.default_rng(V)
+    x = (rng.standard_normal((6, V)) * 2).astype(np.float16)
+    places = [V - 1, 0, V - 2, (V // 8 * 8 - 1) % V, min(8192, V) - 1]
+    for r, t in enumerate(places):
+        x[r, t] = np.float16(30)  # takes all
+    u = rng.random(6).astype(np.float32)
+    tok = sample_check(x, u)
+    assert tok.tolist()[:5] == places
+    sample_check(x, u, temperature=[5.0] * 6, top_k=[3, 0, V, V - 1, 10, 1], top_p=[0.9, 0.5, 1, 1, 0.99, 1])
+    sample_check(x, u, temperature=[0.0] * 6)
+
+
+@pytest.mark.parametrize("n", [1, 2, 1023, 1024, 1025, 2048, 4097])
+def test_sample_equal_tokens(n):
+    """The nth of so many tokens of one value, of which 1024 are listed."""
+    say("sample equal tokens", n)
+    V = 20011
+    rng = np.random.default_rng(n)
+    x = np.full((7, V), -np.inf, dtype=np.float16)
+    for r in range(7):
+        x[r, rng.permutation(V)[:n]] = np.float16(2.5)
+    sample_check(x, np.array([0.0, 0.2, 0.5, 0.7, 0.999, 1.0, 1 / 3], dtype=np.float32))
+    sample_check(x, np.full(7, 0.99, dtype=np.float32), top_k=[1, n, 1024, 1025, 0, n + 1, max(n - 1, 1)])
