@@ -373,6 +373,8 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, const int* __res
   const uint64_t past = __ballot(upto > idx);
   if (!past) return it;
   const int l = __ffsll((unsigned long long)past) - 1;
+  const int i = idx - readlane(upto - own, l);
+  if (i < 0) return it;  // (token_start out of order, so far that sums of a plan pass 2^31)
   it.found = true;
   it.b = b0 + l;
   it.s0 = readlane(q.s0, l);
@@ -381,7 +383,6 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, const int* __res
   it.end = readlane(q.end, l);
   it.lo = readlane(q.lo, l);
   it.splits = readlane(splits, l);
-  const int i = idx - readlane(upto - own, l);
   // the last tiles of a prompt see the most positions: they go first
   // (divisions of uniform values are vector instructions: their results are made uniform again)
   const int back = SPLIT ? i : uniform(i / it.splits);
