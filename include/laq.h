@@ -542,7 +542,8 @@ laq_status laq_silu_mul_f16(const void *gate_up, void *y, int64_t M, int64_t I, 
  *
  * page_table, token_start and seq_len are DEVICE arrays that the host does not
  * read: a captured graph follows their contents.  token_start must not
- * decrease.  Rows below token_start[0] or from token_start[B] on belong to no
+ * decrease, and lies in 0..T (what does not counts as the nearer of the two).
+ * Rows below token_start[0] or from token_start[B] on belong to no
  * sequence: their outputs are left as they were.  What the arrays hold is
  * checked on the device: a page number outside 0..num_pages-1 (-1, say, for a
  * page that was given back) is a page that is not there, positions from

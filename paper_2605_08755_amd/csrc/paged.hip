@@ -104,9 +104,9 @@ __device__ __forceinline__ int wave_sum(int v) {
 // lanes a head: lane i holds dimensions 8i .. 8i + 7 and their rotation partners 64
 // further, so a head's two 128-byte halves are loaded and stored whole and the
 // norm needs one sum over eight lanes.  What bounds it: the bytes of the rows
-// in and out (measured on MI355X, 16384 rows, 32:8 heads: 82 us, 4.9 TB/s,
+// in and out (measured on MI355X, 16384 rows, 32:8 heads: 84 us, 4.9 TB/s,
 // a large copy moves 5.0); few rows are a launch and three dependent reads
-// (16 rows: 3.6 us).  The row's table line is read once per wave.
+// (16 rows: 3.7 us).  The row's table line is read once per wave.
 // The row's sequence is found while its first loads are in flight: among the
 // sequences' ends, which do not decrease, by 64 of them a step (up to 64
 // sequences one step, 2^20 four).
@@ -462,10 +462,11 @@ struct Out {
 // the probabilities stay in 32 bits.  Two blocks per compute unit: one's
 // search for its item, first loads and last joining lie under the other's
 // stream.  (Measured on MI355X: sequences of 131072, 77777 and 901 positions,
-// 64:8 heads, 140 us, 6.1 TB/s; 16 of up to 8192, 32:8 heads, 37 us, of which
-// about 8 are the search, the first loads and the joining of the waves; one of
-// 300, 7.4 us.)  The page numbers of 32 steps sit in one register of a wave (lane l:
-// half l & 1 of step l >> 1) and become scalar buffer descriptors.
+// 64:8 heads, 147 us, 5.8 TB/s (the shortest of 24 calls 140); 16 of up to 8192,
+// 32:8 heads, 40 us (37), of which about 8 are the search, the first loads and
+// the joining of the waves; one of 300, 7.6 us (7.3).)  The page numbers of 32
+// steps sit in one register of a wave (lane l: half l & 1 of step l >> 1) and
+// become scalar buffer descriptors.
 constexpr int kWaves = 4;
 constexpr int kStep = 32;
 constexpr int kRowBytes = (kStep + 4) * 4;         // a row of probabilities (4 words of padding)
@@ -768,14 +769,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // chunk beside 15 decoding rows 77.8 -> 78.2 us; two waves more for the
 // probabilities' remainders instead, 84.8.)
 //
-// What bounds it: LDS bandwidth.  A wave's 32 rows need a tile's keys and
-// values from LDS whole, 32 KiB a wave and tile, and the staging writes 32 KiB
-// a block: a compute unit's eight waves take 288 KiB for 8 x 32 matrix
-// instructions (as two blocks of 128 rows, 320 KiB and twice the staging
-// instructions: prompts 945 us, a chunk beside 15 decoding rows 80).  (Measured
-// on MI355X, kernel alone, without the joining: two prompts of 8192 and 4001
-// rows, 32:8 heads, 860 us back to back, 790 the shortest, 860 TFLOP/s; a
-// library's fp16 8192^3 product reaches 1150.  With 128 rows a tile took a wave
+// What bounds it: the issue of matrix and vector instructions by two waves a
+// SIMD that do little of the one while the other does the other.  (Counters of
+// two prompts of 8192 and 4001 rows, 32:8 heads, on MI355X: matrix instructions
+// 42 % of the SIMDs' cycles, vector instructions 48 %; LDS active 27 % of the
+// compute units' cycles, no bank conflicts.  Kernel alone, without the joining:
+// 874 us, 780 TFLOP/s, the median of 24 calls under a kernel trace, 823 the
+// shortest; a call with the joining 770 us, 885 TFLOP/s, where nothing traces; a
+// library's fp16 8192^3 product reaches 1150.  As two blocks of 128 rows, with
+// twice the staging instructions, 945.  With 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
 // exponentials, 850 the value sums, 1100 issuing the next tile's loads and
 // stores.  Not faster: the two waves of a SIMD kept a phase apart, the operands
@@ -1253,7 +1255,11 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
 // Up to 16 rows per sequence on average go to the 16-row kernel.  (Measured on
 // MI355X, 16-row -> 256-row kernel at twice and four times that: 32:8 heads, one
 // sequence of 6000, 20 -> 14.5 and 25 -> 16 us; eight of 2000, 35 -> 29 and 52 ->
-// 34; 64:8, four of 8000, 47 -> 43 and 75 -> 51; but one of 500, 12 -> 15.)
+// 34; 64:8, four of 8000, 47 -> 43 and 75 -> 51; but one of 500, 12 -> 15.  Where
+// sequences are of unequal size, at the border, 32:8: 63 decoding rows beside a
+// chunk of 193 rows, all at 500 or at 2000, 67 -> 82 and 161 -> 189; a chunk of 256
+// rows at 6000 beside 63 waiting sequences 180 -> 119, of 16 rows 30 -> 42; 64
+// decoding rows and 193 of padding 98 -> 97, 16 and 49 of padding 35 -> 38.)
 AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
   if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity);
   return plan_of<kLargeRows>(B, T, R, Hkv, capacity);

@@ -61,8 +61,8 @@ __device__ __forceinline__ double logit_of(int k) {
 __device__ __forceinline__ int place_of(int k) { return 32767 - k; }
 __device__ __forceinline__ int value_at(int b) { return 32767 - b; }
 
-// 2^y for y <= 0, to about 2^-50 of it: y = n + f, |f| <= 1/2, and the series
-// of exp(f ln 2), of which the term after the last is below 1e-14.
+// 2^y for y <= 0, to 2^-46 of it: y = n + f, |f| <= 1/2, and the series of
+// exp(f ln 2), of which what is left out is below 9e-15.
 __device__ __forceinline__ double exp2_neg(double y) {
   y = fmax(y, -2000.0);
   const double n = rint(y);

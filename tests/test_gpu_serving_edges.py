@@ -339,6 +339,27 @@ def test_strides_of_dimensions_of_one_element(tokens):
     assert torch.equal(laq.paged_attention(dev(q), one, one, *args), laq.paged_attention(dev(q), same, same, *args))
 
 
+@pytest.mark.parametrize("tokens", [[2, 1, 3], [2, 40, 30]])
+def test_row_starts_outside_the_batch(tokens):
+    """Row starts below 0 count as 0 and ones above T as T."""
+    say("row starts outside", tokens)
+    rng = np.random.default_rng(12)
+    Hq, Hkv = 4, 2
+    bt = Batch(rng, tokens, [30, 70, 9], 16, Hkv, garbage=None)
+    q, qkv = f16(rng, (bt.T, Hq, 128)), f16(rng, (bt.T, (Hq + 2 * Hkv) * 128))
+    cs = decode.rope_table(200, 1e6, DEV)
+    got = []
+    for start in (bt.start, np.array([-7, *bt.start[1:3], bt.T + 1000], dtype=np.int32),
+                  np.array([-2**31, *bt.start[1:3], 2**31 - 1], dtype=np.int32)):
+        k, v, table, _, lens = bt.device()
+        rows = laq.paged_append(dev(qkv), None, None, cs, k, v, table, dev(start), lens, Hq, 1e-6)
+        got.append((rows, k, v, laq.paged_attention(dev(q), k, v, table, dev(start), lens)))
+    torch.cuda.synchronize()
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert torch.equal(a, b)
+
+
 # ---------------------------------------------------------------------------
 # few rows beside a chunk: the checks of decoding batches, in the kernel of chunks
 # ---------------------------------------------------------------------------
