@@ -123,7 +123,7 @@ def sample_row(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     kept = math.fsum(w)
     u = float(u) if u > 0 else 0.0
     run = 0.0
-    for i, a in enumerate(w):
+    for i, a in enumerate(w if u < 1 else []):  # (the sum of all may be rounded above `kept` before the last)
         run += a
         if run > u * kept:
             return order[i], a / kept
