@@ -775,7 +775,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 // 42 % of the SIMDs' cycles, vector instructions 48 %; LDS active 27 % of the
 // compute units' cycles, no bank conflicts.  Kernel alone, without the joining:
 // 874 us, 780 TFLOP/s, the median of 24 calls under a kernel trace, 823 the
-// shortest; a call with the joining 770 us, 885 TFLOP/s, where nothing traces; a
+// shortest; a call with the joining 768 to 804, 847 to 887 TFLOP/s, untraced; a
 // library's fp16 8192^3 product reaches 1150.  As two blocks of 128 rows, with
 // twice the staging instructions, 945.  With 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
