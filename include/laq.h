@@ -621,6 +621,105 @@ laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, 
                                    int64_t head_dim, int64_t window, void *out, void *workspace,
                                    int64_t workspace_bytes, void *stream);
 
+/* Caches of 8 bits.  A key or value is code * 2^(scale - 127): the code a byte
+ * in e4m3 (OCP: sign, 4 exponent bits of bias 7, 3 of significand; 0x7F and 0xFF
+ * are NaN), the scale a byte (e8m0) that 16 consecutive positions of one
+ * key/value head share, one for their keys and one for their values.  The
+ * batch is a laq_paged_batch whose k_pages and v_pages hold codes: strides
+ * count codes (bytes) and are multiples of 16.  The scales of block
+ * (t % page_size) / 16 of a page lie at
+ *   scales[(page * Hkv + g) * (page_size / 16) + (t % page_size) / 16].
+ * Scales are 112..134 (2^-15 to 2^7, with which every value is an fp16 number);
+ * bytes outside are taken as the nearer of the two. */
+
+/* laq_paged_append_e4m3 -- laq_paged_append_f16 into a cache of 8 bits: the
+ * same q_out, bit for bit; keys (normalized and rotated, in fp32) and values
+ * become codes.  For every block of 16 positions that gets new rows, and each
+ * of keys and values of a head:
+ *   scale = the least of 112..134 with max |x| <= 448 * 2^(scale - 127), x the
+ *           block's new values that are finite; not below the scale that the
+ *           block has, when it holds earlier positions of the sequence, whose
+ *           codes are rounded again by the new scale where it is larger
+ *   code  = x / 2^(scale - 127), rounded to nearest even, saturated at 448 (x
+ *           past 57344); NaN where x is not finite.
+ * The scale and the codes of earlier positions in a block that gets new rows are
+ * thus written by the call: two sequences of one call must not append to the
+ * same block of 16, and a block that is appended to must not be read by another
+ * sequence meanwhile.  Blocks whose first position is new start anew, whatever
+ * their scales and codes were.
+ *   k_scales, v_scales  [in/out] uint8 [num_pages][Hkv][page_size / 16].
+ * Everything else, rows without a place among it, as for laq_paged_append_f16.
+ * Errors: as laq_paged_append_f16's (strides of the pages: MISALIGNED unless
+ * multiples of 16); NULL_POINTER also for the scales. */
+laq_status laq_paged_append_e4m3(const laq_paged_batch *batch, uint8_t *k_scales, uint8_t *v_scales, const void *qkv,
+                                 int64_t qkv_stride, const void *q_norm_weight, const void *k_norm_weight,
+                                 const float *cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv, int64_t head_dim,
+                                 float eps, void *q_out, void *stream);
+
+/* laq_paged_attention_e4m3 -- laq_paged_attention_f16 over a cache of 8 bits:
+ * the attention over the values that its codes stand for, which are fp16
+ * numbers, so that nothing is rounded on reading them.  Probabilities of
+ * sequences with at most 16 / (Hq / Hkv) rows keep 22 bits (two fp16 numbers
+ * whose sum has them) whatever else the batch holds; those of longer chunks as
+ * for laq_paged_attention_f16.  The workspace is
+ * laq_paged_attention_workspace_bytes', whatever the cache.
+ * Errors: as laq_paged_attention_f16's (strides of the pages: MISALIGNED unless
+ * multiples of 16); NULL_POINTER also for the scales. */
+laq_status laq_paged_attention_e4m3(const laq_paged_batch *batch, const uint8_t *k_scales, const uint8_t *v_scales,
+                                    const void *q, int64_t Hq, int64_t Hkv, int64_t head_dim, int64_t window, void *out,
+                                    void *workspace, int64_t workspace_bytes, void *stream);
+
+/* laq_logits_adjust -- what laq_adjust_logits_f16 applies to each row.  Device
+ * arrays that the host does not read (a captured graph follows them); each
+ * group of members may be absent (NULL). */
+#define LAQ_MAX_BIASES 2047
+typedef struct laq_logits_adjust {
+    /* tokens so far: row r's are history[r * history_stride + i], i <
+     * history_len[r] (taken into 0..history_room), the first prompt_len[r] of
+     * them the prompt's and the others generated (NULL: all are generated).
+     * Entries outside 0..V-1 name nothing. */
+    const int32_t *history;
+    const int32_t *history_len; /* [rows] */
+    const int32_t *prompt_len;  /* [rows], or NULL */
+    int64_t history_stride;     /* 0..2^32 (0: all rows share one) */
+    int64_t history_room;       /* entries a row can have, below 2^20 */
+    const float *repetition;    /* [rows], or NULL: 1 */
+    const float *frequency;     /* [rows], or NULL: 0 */
+    const float *presence;      /* [rows], or NULL: 0 */
+    /* biases: row r's are bias_value[r * bias_stride + i] for token
+     * bias_token[r * bias_stride + i], i < biases; tokens outside 0..V-1 are
+     * passed over, and of several for one token the last counts. */
+    const int32_t *bias_token;
+    const float *bias_value;
+    int64_t bias_stride; /* 0..2^32 */
+    int64_t biases;      /* 0..LAQ_MAX_BIASES */
+    /* allowed tokens: bit v % 32 of mask[r * mask_stride + v / 32] is set for
+     * those that may be drawn (V / 32 words, rounded up). */
+    const uint32_t *mask;
+    int64_t mask_stride; /* 0..2^32 */
+} laq_logits_adjust;
+
+/* laq_adjust_logits_f16 -- logits fp16 [rows][V] before sampling.  Of token v's
+ * logit x, with c the times that the row's generated tokens name v:
+ *   x = x > 0 ? x / repetition[r] : x * repetition[r]   if history names v
+ *   x = x - frequency[r] * c - presence[r]              if c > 0
+ *   x = x + bias                                        if v is listed
+ *   x = -inf                                            if v is not allowed
+ * in fp32 (each step rounded by itself), rounded to fp16 once.  Logits that
+ * none of this touches are copied as they are.  Settings are not checked: what
+ * the formulas give is what is written.
+ *   out  [out] fp16 [rows][V], out_stride elements between rows: logits itself
+ *        with the same stride (logits that nothing touches are then not
+ *        written), or memory that does not overlap it.
+ * rows == 0: nothing is done.
+ * Errors: NULL_POINTER (adjust, logits, out; history without history_len,
+ * bias_token without bias_value); BAD_SHAPE (V outside 1..2^24, rows < 0 or >=
+ * 2^22, sizes above, strides of logits and out below V or above 2^32, partial
+ * overlap, logits that would take 2^32 threads and more); MISALIGNED (logits
+ * and out 2-byte, the others 4-byte). */
+laq_status laq_adjust_logits_f16(const laq_logits_adjust *adjust, const void *logits, int64_t logits_stride,
+                                 int64_t rows, int64_t V, void *out, int64_t out_stride, void *stream);
+
 /* laq_sample_f16 -- draws one token per row from logits fp16 [rows][V]
  * (logits_stride elements between rows, >= V), each row with its own settings
  * and its own uniform number u.  With the tokens ordered by logit, largest

@@ -128,3 +128,118 @@ def sample_row(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         if run > u * kept:
             return order[i], a / kept
     return order[n - 1], w[-1] / kept
+
+
+# ---------------------------------------------------------------------------
+# caches of 8 bits: e4m3 codes, an e8m0 scale for each 16 positions of a head
+# ---------------------------------------------------------------------------
+BLOCK = 16
+LOWEST, HIGHEST = 112, 134
+
+
+def e4m3_values():
+    """float64 [256]: the numbers that the codes stand for."""
+    out = []
+    for c in range(256):
+        e, m = c >> 3 & 15, c & 7
+        v = math.nan if c & 127 == 127 else math.ldexp(8 + m, e - 10) if e else math.ldexp(m, -9)
+        out.append(-v if c & 128 else v)
+    return np.array(out)
+
+
+def e4m3(x):
+    """Codes of float64 values: the nearest, of two the even one; saturated;
+    0x7F where not finite."""
+    x = np.asarray(x, dtype=np.float64)
+    a = np.minimum(np.abs(np.where(np.isfinite(x), x, 0.0)), 448.0)
+    v = e4m3_values()[:127]  # 0 .. 448, ascending
+    i = np.clip(np.searchsorted(v, a, side="right") - 1, 0, 125)
+    below, above = a - v[i], v[i + 1] - a
+    c = np.where((above < below) | ((above == below) & (i % 2 == 1)), i + 1, i)
+    c = np.where(np.signbit(x), c | 128, c)
+    return np.where(np.isfinite(x), c, 127).astype(np.uint8)
+
+
+def least_scale(a):
+    """The least of 112..134 with a <= 448 * 2^(scale - 127), else 134."""
+    for s in range(LOWEST, HIGHEST):
+        if a <= math.ldexp(448.0, s - 127):
+            return s
+    return HIGHEST
+
+
+def clamp_scale(s):
+    return min(max(int(s), LOWEST), HIGHEST)
+
+
+def cache_values(codes, scales):
+    """float64 [P][Hkv][page_size][d] of codes and scales [P][Hkv][page_size / 16]."""
+    s = np.repeat(np.clip(scales.astype(np.int64), LOWEST, HIGHEST) - 127, BLOCK, axis=2)
+    return np.ldexp(e4m3_values()[codes], s[..., None])
+
+
+def paged_append_e4m3(qkv, q_w, k_w, cos_sin, caches, table, start, seq_len, Hq, eps, q_out):
+    """caches: (codes, scales) of keys and of values.  Returns (q_out in
+    float64, [(codes, scales, exact)] of keys and values): `exact` holds the new
+    positions' x / 2^(scale - 127) before rounding and saturation, NaN elsewhere;
+    the codes there are its rounding."""
+    P, Hkv, ps, d = caches[0][0].shape
+    nothing = [np.full((P, Hkv, ps, d), np.nan) for _ in range(2)]
+    q, new_k, new_v = paged_append(qkv, q_w, k_w, cos_sin, *nothing, table, start, seq_len, Hq, eps, q_out)
+    blocks = {}  # (page, block) -> (slots of the new rows, whether earlier positions are there)
+    for r, b, pos in rows(start, seq_len):
+        at = place(table, b, pos, ps, P)
+        if at is None or pos >= cos_sin.shape[0]:
+            continue
+        slots, before = blocks.setdefault((at[0], at[1] // BLOCK), ([], pos % BLOCK))
+        slots.append(at[1])
+    done = []
+    for (codes, scales), new in zip(caches, (new_k, new_v)):
+        codes, scales, exact = codes.copy(), scales.copy(), np.full((P, Hkv, ps, d), np.nan)
+        for (page, block), (slots, before) in blocks.items():
+            for g in range(Hkv):
+                x = new[page, g, slots]
+                s = least_scale(np.abs(x[np.isfinite(x)]).max(initial=0.0))
+                if before:
+                    was = clamp_scale(scales[page, g, block])
+                    s = max(s, was)
+                    if s > was:
+                        old = codes[page, g, block * BLOCK:block * BLOCK + before]
+                        again = e4m3(np.ldexp(e4m3_values()[old], was - s))
+                        codes[page, g, block * BLOCK:block * BLOCK + before] = again
+                if not before or clamp_scale(scales[page, g, block]) != s:
+                    scales[page, g, block] = s
+                exact[page, g, slots] = np.ldexp(x, 127 - s)
+                codes[page, g, slots] = e4m3(exact[page, g, slots])
+        done.append((codes, scales, exact))
+    return q, done
+
+
+# ---------------------------------------------------------------------------
+# logits before sampling
+# ---------------------------------------------------------------------------
+def adjust_row(logits, history=(), prompt=0, repetition=1.0, frequency=0.0, presence=0.0, biases=(), mask=None):
+    """float64: one row's logits after the penalties for the tokens of `history`
+    (its first `prompt` the prompt's), the biases ((token, value), the last for a
+    token) and the mask (words of 32 tokens)."""
+    x = np.array(logits, dtype=np.float64)
+    V = len(x)
+    count, seen = {}, set()
+    for i, t in enumerate(history):
+        if 0 <= t < V:
+            seen.add(int(t))
+            if i >= prompt:
+                count[int(t)] = count.get(int(t), 0) + 1
+    with np.errstate(all="ignore"):
+        for t in seen:
+            x[t] = x[t] / np.float64(repetition) if x[t] > 0 else x[t] * np.float64(repetition)
+        for t, c in count.items():
+            x[t] = x[t] - np.float64(frequency) * c - np.float64(presence)
+        for t, v in dict((int(t), v) for t, v in biases).items():
+            if 0 <= t < V:
+                x[t] = x[t] + np.float64(v)
+    if mask is not None:
+        for t in range(V):
+            if not int(mask[t // 32]) >> (t % 32) & 1:
+                x[t] = -np.inf
+    return x

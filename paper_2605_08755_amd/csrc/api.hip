@@ -551,7 +551,8 @@ namespace {
 bool finite_eps(float eps) { return eps >= 0.0f && eps < INFINITY; }
 
 // Checks a batch's sizes (no pointers: an empty batch may have none).
-laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int64_t Hkv, int64_t head_dim) {
+// bytes: of an element of the caches.
+laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int64_t Hkv, int64_t head_dim, int bytes = 2) {
   if (!b) return fail(LAQ_ERR_NULL_POINTER, fn, "null batch");
   if (head_dim != kHeadDimAbi) return fail(LAQ_ERR_BAD_SHAPE, fn, "head_dim must be 128");
   if (Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096)
@@ -570,8 +571,8 @@ laq_status check_batch(const char* fn, const laq_paged_batch* b, int64_t Hq, int
   if (b->slot_stride < kHeadDimAbi || b->slot_stride > (1 << 26) || b->head_stride < kHeadDimAbi ||
       b->head_stride > (1LL << 40) || b->page_stride < kHeadDimAbi || b->page_stride >= (1LL << 31))
     return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be at least 128 (slots at most 2^26, pages below 2^31, heads at most 2^40)");
-  if (b->slot_stride % 8 != 0 || b->head_stride % 8 != 0 || b->page_stride % 8 != 0)
-    return fail(LAQ_ERR_MISALIGNED, fn, "strides must be multiples of 8 elements");
+  if (b->slot_stride * bytes % 16 != 0 || b->head_stride * bytes % 16 != 0 || b->page_stride * bytes % 16 != 0)
+    return fail(LAQ_ERR_MISALIGNED, fn, "strides must be multiples of 16 bytes");
   return LAQ_OK;
 }
 
@@ -603,6 +604,68 @@ laq::PagedBatch internal_batch(const laq_paged_batch& b) {
   return p;
 }
 
+laq::PagedCodes internal_codes(const laq_paged_batch& b, uint8_t* k_scales, uint8_t* v_scales, int64_t Hkv) {
+  laq::PagedCodes p;
+  static_cast<laq::PagedBatch&>(p) = internal_batch(b);
+  p.page_bytes = (uint32_t)b.page_stride;
+  p.k_scales = k_scales;
+  p.v_scales = v_scales;
+  p.scale_page = Hkv * (b.page_size / 16);
+  return p;
+}
+
+// What is checked of an append and of an attention, whatever the type of the
+// caches, in this order; a batch without rows is `nothing`.
+laq_status check_append(const char* fn, const laq_paged_batch* batch, const void* qkv, int64_t qkv_stride,
+                        const void* q_norm_weight, const void* k_norm_weight, const float* cos_sin, int64_t rope_rows,
+                        int64_t Hq, int64_t Hkv, int64_t head_dim, float eps, const void* q_out, int bytes,
+                        bool* nothing) {
+  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim, bytes);
+  if (st != LAQ_OK) return st;
+  if (rope_rows < 1 || rope_rows > (1LL << 31)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= rope_rows <= 2^31");
+  if (qkv_stride < (Hq + 2 * Hkv) * head_dim || qkv_stride > (1LL << 40))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "qkv_stride must be at least (Hq + 2 Hkv) * 128");
+  if (qkv_stride % 8 != 0) return fail(LAQ_ERR_MISALIGNED, fn, "qkv_stride must be a multiple of 8 elements");
+  if (!finite_eps(eps)) return fail(LAQ_ERR_BAD_SHAPE, fn, "eps must be finite and >= 0");
+  if ((*nothing = batch->B == 0 || batch->T == 0)) return LAQ_OK;
+  if (!qkv || !cos_sin || !q_out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
+  const int64_t threads = bytes == 2 ? laq::paged_append_threads(batch->T, Hq, Hkv)
+                                     : laq::paged_append_codes_threads(batch->T, Hq, Hkv);
+  if (threads > 0xFFFFFFFFLL) return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
+  if (!aligned(qkv, 16) || !aligned(q_norm_weight, 16) || !aligned(k_norm_weight, 16) || !aligned(cos_sin, 4) ||
+      !aligned(q_out, 16))
+    return fail(LAQ_ERR_MISALIGNED, fn, "cos_sin must be 4-byte, fp16 arrays 16-byte aligned");
+  return LAQ_OK;
+}
+
+laq_status check_attention(const char* fn, const laq_paged_batch* batch, const void* q, int64_t Hq, int64_t Hkv,
+                           int64_t head_dim, int64_t window, const void* out, const void* workspace,
+                           int64_t workspace_bytes, int bytes, bool* nothing) {
+  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim, bytes);
+  if (st != LAQ_OK) return st;
+  if (window < 0 || window > (1LL << 30)) return fail(LAQ_ERR_BAD_SHAPE, fn, "window must be in 0..2^30");
+  if ((*nothing = batch->B == 0 || batch->T == 0)) return LAQ_OK;
+  if (!q || !out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
+  const int64_t capacity = batch->table_pages * batch->page_size;
+  const int64_t need = laq::paged_attention_workspace(batch->B, batch->T, Hq, Hkv, capacity);
+  if (need > 0 && !workspace) return fail(LAQ_ERR_NULL_POINTER, fn, "null workspace");
+  if (workspace_bytes < need)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below laq_paged_attention_workspace_bytes");
+  if (laq::paged_attention_threads(batch->B, batch->T, Hq, Hkv, capacity) > 0xFFFFFFFFLL)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
+    return fail(LAQ_ERR_MISALIGNED, fn, "q, out and workspace must be 16-byte aligned");
+  return LAQ_OK;
+}
+
+// Bytes [a, a + an) and [b, b + bn) have some in common.
+bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+}
+
 }  // namespace
 
 extern "C" {
@@ -613,26 +676,35 @@ laq_status laq_paged_append_f16(const laq_paged_batch* batch, const void* qkv, i
                                 void* stream) {
   const char* fn = "laq_paged_append_f16";
   const laq::LaunchEvents ev = take_events();
-  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim);
+  bool nothing = false;
+  const laq_status st = check_append(fn, batch, qkv, qkv_stride, q_norm_weight, k_norm_weight, cos_sin, rope_rows, Hq, Hkv,
+                                     head_dim, eps, q_out, 2, &nothing);
   if (st != LAQ_OK) return st;
-  if (rope_rows < 1 || rope_rows > (1LL << 31)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= rope_rows <= 2^31");
-  if (qkv_stride < (Hq + 2 * Hkv) * head_dim || qkv_stride > (1LL << 40))
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "qkv_stride must be at least (Hq + 2 Hkv) * 128");
-  if (qkv_stride % 8 != 0) return fail(LAQ_ERR_MISALIGNED, fn, "qkv_stride must be a multiple of 8 elements");
-  if (!finite_eps(eps)) return fail(LAQ_ERR_BAD_SHAPE, fn, "eps must be finite and >= 0");
-  if (batch->B == 0 || batch->T == 0) return ok();
-  if (!qkv || !cos_sin || !q_out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
-  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
-  if (laq::paged_append_threads(batch->T, Hq, Hkv) > 0xFFFFFFFFLL)
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
-  if (!aligned(qkv, 16) || !aligned(q_norm_weight, 16) || !aligned(k_norm_weight, 16) || !aligned(cos_sin, 4) ||
-      !aligned(q_out, 16))
-    return fail(LAQ_ERR_MISALIGNED, fn, "cos_sin must be 4-byte, fp16 arrays 16-byte aligned");
+  if (nothing) return ok();
   return hip_status(fn, laq::launch_paged_append(
                             internal_batch(*batch), static_cast<const uint16_t*>(qkv), qkv_stride,
                             static_cast<const uint16_t*>(q_norm_weight), static_cast<const uint16_t*>(k_norm_weight),
                             cos_sin, rope_rows, Hq, Hkv, eps, static_cast<uint16_t*>(q_out),
                             static_cast<hipStream_t>(stream), ev));
+}
+
+laq_status laq_paged_append_e4m3(const laq_paged_batch* batch, uint8_t* k_scales, uint8_t* v_scales, const void* qkv,
+                                 int64_t qkv_stride, const void* q_norm_weight, const void* k_norm_weight,
+                                 const float* cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv, int64_t head_dim,
+                                 float eps, void* q_out, void* stream) {
+  const char* fn = "laq_paged_append_e4m3";
+  const laq::LaunchEvents ev = take_events();
+  bool nothing = false;
+  const laq_status st = check_append(fn, batch, qkv, qkv_stride, q_norm_weight, k_norm_weight, cos_sin, rope_rows, Hq, Hkv,
+                                     head_dim, eps, q_out, 1, &nothing);
+  if (st != LAQ_OK) return st;
+  if (nothing) return ok();
+  if (!k_scales || !v_scales) return fail(LAQ_ERR_NULL_POINTER, fn, "null scales");
+  return hip_status(fn, laq::launch_paged_append_codes(
+                            internal_codes(*batch, k_scales, v_scales, Hkv), static_cast<const uint16_t*>(qkv),
+                            qkv_stride, static_cast<const uint16_t*>(q_norm_weight),
+                            static_cast<const uint16_t*>(k_norm_weight), cos_sin, rope_rows, Hq, Hkv, eps,
+                            static_cast<uint16_t*>(q_out), static_cast<hipStream_t>(stream), ev));
 }
 
 int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
@@ -647,25 +719,94 @@ laq_status laq_paged_attention_f16(const laq_paged_batch* batch, const void* q, 
                                    int64_t workspace_bytes, void* stream) {
   const char* fn = "laq_paged_attention_f16";
   const laq::LaunchEvents ev = take_events();
-  laq_status st = check_batch(fn, batch, Hq, Hkv, head_dim);
+  bool nothing = false;
+  const laq_status st = check_attention(fn, batch, q, Hq, Hkv, head_dim, window, out, workspace, workspace_bytes, 2, &nothing);
   if (st != LAQ_OK) return st;
-  if (window < 0 || window > (1LL << 30)) return fail(LAQ_ERR_BAD_SHAPE, fn, "window must be in 0..2^30");
-  if (batch->B == 0 || batch->T == 0) return ok();
-  if (!q || !out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
-  if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
-  const int64_t capacity = batch->table_pages * batch->page_size;
-  const int64_t need = laq::paged_attention_workspace(batch->B, batch->T, Hq, Hkv, capacity);
-  if (need > 0 && !workspace) return fail(LAQ_ERR_NULL_POINTER, fn, "null workspace");
-  if (workspace_bytes < need)
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below laq_paged_attention_workspace_bytes");
-  if (laq::paged_attention_threads(batch->B, batch->T, Hq, Hkv, capacity) > 0xFFFFFFFFLL)
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "the batch has too many rows for one launch");
-  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16))
-    return fail(LAQ_ERR_MISALIGNED, fn, "q, out and workspace must be 16-byte aligned");
+  if (nothing) return ok();
   return hip_status(fn, laq::launch_paged_attention(internal_batch(*batch), static_cast<const uint16_t*>(q), Hq, Hkv,
                                                     window, static_cast<uint16_t*>(out),
                                                     static_cast<float*>(workspace), static_cast<hipStream_t>(stream),
                                                     ev));
+}
+
+laq_status laq_paged_attention_e4m3(const laq_paged_batch* batch, const uint8_t* k_scales, const uint8_t* v_scales,
+                                    const void* q, int64_t Hq, int64_t Hkv, int64_t head_dim, int64_t window, void* out,
+                                    void* workspace, int64_t workspace_bytes, void* stream) {
+  const char* fn = "laq_paged_attention_e4m3";
+  const laq::LaunchEvents ev = take_events();
+  bool nothing = false;
+  const laq_status st = check_attention(fn, batch, q, Hq, Hkv, head_dim, window, out, workspace, workspace_bytes, 1, &nothing);
+  if (st != LAQ_OK) return st;
+  if (nothing) return ok();
+  if (!k_scales || !v_scales) return fail(LAQ_ERR_NULL_POINTER, fn, "null scales");
+  return hip_status(fn, laq::launch_paged_attention_codes(
+                            internal_codes(*batch, const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(v_scales), Hkv),
+                            static_cast<const uint16_t*>(q), Hq, Hkv, window, static_cast<uint16_t*>(out),
+                            static_cast<float*>(workspace), static_cast<hipStream_t>(stream), ev));
+}
+
+laq_status laq_adjust_logits_f16(const laq_logits_adjust* adjust, const void* logits, int64_t logits_stride, int64_t rows,
+                                 int64_t V, void* out, int64_t out_stride, void* stream) {
+  const char* fn = "laq_adjust_logits_f16";
+  const laq::LaunchEvents ev = take_events();
+  if (!adjust) return fail(LAQ_ERR_NULL_POINTER, fn, "null adjust");
+  const laq_logits_adjust& a = *adjust;
+  if (rows < 0 || rows >= (1LL << 22)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= rows < 2^22");
+  if (V < 1 || V > (1 << 24)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 1 <= V <= 2^24");
+  for (int64_t s : {logits_stride, out_stride}) {
+    if (s < V && rows > 1) return fail(LAQ_ERR_BAD_SHAPE, fn, "strides of logits and out must be at least V");
+    if (s < 0 || s > (1LL << 32)) return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be in 0..2^32");
+  }
+  if (a.history) {
+    if (a.history_room < 0 || a.history_room >= (1 << 20)) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= history_room < 2^20");
+    if (a.history_stride < 0 || a.history_stride > (1LL << 32)) return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be in 0..2^32");
+    if (!a.history_len) return fail(LAQ_ERR_NULL_POINTER, fn, "null history_len");
+  }
+  if (a.bias_token) {
+    if (a.biases < 0 || a.biases > LAQ_MAX_BIASES) return fail(LAQ_ERR_BAD_SHAPE, fn, "need 0 <= biases <= 2047");
+    if (a.bias_stride < 0 || a.bias_stride > (1LL << 32)) return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be in 0..2^32");
+    if (!a.bias_value) return fail(LAQ_ERR_NULL_POINTER, fn, "null bias_value");
+  }
+  if (a.mask && (a.mask_stride < 0 || a.mask_stride > (1LL << 32)))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "strides must be in 0..2^32");
+  if (rows == 0) return ok();
+  if (!logits || !out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
+  if (!aligned(logits, 2) || !aligned(out, 2)) return fail(LAQ_ERR_MISALIGNED, fn, "logits and out must be 2-byte aligned");
+  for (const void* p : {(const void*)a.history, (const void*)a.history_len, (const void*)a.prompt_len,
+                        (const void*)a.repetition, (const void*)a.frequency, (const void*)a.presence,
+                        (const void*)a.bias_token, (const void*)a.bias_value, (const void*)a.mask})
+    if (!aligned(p, 4)) return fail(LAQ_ERR_MISALIGNED, fn, "the arrays of adjust must be 4-byte aligned");
+  const bool same = out == logits && (rows == 1 || out_stride == logits_stride);
+  if (!same && overlap(logits, ((rows - 1) * logits_stride + V) * 2, out, ((rows - 1) * out_stride + V) * 2))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "out must be logits itself or not overlap it");
+  laq::Adjust d{};
+  d.logits = static_cast<const uint16_t*>(logits);
+  d.out = static_cast<uint16_t*>(out);
+  d.stride = logits_stride;
+  d.out_stride = out_stride;
+  if (a.history && a.history_room > 0 && (a.repetition || a.frequency || a.presence)) {
+    d.history = a.history;
+    d.history_len = a.history_len;
+    d.prompt_len = a.prompt_len;
+    d.history_stride = a.history_stride;
+    d.room = (int)a.history_room;
+    d.repetition = a.repetition;
+    d.frequency = a.frequency;
+    d.presence = a.presence;
+  }
+  if (a.bias_token && a.biases > 0) {
+    d.bias_token = a.bias_token;
+    d.bias_value = a.bias_value;
+    d.bias_stride = a.bias_stride;
+    d.biases = (int)a.biases;
+  }
+  d.mask = reinterpret_cast<const int*>(a.mask);
+  d.mask_stride = a.mask_stride;
+  d.V = (int)V;
+  d.in_place = same;
+  if (laq::adjust_logits_threads(d, rows) > 0xFFFFFFFFLL)
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "too many logits for one launch");
+  return hip_status(fn, laq::launch_adjust_logits(d, rows, static_cast<hipStream_t>(stream), ev));
 }
 
 laq_status laq_sample_f16(const void* logits, int64_t logits_stride, int64_t rows, int64_t V, const float* u,

@@ -261,6 +261,16 @@ struct PagedBatch {
   uint32_t page_bytes;  // between pages
   int slot_stride, page_shift, num_pages, table_pages, B, T;
 };
+// The same with caches of e4m3 codes (k and v then hold bytes), whose scales are
+// e8m0 bytes [num_pages][Hkv][page_size / 16].
+struct PagedCodes : PagedBatch {
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  int64_t scale_page;  // between pages
+  __device__ __forceinline__ int64_t scale_at(int page, int g, int t) const {  // of position t, in this page
+    return page * scale_page + ((int64_t)g << (page_shift - 4)) + ((t & ((1 << page_shift) - 1)) >> 4);
+  }
+};
 // Threads of the append's launch.
 int64_t paged_append_threads(int64_t T, int64_t Hq, int64_t Hkv);
 hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
@@ -272,6 +282,37 @@ int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv,
 int64_t paged_attention_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
 hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,
                                   uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev);
+int64_t paged_append_codes_threads(int64_t T, int64_t Hq, int64_t Hkv);
+hipError_t launch_paged_append_codes(const PagedCodes& pb, const uint16_t* qkv, int64_t qkv_stride, const uint16_t* qw,
+                                     const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq,
+                                     int64_t Hkv, float eps, uint16_t* q_out, hipStream_t stream,
+                                     const LaunchEvents& ev);
+hipError_t launch_paged_attention_codes(const PagedCodes& pb, const uint16_t* q, int64_t Hq, int64_t Hkv,
+                                        int64_t window, uint16_t* out, float* ws, hipStream_t stream,
+                                        const LaunchEvents& ev);
+
+// Logits to be adjusted (laq_logits_adjust of include/laq.h, checked).
+struct Adjust {
+  const uint16_t* logits;
+  uint16_t* out;
+  int64_t stride, out_stride;
+  const int* history;  // null: none
+  const int* history_len;
+  const int* prompt_len;
+  int64_t history_stride;
+  const float* repetition;
+  const float* frequency;
+  const float* presence;
+  const int* bias_token;  // null: none
+  const float* bias_value;
+  int64_t bias_stride;
+  const int* mask;
+  int64_t mask_stride;
+  int V, room, biases;  // tokens; of a row's history; biases of a row
+  bool in_place;
+};
+int64_t adjust_logits_threads(const Adjust& a, int64_t rows);
+hipError_t launch_adjust_logits(const Adjust& a, int64_t rows, hipStream_t stream, const LaunchEvents& ev);
 hipError_t launch_sample(const uint16_t* logits, int64_t stride, int64_t rows, int64_t V, const float* u,
                          const float* temperature, const int* top_k, const float* top_p, const float* min_p, int* token,
                          float* prob, hipStream_t stream, const LaunchEvents& ev);

@@ -36,7 +36,8 @@ EXPORTS = ("laq_abi_version", "laq_status_string", "laq_last_error", "laq_profil
            "laq_add_rmsnorm_linear_swiglu_w3g128", "laq_add_rmsnorm_linear_swiglu_w4g128",
            "laq_mlp_workspace_bytes", "laq_add_rmsnorm_mlp_w3g128", "laq_linear_residual_w3g128",
            "laq_linear_residual_w4g128", "laq_paged_append_f16", "laq_paged_attention_workspace_bytes",
-           "laq_paged_attention_f16", "laq_sample_f16")
+           "laq_paged_attention_f16", "laq_sample_f16", "laq_paged_append_e4m3", "laq_paged_attention_e4m3",
+           "laq_adjust_logits_f16")
 HEAD_DIM = 128
 
 
@@ -48,6 +49,10 @@ class LinearCall(ctypes.Structure):
 
 # laq_paged_batch of include/laq.h: five pointers, then nine int64.
 _PAGED_BATCH = struct.Struct("5P9q")
+# laq_logits_adjust: the history with its lengths and sizes, three settings, the
+# biases, the mask.
+_LOGITS_ADJUST = struct.Struct("3P2q3P2P2qPq")
+MAX_BIASES = 2047  # LAQ_MAX_BIASES
 
 
 _lib = None
@@ -137,6 +142,12 @@ def lib():
         L.laq_paged_attention_f16.restype = ctypes.c_int32
         L.laq_sample_f16.argtypes = [P, I64, I64, I64, P, P, P, P, P, P, P, P]
         L.laq_sample_f16.restype = ctypes.c_int32
+        L.laq_paged_append_e4m3.argtypes = [P, P, P, P, I64, P, P, P, I64, I64, I64, I64, F32, P, P]
+        L.laq_paged_append_e4m3.restype = ctypes.c_int32
+        L.laq_paged_attention_e4m3.argtypes = [P, P, P, P, I64, I64, I64, I64, P, P, I64, P]
+        L.laq_paged_attention_e4m3.restype = ctypes.c_int32
+        L.laq_adjust_logits_f16.argtypes = [P, P, I64, I64, I64, P, I64, P]
+        L.laq_adjust_logits_f16.restype = ctypes.c_int32
         _lib = L
     return _lib
 
@@ -543,13 +554,14 @@ def silu_mul(gate_up, out=None):
 # append of 16 rows 8.5 -> 7.5 us a call, attention of one token 11.4 -> 10.3.)
 class _Torch:
     """torch's names that a call needs, filled in at the first one."""
-    f16 = f32 = i32 = u8 = empty = zeros = current = stream = guard = None
+    f16 = f32 = i32 = u8 = e4m3 = e8m0 = empty = zeros = current = stream = guard = None
 
 
 def _torch():
     if _Torch.f16 is None:
         import torch
         _Torch.f32, _Torch.i32, _Torch.u8 = torch.float32, torch.int32, torch.uint8
+        _Torch.e4m3, _Torch.e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
         _Torch.empty, _Torch.zeros = torch.empty, torch.zeros
         _Torch.current, _Torch.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _Torch.guard = torch.cuda.device
@@ -570,12 +582,12 @@ def _launch(dev, fn, *args):
         _check(status)
 
 
-def _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T):
+def _paged_batch(dev, dtype, k_pages, v_pages, page_table, token_start, seq_len, T):
     """(laq_paged_batch, Hkv, B, positions a table row holds) of tensors on device number `dev`."""
     t = _Torch
     num_pages, Hkv, page_size, d = shape = k_pages.shape
     strides = k_pages.stride()
-    assert d == HEAD_DIM and k_pages.dtype is t.f16 and v_pages.dtype is t.f16
+    assert d == HEAD_DIM and k_pages.dtype is dtype and v_pages.dtype is dtype
     assert v_pages.shape == shape
     # (a dimension of one element has any stride, here and below)
     v_strides = v_pages.stride()
@@ -598,23 +610,10 @@ def _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T):
                              table_stride if B > 1 else pages, B, T), Hkv, B, pages * page_size
 
 
-def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, page_table, token_start, seq_len, Hq,
-                 eps, q_out=None):
-    """qk_norm_rope for the rows of several sequences with paged caches: fp16
-    qkv [T][(Hq + 2 Hkv) * 128] (rows may be strided) -> normalized, rotated q
-    (returned, fp16 [T][Hq][128]); k and v written to the rows' places.
-
-    k_pages / v_pages fp16 [num_pages][Hkv][page_size][128], of any strides
-    with contiguous rows of 128 (a transposed [num_pages][page_size][Hkv][128]
-    for instance); page_table int32 [B][pages], token_start int32 [B + 1],
-    seq_len int32 [B] (the new rows included), as laq_paged_batch of
-    include/laq.h describes them.  q_norm_weight / k_norm_weight fp16 [128] or
-    None.  cos_sin fp32 [positions][128] (decode.rope_table)."""
-    t = _torch()
-    dev = qkv.get_device()
+def _append_args(dev, t, qkv, q_norm_weight, k_norm_weight, cos_sin, Hq, Hkv, q_out):
+    """(q_out, row stride, weights' pointers, positions) of an append's tensors, checked."""
     T, width = qkv.shape
     row_stride, one = qkv.stride()
-    batch, Hkv, _, _ = _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T)
     assert qkv.dtype is t.f16 and one == 1 and width == (Hq + 2 * Hkv) * HEAD_DIM
     positions, d = cos_sin.shape
     assert cos_sin.dtype is t.f32 and d == HEAD_DIM and cos_sin.is_contiguous() and cos_sin.get_device() == dev
@@ -629,7 +628,53 @@ def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, p
     else:
         assert q_out.dtype is t.f16 and q_out.shape == (T, Hq, HEAD_DIM) and q_out.is_contiguous()
         assert q_out.get_device() == dev
-    _launch(dev, lib().laq_paged_append_f16, batch, qkv.data_ptr(), row_stride if T > 1 else width, norms[0], norms[1],
+    return q_out, row_stride if T > 1 else width, norms, positions
+
+
+def paged_append(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, page_table, token_start, seq_len, Hq,
+                 eps, q_out=None):
+    """qk_norm_rope for the rows of several sequences with paged caches: fp16
+    qkv [T][(Hq + 2 Hkv) * 128] (rows may be strided) -> normalized, rotated q
+    (returned, fp16 [T][Hq][128]); k and v written to the rows' places.
+
+    k_pages / v_pages fp16 [num_pages][Hkv][page_size][128], of any strides
+    with contiguous rows of 128 (a transposed [num_pages][page_size][Hkv][128]
+    for instance); page_table int32 [B][pages], token_start int32 [B + 1],
+    seq_len int32 [B] (the new rows included), as laq_paged_batch of
+    include/laq.h describes them.  q_norm_weight / k_norm_weight fp16 [128] or
+    None.  cos_sin fp32 [positions][128] (decode.rope_table)."""
+    t = _torch()
+    dev = qkv.get_device()
+    batch, Hkv, _, _ = _paged_batch(dev, t.f16, k_pages, v_pages, page_table, token_start, seq_len, qkv.shape[0])
+    q_out, stride, norms, positions = _append_args(dev, t, qkv, q_norm_weight, k_norm_weight, cos_sin, Hq, Hkv, q_out)
+    _launch(dev, lib().laq_paged_append_f16, batch, qkv.data_ptr(), stride, norms[0], norms[1], cos_sin.data_ptr(),
+            positions, Hq, Hkv, HEAD_DIM, eps, q_out.data_ptr())
+    return q_out
+
+
+def _scales(dev, t, pages, k_scales, v_scales):
+    """Pointers of a cache's scales, checked against its pages."""
+    num_pages, Hkv, page_size, _ = pages.shape
+    shape = (num_pages, Hkv, page_size // 16)
+    for x in (k_scales, v_scales):
+        assert x.dtype is t.e8m0 and x.shape == shape and x.is_contiguous() and x.get_device() == dev
+    return k_scales.data_ptr(), v_scales.data_ptr()
+
+
+def paged_append_e4m3(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pages, k_scales, v_scales, page_table,
+                      token_start, seq_len, Hq, eps, q_out=None):
+    """paged_append into caches of 8 bits: k_pages / v_pages float8_e4m3fn
+    [num_pages][Hkv][page_size][128] (strides as there, multiples of 16) and
+    k_scales / v_scales float8_e8m0fnu [num_pages][Hkv][page_size / 16],
+    contiguous: 16 consecutive positions of a head share a power of two, which
+    grows where their values need it (laq_paged_append_e4m3 of include/laq.h).
+    Returns q, the same as paged_append's."""
+    t = _torch()
+    dev = qkv.get_device()
+    batch, Hkv, _, _ = _paged_batch(dev, t.e4m3, k_pages, v_pages, page_table, token_start, seq_len, qkv.shape[0])
+    ks, vs = _scales(dev, t, k_pages, k_scales, v_scales)
+    q_out, stride, norms, positions = _append_args(dev, t, qkv, q_norm_weight, k_norm_weight, cos_sin, Hq, Hkv, q_out)
+    _launch(dev, lib().laq_paged_append_e4m3, batch, ks, vs, qkv.data_ptr(), stride, norms[0], norms[1],
             cos_sin.data_ptr(), positions, Hq, Hkv, HEAD_DIM, eps, q_out.data_ptr())
     return q_out
 
@@ -641,18 +686,12 @@ def paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity):
     return int(lib().laq_paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity))
 
 
-def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, window=0, out=None, workspace=None):
-    """Causal attention of the rows of several sequences over their paged
-    caches (after paged_append): fp16 q [T][Hq][128] -> fp16 [T][Hq][128].
-    window > 0: a row sees its own and the window - 1 positions before it.
-    The cache and the batch as for paged_append.  workspace: uint8, at least
-    paged_attention_workspace_bytes; taken from torch's allocator on the
-    current stream when not given."""
-    t = _torch()
-    dev = q.get_device()
-    T, Hq, d = shape = q.shape
+def _attention_args(dev, t, q, batch, out, workspace):
+    """(out, workspace, its bytes) of an attention's tensors, checked, made where not given."""
+    _, Hkv, B, capacity = batch
+    shape = q.shape
+    T, Hq, d = shape
     assert q.dtype is t.f16 and d == HEAD_DIM and q.is_contiguous()
-    batch, Hkv, B, capacity = _paged_batch(dev, k_pages, v_pages, page_table, token_start, seq_len, T)
     if out is None:
         out = t.zeros(shape, dtype=t.f16, device=q.device)
     else:
@@ -664,8 +703,96 @@ def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, windo
     else:
         assert workspace.get_device() == dev and workspace.is_contiguous()
         nbytes = workspace.numel() * workspace.element_size()
-    _launch(dev, lib().laq_paged_attention_f16, batch, q.data_ptr(), Hq, Hkv, HEAD_DIM, window, out.data_ptr(),
-            None if workspace is None else workspace.data_ptr(), nbytes)
+    return out, workspace, nbytes
+
+
+def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, window=0, out=None, workspace=None):
+    """Causal attention of the rows of several sequences over their paged
+    caches (after paged_append): fp16 q [T][Hq][128] -> fp16 [T][Hq][128].
+    window > 0: a row sees its own and the window - 1 positions before it.
+    The cache and the batch as for paged_append.  workspace: uint8, at least
+    paged_attention_workspace_bytes; taken from torch's allocator on the
+    current stream when not given."""
+    t = _torch()
+    dev = q.get_device()
+    batch = _paged_batch(dev, t.f16, k_pages, v_pages, page_table, token_start, seq_len, q.shape[0])
+    out, workspace, nbytes = _attention_args(dev, t, q, batch, out, workspace)
+    _launch(dev, lib().laq_paged_attention_f16, batch[0], q.data_ptr(), q.shape[1], batch[1], HEAD_DIM, window,
+            out.data_ptr(), None if workspace is None else workspace.data_ptr(), nbytes)
+    return out
+
+
+def paged_attention_e4m3(q, k_pages, v_pages, k_scales, v_scales, page_table, token_start, seq_len, window=0, out=None,
+                         workspace=None):
+    """paged_attention over caches of 8 bits (after paged_append_e4m3, which
+    describes them)."""
+    t = _torch()
+    dev = q.get_device()
+    batch = _paged_batch(dev, t.e4m3, k_pages, v_pages, page_table, token_start, seq_len, q.shape[0])
+    ks, vs = _scales(dev, t, k_pages, k_scales, v_scales)
+    out, workspace, nbytes = _attention_args(dev, t, q, batch, out, workspace)
+    _launch(dev, lib().laq_paged_attention_e4m3, batch[0], ks, vs, q.data_ptr(), q.shape[1], batch[1], HEAD_DIM, window,
+            out.data_ptr(), None if workspace is None else workspace.data_ptr(), nbytes)
+    return out
+
+
+def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None,
+                  presence=None, bias_token=None, bias_value=None, mask=None, out=None):
+    """Penalties, biases and a mask on fp16 logits [rows][V] (rows may be
+    strided) before `sample`; returns out (fp16 [rows][V], new when not given;
+    logits itself: in place).  laq_adjust_logits_f16 of include/laq.h defines it.
+
+    history int32 [rows][room] (rows may be strided or one expanded): the tokens
+    so far, of which history_len int32 [rows] are there and the first prompt_len
+    int32 [rows] (None: none) the prompt's.  repetition, frequency, presence
+    fp32 [rows] or None.  bias_token int32 and bias_value fp32 [rows][n]: added
+    to listed tokens (-1: none).  mask int32 [rows][(V + 31) // 32]: bit v % 32
+    of word v // 32 is set for tokens that may be drawn (one row may be expanded
+    to all)."""
+    t = _torch()
+    dev = logits.get_device()
+    rows, V = logits.shape
+    stride, one = logits.stride()
+    assert dev >= 0 and logits.dtype is t.f16 and (one == 1 or V == 1)
+    if out is None:
+        out = t.empty((rows, V), dtype=t.f16, device=logits.device)
+    else:
+        assert out.dtype is t.f16 and out.shape == (rows, V) and out.get_device() == dev
+    out_stride, one = out.stride()
+    assert one == 1 or V == 1
+
+    def rows_of(x, dtype, width=None):
+        """(pointer, stride between rows, width) of a tensor [rows][width]"""
+        n, w = x.shape
+        a, b = x.stride()
+        assert x.dtype is dtype and n == rows and (width is None or w == width) and (b == 1 or w == 1)
+        assert x.get_device() == dev
+        return x.data_ptr(), a if n > 1 else w, w
+    h = b = (0, 0, 0)
+    v = m = 0
+    if history is not None:
+        h = rows_of(history, t.i32)
+    else:
+        assert history_len is None and prompt_len is None
+    if bias_token is not None:
+        b = rows_of(bias_token, t.i32)
+        v, v_stride, _ = rows_of(bias_value, t.f32, b[2])
+        assert v_stride == b[1] or rows == 1
+    else:
+        assert bias_value is None
+    m_stride = 0
+    if mask is not None:
+        m, m_stride, _ = rows_of(mask, t.i32, (V + 31) // 32)
+    ptr = []
+    for x, dtype in ((history_len, t.i32), (prompt_len, t.i32), (repetition, t.f32), (frequency, t.f32), (presence, t.f32)):
+        if x is not None:
+            assert x.dtype is dtype and x.numel() == rows and x.is_contiguous() and x.get_device() == dev
+            ptr.append(x.data_ptr())
+        else:
+            ptr.append(0)
+    adjust = _LOGITS_ADJUST.pack(h[0], ptr[0], ptr[1], h[1], h[2], ptr[2], ptr[3], ptr[4], b[0], v, b[1], b[2], m, m_stride)
+    _launch(dev, lib().laq_adjust_logits_f16, adjust, logits.data_ptr(), stride if rows > 1 else V, rows, V,
+            out.data_ptr(), out_stride if rows > 1 else V)
     return out
 
 

@@ -1,7 +1,8 @@
 // Driver for a sanitizer build (AddressSanitizer + UndefinedBehaviorSanitizer
 // on the host code) of the entry points that abi_sanitize.cpp does not call: the
 // batched serving ones (paged append, paged attention and its workspace size,
-// sampling), the linears that update the residual stream, and the MLP block.
+// sampling; their forms over caches of 8 bits; the logits' adjustment), the
+// linears that update the residual stream, and the MLP block.
 // Arguments that their host-side validation must reject, sizes at and past every
 // limit and extreme integers among them, checking the returned status and the
 // last-error text; and the workspace sizes over grids of sizes, valid and not.
@@ -237,6 +238,93 @@ int main() {
   EXPECT(laq_sample_f16(P, 1000, 4, 1000, off(F, 2), F, I, F, F, I, F, nullptr), LAQ_ERR_MISALIGNED, fn);
   EXPECT(laq_sample_f16(P, 1000, 4, 1000, F, F, off(I, 1), F, F, I, F, nullptr), LAQ_ERR_MISALIGNED, fn);
   EXPECT(laq_sample_f16(P, 1000, 4, 1000, F, F, I, F, F, I, off(F, 3), nullptr), LAQ_ERR_MISALIGNED, fn);
+
+  // caches of 8 bits: what the fp16 calls check, strides of whole 16 bytes, and the scales
+  uint8_t* const S = static_cast<uint8_t*>(P);
+  auto append8 = [&](const laq_paged_batch* b, uint8_t* ks, uint8_t* vs, int64_t Hq = 32, int64_t Hkv = 8,
+                     int64_t stride = (int64_t)1 << 40) {
+    return laq_paged_append_e4m3(b, ks, vs, P, stride, P, P, F, 100, Hq, Hkv, 128, 1e-6f, P, nullptr);
+  };
+  auto attention8 = [&](const laq_paged_batch* b, const uint8_t* ks, const uint8_t* vs, int64_t Hq = 32, int64_t Hkv = 8,
+                        int64_t window = 0, int64_t bytes = (int64_t)1 << 40) {
+    return laq_paged_attention_e4m3(b, ks, vs, P, Hq, Hkv, 128, window, P, P, bytes, nullptr);
+  };
+  for (int64_t v : {kMin, (int64_t)-1, (int64_t)0, (int64_t)8, (int64_t)24, (int64_t)130, kMax}) {
+    const auto each = [&](int64_t laq_paged_batch::*m, laq_status want) {
+      laq_paged_batch b = batch();
+      b.*m = v;
+      EXPECT(append8(&b, S, S), want, "laq_paged_append_e4m3");
+      EXPECT(attention8(&b, S, S), want, "laq_paged_attention_e4m3");
+    };
+    each(&laq_paged_batch::page_size, LAQ_ERR_BAD_SHAPE);
+    each(&laq_paged_batch::slot_stride, v == 130 ? LAQ_ERR_MISALIGNED : LAQ_ERR_BAD_SHAPE);
+    each(&laq_paged_batch::head_stride, v == 130 ? LAQ_ERR_MISALIGNED : LAQ_ERR_BAD_SHAPE);
+    each(&laq_paged_batch::page_stride, v == 130 ? LAQ_ERR_MISALIGNED : LAQ_ERR_BAD_SHAPE);
+    if (v == 8 || v == 24) continue;
+    EXPECT(append8(&good, S, S, v, 8), LAQ_ERR_BAD_SHAPE, "laq_paged_append_e4m3");
+    EXPECT(attention8(&good, S, S, v, 8), LAQ_ERR_BAD_SHAPE, "laq_paged_attention_e4m3");
+  }
+  EXPECT(append8(nullptr, S, S), LAQ_ERR_NULL_POINTER, "laq_paged_append_e4m3");
+  EXPECT(append8(&good, nullptr, S), LAQ_ERR_NULL_POINTER, "laq_paged_append_e4m3");
+  EXPECT(append8(&good, S, nullptr), LAQ_ERR_NULL_POINTER, "laq_paged_append_e4m3");
+  EXPECT(attention8(nullptr, S, S), LAQ_ERR_NULL_POINTER, "laq_paged_attention_e4m3");
+  EXPECT(attention8(&good, nullptr, S), LAQ_ERR_NULL_POINTER, "laq_paged_attention_e4m3");
+  EXPECT(attention8(&good, S, nullptr), LAQ_ERR_NULL_POINTER, "laq_paged_attention_e4m3");
+  for (int64_t v : {kMin, (int64_t)-1, ((int64_t)1 << 30) + 1, kMax})
+    EXPECT(attention8(&good, S, S, 32, 8, v), LAQ_ERR_BAD_SHAPE, "laq_paged_attention_e4m3");
+  for (int64_t v : {kMin, (int64_t)-1, (int64_t)0})
+    EXPECT(attention8(&good, S, S, 32, 8, 0, v), LAQ_ERR_BAD_SHAPE, "laq_paged_attention_e4m3");
+  {
+    laq_paged_batch b = batch();
+    b.T = (int64_t)1 << 18;  // 2^14 windows of 2 x 4096 + 512 waves, 2^33 threads
+    EXPECT(append8(&b, S, S, 4096, 4096), LAQ_ERR_BAD_SHAPE, "laq_paged_append_e4m3");
+  }
+
+  fn = "laq_adjust_logits_f16";
+  const uint32_t* const M = static_cast<const uint32_t*>(P);
+  const laq_logits_adjust all = {I, I, I, 100, 100, F, F, F, I, F, 5, 5, M, 32};
+  void* const O = off(P, 1 << 24);
+  auto adjust = [&](const laq_logits_adjust* a, int64_t rows = 4, int64_t V = 1000, int64_t stride = 1000,
+                    int64_t out_stride = 1000, const void* x = P, void* y = nullptr) {
+    return laq_adjust_logits_f16(a, x, stride, rows, V, y ? y : O, out_stride, nullptr);
+  };
+  EXPECT(adjust(nullptr), LAQ_ERR_NULL_POINTER, fn);
+  EXPECT(adjust(&all, 4, 1000, 1000, 1000, nullptr), LAQ_ERR_NULL_POINTER, fn);
+  EXPECT(laq_adjust_logits_f16(&all, P, 1000, 4, 1000, nullptr, 1000, nullptr), LAQ_ERR_NULL_POINTER, fn);
+  for (int64_t v : {kMin, (int64_t)-1, (int64_t)1 << 22, kMax}) EXPECT(adjust(&all, v), LAQ_ERR_BAD_SHAPE, fn);
+  for (int64_t v : {kMin, (int64_t)-1, (int64_t)0, (int64_t)1001, (int64_t)(1 << 24) + 1, kMax})
+    EXPECT(adjust(&all, 4, v), LAQ_ERR_BAD_SHAPE, fn);
+  for (int64_t v : {kMin, (int64_t)-1, (int64_t)0, (int64_t)999, ((int64_t)1 << 32) + 1, kMax}) {
+    EXPECT(adjust(&all, 4, 1000, v), LAQ_ERR_BAD_SHAPE, fn);
+    EXPECT(adjust(&all, 4, 1000, 1000, v), LAQ_ERR_BAD_SHAPE, fn);
+  }
+  for (int64_t v : {kMin, (int64_t)-1, ((int64_t)1 << 32) + 1, kMax})
+    for (int64_t laq_logits_adjust::*m : {&laq_logits_adjust::history_stride, &laq_logits_adjust::history_room,
+                                          &laq_logits_adjust::bias_stride, &laq_logits_adjust::biases,
+                                          &laq_logits_adjust::mask_stride}) {
+      laq_logits_adjust a = all;
+      a.*m = v;
+      EXPECT(adjust(&a), LAQ_ERR_BAD_SHAPE, fn);
+    }
+  {
+    laq_logits_adjust a = all;
+    a.history_len = nullptr;
+    EXPECT(adjust(&a), LAQ_ERR_NULL_POINTER, fn);
+    a = all;
+    a.bias_value = nullptr;
+    EXPECT(adjust(&a), LAQ_ERR_NULL_POINTER, fn);
+    a = all;
+    a.mask = off(const_cast<uint32_t*>(M), 2);
+    EXPECT(adjust(&a), LAQ_ERR_MISALIGNED, fn);
+    a = all;
+    a.repetition = off(F, 1);
+    EXPECT(adjust(&a), LAQ_ERR_MISALIGNED, fn);
+  }
+  EXPECT(adjust(&all, 4, 1000, 1000, 1000, off(P, 1)), LAQ_ERR_MISALIGNED, fn);
+  EXPECT(adjust(&all, 4, 1000, 1000, 1000, P, off(P, 1 << 12)), LAQ_ERR_BAD_SHAPE, fn);
+  EXPECT(adjust(&all, 4, 1000, 1000, 1001, P, P), LAQ_ERR_BAD_SHAPE, fn);
+  EXPECT(adjust(&all, (1 << 22) - 1, 1 << 24, (int64_t)1 << 32, (int64_t)1 << 32, P,
+                reinterpret_cast<void*>((uintptr_t)1 << 62)), LAQ_ERR_BAD_SHAPE, fn);
 
   if (g_bad) {
     std::printf("%d of %d checks failed\n", g_bad, g_checks);
