@@ -632,9 +632,8 @@ laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, 
  * Scales are 112..134 (2^-15 to 2^7, with which every value is an fp16 number);
  * bytes outside are taken as the nearer of the two. */
 
-/* laq_paged_append_e4m3 -- laq_paged_append_f16 into a cache of 8 bits: the
- * same q_out, bit for bit; keys (normalized and rotated, in fp32) and values
- * become codes.  For every block of 16 positions that gets new rows, and each
+/* laq_paged_append_e4m3 -- laq_paged_append_f16 into a cache of 8 bits: q_out as
+ * there; keys (normalized and rotated, in fp32) and values become codes.  For every block of 16 positions that gets new rows, and each
  * of keys and values of a head:
  *   scale = the least of 112..134 with max |x| <= 448 * 2^(scale - 127), x the
  *           block's new values that are finite; not below the scale that the
@@ -701,10 +700,10 @@ typedef struct laq_logits_adjust {
 
 /* laq_adjust_logits_f16 -- logits fp16 [rows][V] before sampling.  Of token v's
  * logit x, with c the times that the row's generated tokens name v:
- *   x = x > 0 ? x / repetition[r] : x * repetition[r]   if history names v
- *   x = x - frequency[r] * c - presence[r]              if c > 0
- *   x = x + bias                                        if v is listed
- *   x = -inf                                            if v is not allowed
+ *   x = x * (x > 0 ? 1 / repetition[r] : repetition[r])   if history names v
+ *   x = x - frequency[r] * c - presence[r]                if c > 0
+ *   x = x + bias                                          if v is listed
+ *   x = -inf                                              if v is not allowed
  * in fp32 (each step rounded by itself), rounded to fp16 once.  Logits that
  * none of this touches are copied as they are.  Settings are not checked: what
  * the formulas give is what is written.

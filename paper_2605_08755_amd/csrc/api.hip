@@ -800,7 +800,7 @@ laq_status laq_adjust_logits_f16(const laq_logits_adjust* adjust, const void* lo
     d.bias_stride = a.bias_stride;
     d.biases = (int)a.biases;
   }
-  d.mask = reinterpret_cast<const int*>(a.mask);
+  d.mask = a.mask;
   d.mask_stride = a.mask_stride;
   d.V = (int)V;
   d.in_place = same;

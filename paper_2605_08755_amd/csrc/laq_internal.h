@@ -306,7 +306,7 @@ struct Adjust {
   const int* bias_token;  // null: none
   const float* bias_value;
   int64_t bias_stride;
-  const int* mask;
+  const uint32_t* mask;
   int64_t mask_stride;
   int V, room, biases;  // tokens; of a row's history; biases of a row
   bool in_place;

@@ -41,9 +41,19 @@ struct Part {
   float u[8], v[8];
 };
 
-// Normalized (w: not null) and rotated by the row of cosines and sines at cs.
-__device__ __forceinline__ void norm_rope(Part& p, const uint16_t* __restrict__ w, const float* __restrict__ cs, int i,
-                                          float eps) {
+// Their rotation: a row of cosines and sines.
+struct Turn {
+  float c[8], s[8];
+};
+__device__ __forceinline__ Turn turn_of(const float* __restrict__ cs, int i) {
+  Turn t;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t.c[e] = cs[8 * i + e], t.s[e] = cs[64 + 8 * i + e];
+  return t;
+}
+
+// Normalized (w: not null) and rotated.
+__device__ __forceinline__ void norm_rope(Part& p, const uint16_t* __restrict__ w, const Turn& t, int i, float eps) {
   float ss = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) ss = fmaf(p.u[e], p.u[e], fmaf(p.v[e], p.v[e], ss));
@@ -57,14 +67,19 @@ __device__ __forceinline__ void norm_rope(Part& p, const uint16_t* __restrict__ 
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float c = cs[8 * i + e], s = cs[64 + 8 * i + e];
-    const float u = p.u[e] * c - p.v[e] * s, v = p.v[e] * c + p.u[e] * s;
+    const float u = p.u[e] * t.c[e] - p.v[e] * t.s[e], v = p.v[e] * t.c[e] + p.u[e] * t.s[e];
     p.u[e] = u, p.v[e] = v;
   }
 }
 
-__device__ __forceinline__ Part part_of(const uint16_t* head, int i) {
-  const half8_t a = *reinterpret_cast<const half8_t*>(head + 8 * i), b = *reinterpret_cast<const half8_t*>(head + 64 + 8 * i);
+struct Raw {
+  u32x4 a, b;
+};
+__device__ __forceinline__ Raw raw_of(const uint16_t* head, int i) {
+  return Raw{*reinterpret_cast<const u32x4*>(head + 8 * i), *reinterpret_cast<const u32x4*>(head + 64 + 8 * i)};
+}
+__device__ __forceinline__ Part part_of(const Raw& r) {
+  const half8_t a = __builtin_bit_cast(half8_t, r.a), b = __builtin_bit_cast(half8_t, r.b);
   Part p;
 #pragma unroll
   for (int e = 0; e < 8; ++e) p.u[e] = (float)a[e], p.v[e] = (float)b[e];
@@ -105,63 +120,67 @@ __device__ __forceinline__ float wave_max(float v) {
   return fmaxf(fmaxf(f(readlane(u, 0)), f(readlane(u, 16))), fmaxf(f(readlane(u, 32)), f(readlane(u, 48))));
 }
 
-// A wave takes a window of `window` rows and either every q_waves-th group of
-// eight query heads, or the keys or the values of one key/value head: of these
-// the blocks of 16 positions whose first new row lies in the window (all of a
-// block's new rows are one sequence's, so one wave sees the whole block and the
-// scale needs no exchange between waves).  Eight lanes a row: lane i holds
-// dimensions 8i .. 8i + 7 and their partners.  What bounds it: the bytes of the
-// rows in and out where there are many; few rows are a launch and the chain of
-// dependent reads: sequence, page, the block's old scale.
+// A wave takes either the keys or the values of one key/value head in a window
+// of `window` rows: the blocks of 16 positions whose first new row lies in the
+// window (all of a block's new rows are one sequence's, so one wave sees the
+// whole block and the scale needs no exchange between waves); or one row and
+// every q_waves-th group of eight query heads.  Eight lanes a row or head: lane i
+// holds dimensions 8i .. 8i + 7 and their partners.  What bounds it: the bytes of
+// the rows in and out where there are many; few rows are a launch and the chain
+// of dependent reads: sequence, page, the block's old scale.
 __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedCodes pb, const uint16_t* __restrict__ qkv,
                                                                  int64_t qkv_stride, const uint16_t* __restrict__ qw,
                                                                  const uint16_t* __restrict__ kw,
                                                                  const float* __restrict__ cos_sin, int rope_rows,
                                                                  int Hq, int Hkv, float eps,
-                                                                 uint16_t* __restrict__ q_out, int window, int q_waves) {
+                                                                 uint16_t* __restrict__ q_out, int window, int q_waves,
+                                                                 uint32_t kv_waves) {
   const int lane = threadIdx.x & 63;
-  const int units = 2 * Hkv + q_waves;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
-  const int64_t at_window = wave / units;
-  const int unit = uniform((int)(wave - at_window * units));
-  if (at_window * window >= pb.T) return;
-  const int first = uniform((int)(at_window * window));
-  const int end = min(first + window, pb.T);
+  const uint32_t wave = blockIdx.x * 4 + (uint32_t)uniform(threadIdx.x >> 6);
   const int i = lane & 7;
   const int64_t cap = (int64_t)pb.table_pages << pb.page_shift;
   const int most = (int)min(cap, (int64_t)rope_rows);  // positions from here on have no place or no rotation
-  int seq = sequence_of(pb, 0, first, lane);
 
-  if (unit >= 2 * Hkv) {
+  if (wave >= kv_waves) {
+    const int row = uniform((int)((wave - kv_waves) / (uint32_t)q_waves));
+    const int at = uniform((int)(wave - kv_waves - (uint32_t)row * (uint32_t)q_waves));
+    if (row >= pb.T) return;
     const int groups = (Hq + 7) >> 3;
-    int s1 = -1, s0 = 0, len = 0;
-    for (int row = first; row < end; ++row) {
-      if (row >= s1) {
-        if (s1 >= 0) seq = sequence_of(pb, seq, row, lane);
-        if (seq >= pb.B) return;  // behind the last sequence
-        s0 = pb.token_start[seq], s1 = min(pb.token_start[seq + 1], pb.T), len = pb.seq_len[seq];
-      }
-      if (row < s0) continue;  // before the first
-      const int64_t pos = (int64_t)len - s1 + row;
-      const bool placed = pos >= 0 && pos < most;
-      const float* const cs = cos_sin + (placed ? pos : 0) * kHeadDim;
-      for (int grp = unit - 2 * Hkv; grp < groups; grp += q_waves) {
-        const int h = grp * 8 + (lane >> 3);
-        if (h >= Hq) break;
-        Part p = part_of(qkv + row * qkv_stride + (int64_t)h * kHeadDim, i);
-        norm_rope(p, qw, cs, i, eps);
-        half8_t x, y;
+    const uint16_t* const src = qkv + row * qkv_stride;
+    auto load = [&](int grp) { return raw_of(src + (int64_t)min(grp * 8 + (lane >> 3), Hq - 1) * kHeadDim, i); };
+    Raw raw = load(at);
+    const int seq = sequence_of(pb, 0, row, lane);
+    if (seq >= pb.B) return;  // behind the last sequence
+    const int s0 = pb.token_start[seq], s1 = min(pb.token_start[seq + 1], pb.T);
+    if (row < s0) return;  // before the first
+    const int64_t pos = (int64_t)pb.seq_len[seq] - s1 + row;
+    const bool placed = pos >= 0 && pos < most;
+    const Turn turn = turn_of(cos_sin + (placed ? pos : 0) * kHeadDim, i);
+    for (int grp = at; grp < groups;) {
+      const int h = grp * 8 + (lane >> 3);
+      Part p = part_of(raw);
+      const int next = grp + q_waves;
+      if (next < groups) raw = load(next);
+      norm_rope(p, qw, turn, i, eps);
+      half8_t x, y;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (_Float16)p.u[e], y[e] = (_Float16)p.v[e];
-        if (!placed) x = half8_t{}, y = half8_t{};
+      for (int e = 0; e < 8; ++e) x[e] = (_Float16)p.u[e], y[e] = (_Float16)p.v[e];
+      if (!placed) x = half8_t{}, y = half8_t{};
+      if (h < Hq) {
         uint16_t* d = q_out + ((int64_t)row * Hq + h) * kHeadDim + 8 * i;
         *reinterpret_cast<half8_t*>(d) = x;
         *reinterpret_cast<half8_t*>(d + 64) = y;
       }
+      grp = next;
     }
     return;
   }
 
+  const int at_window = uniform((int)(wave / (uint32_t)(2 * Hkv)));
+  const int unit = uniform((int)(wave - (uint32_t)at_window * (uint32_t)(2 * Hkv)));
+  const int first = at_window * window;
+  const int end = min(first + window, pb.T);
+  int seq = sequence_of(pb, 0, first, lane);
   const int g = unit >> 1;
   const bool values = unit & 1;
   const uint16_t* const src = qkv + (int64_t)(Hq + (values ? Hkv : 0) + g) * kHeadDim;
@@ -203,8 +222,8 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedCodes pb, 
     for (int k = 0; k < 2; ++k) {
       if (8 * k >= n) break;
       const int r = min(8 * k + (lane >> 3), n - 1);
-      p[k] = part_of(src + (int64_t)(row + r) * qkv_stride, i);
-      if (!values) norm_rope(p[k], kw, cos_sin + (int64_t)(pos + r) * kHeadDim, i, eps);
+      p[k] = part_of(raw_of(src + (int64_t)(row + r) * qkv_stride, i));
+      if (!values) norm_rope(p[k], kw, turn_of(cos_sin + (int64_t)(pos + r) * kHeadDim, i), i, eps);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float x = fabsf(p[k].u[e]), y = fabsf(p[k].v[e]);
@@ -589,18 +608,25 @@ __device__ __forceinline__ void CacheE4M3::rows16_item(const PagedCodes& pb, con
   }
 }
 
-// Rows of a window of the append, and waves of its query heads: 16 rows where
-// windows of one would be more waves than run at once, then a wave for all
-// heads of a row where that still fills the chip.
+// Rows of a window of the append: the least power of two up to a block's 16 with
+// which the windows' waves run at once (a wave whose rows continue a block costs
+// its search; one whose rows begin many blocks takes them one after another).
+// Waves of a row's query heads: one where rows alone fill the chip, else one per
+// group of eight.  (Measured on MI355X, kernel alone, windows of 1 / 2 / 4 / 8 /
+// 16 rows: 16 decoding rows, 32:8 heads, 4.3 / 6.1 / 9.9 / 17.5 / 32 us; 1617
+// rows of nine sequences, 28:4, 13.6 / 10.7 / 11.0 / 14.4 / 13.9; 16384 of four,
+// 32:8, 225 / 221 / 132 / 98 / 79, of which 72 are the bytes as a large copy
+// moves them.)
 struct AppendShape {
-  int64_t window, q_waves, waves;
+  int64_t window, q_waves, kv_waves, waves;
 };
 AppendShape append_shape(int64_t T, int64_t Hq, int64_t Hkv) {
-  const int64_t groups = (Hq + 7) / 8;
   AppendShape s;
-  s.window = T * (2 * Hkv + groups) > kResidentWaves ? kBlock : 1;
-  s.q_waves = groups;
-  s.waves = (T + s.window - 1) / s.window * (2 * Hkv + s.q_waves);
+  s.window = 1;
+  while (s.window < kBlock && (T + s.window - 1) / s.window * 2 * Hkv > kResidentWaves) s.window *= 2;
+  s.q_waves = std::max<int64_t>(1, std::min<int64_t>((Hq + 7) / 8, kResidentWaves / T));
+  s.kv_waves = (T + s.window - 1) / s.window * 2 * Hkv;
+  s.waves = s.kv_waves + T * s.q_waves;
   return s;
 }
 
@@ -617,7 +643,7 @@ hipError_t launch_paged_append_codes(const PagedCodes& pb, const uint16_t* qkv, 
   const AppendShape s = append_shape(pb.T, Hq, Hkv);
   launch(paged_append_codes_kernel, dim3((unsigned)((s.waves + 3) / 4)), dim3(256), 0, stream, ev, pb, qkv, qkv_stride, qw,
          kw, cos_sin, (int)std::min<int64_t>(rope_rows, 0x7FFFFFFF), (int)Hq, (int)Hkv, eps, q_out, (int)s.window,
-         (int)s.q_waves);
+         (int)s.q_waves, (uint32_t)s.kv_waves);
   return hipGetLastError();
 }
 

@@ -668,7 +668,7 @@ def paged_append_e4m3(qkv, q_norm_weight, k_norm_weight, cos_sin, k_pages, v_pag
     k_scales / v_scales float8_e8m0fnu [num_pages][Hkv][page_size / 16],
     contiguous: 16 consecutive positions of a head share a power of two, which
     grows where their values need it (laq_paged_append_e4m3 of include/laq.h).
-    Returns q, the same as paged_append's."""
+    Returns q as paged_append does."""
     t = _torch()
     dev = qkv.get_device()
     batch, Hkv, _, _ = _paged_batch(dev, t.e4m3, k_pages, v_pages, page_table, token_start, seq_len, qkv.shape[0])
