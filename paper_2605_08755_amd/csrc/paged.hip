@@ -170,6 +170,7 @@ __device__ __forceinline__ void lds_put(uint32_t addr, float v) {
 struct CacheF16 {
   typedef PagedBatch Batch;
   static constexpr int kBytes = 2;
+  static int split_from(int64_t, int64_t) { return 0; }
   template <int WAVES>
   static constexpr int kItemLds = WAVES * (2 * kKeyBytes + 16 * kRowBytes);
   template <int WAVES, int REC>

@@ -153,6 +153,14 @@ __device__ __forceinline__ Seq load_seq(const PagedBatch& pb, int b, int R, int 
   return q;
 }
 
+// Results of one item: rows of partial sums (split) or of outputs.  And the plan.
+struct Out {
+  uint16_t* out;
+  float* ws;
+  const int* plan;
+  int Hq, rec_bound, min_chunk;
+};
+
 struct Item {
   bool found;
   int b, s0, n, pos0, end, lo;
@@ -161,10 +169,10 @@ struct Item {
 };
 
 // The smallest chunk by that bound, of all sequences' tiles x units.
-template <int BM>
-__device__ __forceinline__ int least_chunk(double total, int Hkv) {
+// (min_chunk: that of the call, kMinChunk, or all units where nothing is split.)
+__device__ __forceinline__ int least_chunk(double total, int Hkv, int min_chunk) {
   const double share = total * Hkv * (1.0 / kItems);
-  return uniform(max((int)fmin(share, 33554432.0) + 1, kMinChunk<BM>));
+  return uniform(max((int)fmin(share, 33554432.0) + 1, min_chunk));
 }
 
 // Batches of more than 64 sequences have a plan in the workspace, which a kernel
@@ -180,7 +188,8 @@ __host__ __device__ constexpr int64_t plan_groups(int64_t B) { return B > kGroup
 constexpr int kPlanWaves = 16;
 template <int BM>
 __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(PagedBatch pb, int R, int Hkv,
-                                                                               int window, int* __restrict__ plan) {
+                                                                               int window, int min_chunk,
+                                                                               int* __restrict__ plan) {
   __shared__ double totals[kPlanWaves];
   __shared__ int sums[kPlanWaves][3];
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
@@ -194,7 +203,7 @@ __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(P
   __syncthreads();
   total = 0.0;
   for (int i = 0; i < kPlanWaves; ++i) total += totals[i];
-  const int chunk = least_chunk<BM>(total, Hkv);
+  const int chunk = least_chunk(total, Hkv, min_chunk);
   if (threadIdx.x == 0) plan[0] = chunk;
   int* const before = plan + 1;
   int upto[3] = {0, 0, 0};
@@ -218,8 +227,9 @@ __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(P
 
 // Item `idx` of a key/value head (SPLIT: the idx-th split tile).
 template <int BM, bool SPLIT>
-__device__ __forceinline__ Item find_item(const PagedBatch& pb, const int* __restrict__ plan, int idx, int R, int Hkv,
-                                          int window, int lane) {
+__device__ __forceinline__ Item find_item(const PagedBatch& pb, const Out& o, int idx, int R, int Hkv, int window,
+                                          int lane) {
+  const int* const plan = o.plan;
   Item it;
   it.found = false;
   int items = 0, recs = 0, b0 = 0;
@@ -246,7 +256,7 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, const int* __res
     q = load_seq<BM>(pb, lane, R, window);
     // That chunk, then up to 3/8 and one unit larger until the items are no more
     // than the blocks that run at once (a few more would run alone).
-    const int least = least_chunk<BM>(wave_sum_exact((double)q.tiles * q.units), Hkv);
+    const int least = least_chunk(wave_sum_exact((double)q.tiles * q.units), Hkv, o.min_chunk);
     it.chunk = least;
     for (int i = 0; i < 4; ++i) {
       const int c = least + least * i / 8 + (i > 0);
@@ -353,14 +363,6 @@ __device__ __forceinline__ uint32_t values23(uint32_t codes, float scale) {
 __device__ __forceinline__ uint32_t nan_codes(uint32_t x) { return ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan_codes(x) >> 7) * 0xFFu); }
 
-// Results of one item: rows of partial sums (split) or of outputs.  And the plan.
-struct Out {
-  uint16_t* out;
-  float* ws;
-  const int* plan;
-  int Hq, rec_bound;
-};
-
 // ---------------------------------------------------------------------------
 // attention of prompts' chunks: the matrix cores bound it
 // ---------------------------------------------------------------------------
@@ -403,7 +405,8 @@ struct Out {
 // Tiles of keys and values go memory -> registers -> LDS, two buffers, so that
 // a tile's loads are in flight while the one before is computed and a block
 // meets once per tile.  Piece p (16 bytes) of key row r sits at p ^ (r & 15)
-// and of value row r at p ^ 4 (r & 3): the operand reads touch each bank once.
+// and of value row r at p ^ 4 (r & 3) (codes, whose rows are stored two pieces a
+// lane: ^ (r & 1) too): reads and stores touch each bank once.
 constexpr int kTile = 64;
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 constexpr int kLargeThreads = 512;
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   const int w = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kLargeRows, false>(pb, o_.plan, at_item, R, Hkv, window, lane);
+  const Item it = find_item<kLargeRows, false>(pb, o_, at_item, R, Hkv, window, lane);
   if (!it.found) return;
   if (it.n * R <= kSmallRows) {
     C::template rows16_item<kLargeThreads / 64, kLargeRows>(pb, q, R, window, o_, it, g, lds);
@@ -560,7 +563,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
         if (nan_codes(r.x) | nan_codes(r.y) | nan_codes(r.z) | nan_codes(r.w)) flags[t & 3] = t;
         r = u32x4{number_codes(r.x), number_codes(r.y), number_codes(r.z), number_codes(r.w)};
       }
-      store_codes(d, r, scale_of(set_vs, old_vs, t), 4 * (sr & 3));
+      store_codes(d, r, scale_of(set_vs, old_vs, t), 4 * (sr & 3) ^ (sr & 1));
       return;
     }
     if (is_masked(t)) {
@@ -681,6 +684,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   // Value sums: 16 lanes read 4 positions x 16 dimensions and receive a column each.
   const int vrow = 4 * h + (lane & 15) / 4;
   const int vcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);  // dimension within 32
+  const int vswap = 4 * (vrow & 3) ^ (kCodes ? vrow & 1 : 0);
   auto value_sums = [&](const half8_t(&pf)[4], int B) {
     typedef short short4_t __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) short4_t lds_short4;
@@ -690,7 +694,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const int piece = (32 * d + vcol) >> 3;
-        const char* const a = vd + (16 * ks + vrow) * 256 + 16 * (piece ^ (4 * (vrow & 3))) + 2 * (vcol & 7);
+        const char* const a = vd + (16 * ks + vrow) * 256 + 16 * (piece ^ vswap) + 2 * (vcol & 7);
         const short4_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a));
         const short4_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a + 8 * 256));
         const half8_t v = __builtin_bit_cast(half8_t, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -800,8 +804,8 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
 
 // Joins the ranges of the split tiles in position order.  Records are weighted
 // by 2^(their maximum - the largest of all); a lane holds two dimensions.
-// WAVES == 4: a block per row, its waves take every fourth record and meet in
-// LDS (decoding: few rows, many ranges).  WAVES == 1: a wave per four rows,
+// WAVES == 4: a block takes a row at a time (every gridDim.y-th of its tile), its
+// waves every fourth record, and they meet in LDS (decoding: few rows, many ranges).  WAVES == 1: a wave per four rows,
 // 16 rows a block at a time (a chunk's rows have few ranges each).  Most blocks
 // of the grid can find nothing to do and cost their search, so there are about
 // kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
@@ -816,15 +820,15 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<BM, true>(pb, o_.plan, at_item, R, Hkv, window, lane);
+  const Item it = find_item<BM, true>(pb, o_, at_item, R, Hkv, window, lane);
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
   const int first = WAVES == 4 ? w : 0;
   const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
-  // WAVES == 4: a row, the same for the whole block; else every gridDim.y-th group of 16
+  // WAVES == 4: every gridDim.y-th row, the same for the whole block; else group of 16
 #pragma unroll 1
-  for (int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4; row < rows; row += 16 * gridDim.y) {
+  for (int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4; row < rows; row += (WAVES == 4 ? 1 : 16) * gridDim.y) {
     const float *stat[kRows], *sums[kRows];
     float2_t x[kRows][kB], st[kRows][kB], num[kRows];
     float M[kRows], den[kRows];
@@ -879,10 +883,11 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
     if constexpr (WAVES == 4) {
       part[w][lane] = num[0];
       __syncthreads();
-      if (w > 0) return;
       num[0] = part[0][lane];
 #pragma unroll
       for (int i = 1; i < 4; ++i) num[0] += part[i][lane];
+      __syncthreads();  // the next row's sums take their place
+      if (w > 0) continue;
     }
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
@@ -892,7 +897,6 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
       *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
           half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
     }
-    if constexpr (WAVES == 4) return;
   }
 }
 
@@ -902,16 +906,19 @@ struct AttentionPlan {
   int64_t items, split_tiles, records;  // per key/value head
   int64_t floats;                       // workspace: the records, then the plan
   int64_t plan_at;
+  int min_chunk;
 };
 
+// split_from: units a sequence must be able to have for any to be split.
 template <int BM>
-AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
+AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity, int split_from) {
   AttentionPlan p;
   p.large = BM == kLargeRows;
   const int64_t tiles = (T * R + std::min(B, T) * (BM - 1)) / BM;
   const int64_t per_head = (kItems + Hkv - 1) / Hkv;
   // (with kItems heads and more a head's share of the items is one: no sequence is split)
-  const bool split = capacity > (int64_t)kMinChunk<BM> * kUnit && Hkv < kItems;
+  const bool split = capacity > (int64_t)std::max(kMinChunk<BM>, split_from) * kUnit && Hkv < kItems;
+  p.min_chunk = split ? kMinChunk<BM> : std::max((int)((capacity + kUnit - 1) / kUnit), kMinChunk<BM>);
   p.items = tiles + (split ? per_head : 0);
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
@@ -929,9 +936,9 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
 // chunk of 193 rows, all at 500 or at 2000, 67 -> 82 and 161 -> 189; a chunk of 256
 // rows at 6000 beside 63 waiting sequences 180 -> 119, of 16 rows 30 -> 42; 64
 // decoding rows and 193 of padding 98 -> 97, 16 and 49 of padding 35 -> 38.)
-AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
-  if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity);
-  return plan_of<kLargeRows>(B, T, R, Hkv, capacity);
+AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity, int split_from = 0) {
+  if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity, split_from);
+  return plan_of<kLargeRows>(B, T, R, Hkv, capacity, split_from);
 }
 
 // Up to 16 rows per tile: an item a block.
@@ -942,7 +949,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
                                                                              int Hkv, int window, Out o_) {
   extern __shared__ u32x4 small_lds[];
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kSmallRows, false>(pb, o_.plan, at_item, R, Hkv, window, threadIdx.x & 63);
+  const Item it = find_item<kSmallRows, false>(pb, o_, at_item, R, Hkv, window, threadIdx.x & 63);
   if (!it.found) return;
   C::template rows16_item<kWaves, kSmallRows>(pb, q, R, window, o_, it, g, reinterpret_cast<char*>(small_lds));
 }
@@ -952,7 +959,8 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
                             uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev) {
   const PagedBatch& rows = pb;
   const int64_t R = Hq / Hkv;
-  const AttentionPlan p = attention_plan(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift);
+  const AttentionPlan p = attention_plan(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift,
+                                         C::split_from(pb.B, Hkv));
   LaunchEvents e0, e1 = ev, e2;
   if (p.split_tiles > 0) {  // the measurement hook spans all kernels
     e1.stop = nullptr;
@@ -963,16 +971,20 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
     e0.start = e1.start;
     e1.start = nullptr;
     auto* const kernel = p.large ? paged_attention_plan_kernel<kLargeRows> : paged_attention_plan_kernel<kSmallRows>;
-    launch(kernel, dim3(1), dim3(64 * kPlanWaves), 0, stream, e0, rows, (int)R, (int)Hkv, (int)window, plan);
+    launch(kernel, dim3(1), dim3(64 * kPlanWaves), 0, stream, e0, rows, (int)R, (int)Hkv, (int)window, p.min_chunk, plan);
   }
-  const Out o{out, ws, plan, (int)Hq, (int)p.records};
+  const Out o{out, ws, plan, (int)Hq, (int)p.records, p.min_chunk};
   const dim3 grid((unsigned)(p.items * Hkv));
   // A block joins one row; 16 rows where the tiles (most of them not split) would make many blocks.
   constexpr int64_t kFewTiles = 32, kJoinBlocks = 2048;
   const bool many = p.large && p.split_tiles * Hkv > kFewTiles;
   const int64_t most_rows = std::min<int64_t>(p.large ? kLargeRows : kSmallRows, pb.T * R);
   const int64_t by_16 = std::min((most_rows + 15) / 16, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
-  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_16 : most_rows));
+  // (A block per row where that is about as many as run at once, else fewer that
+  // go on: where nothing is split, each costs its search.  Measured on MI355X, 64
+  // sequences of 400 positions, 64:8 heads, e4m3 codes: 25 -> 19 us.)
+  const int64_t by_row = std::min(most_rows, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
+  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_16 : by_row));
   if (p.large) {
     launch((paged_attention_rows256_kernel<C>), grid, dim3(kLargeThreads), kLargeLds<C>, stream, e1, pb, q,
            (int)R, (int)Hkv, (int)window, o);

@@ -333,6 +333,13 @@ __device__ __forceinline__ float over_quarters(float v, F&& op) {
 struct CacheE4M3 {
   typedef PagedCodes Batch;
   static constexpr int kBytes = 1;
+  // The second kernel costs what eight units do in a block, and the more blocks
+  // there are without it, the less it brings.  (Measured on MI355X, 64:8 heads,
+  // split -> not: one sequence of 300 positions, 10.8 -> 9.1 us, of 600, 10.7 ->
+  // 11.0, of 1000, 10.6 -> 13.6; eight of 600, 12.7 -> 11.2, of 1000, 14.0 -> 13.7;
+  // 16 of 1000, 18.7 -> 14.1; 64 of 1000, 30.5 -> 27.3.  Up to 16 units: where one
+  // sequence is long among short ones, a block walks it alone.)
+  static int split_from(int64_t B, int64_t Hkv) { return (int)std::min<int64_t>(8 + B * Hkv / 16, 16); }
   template <int WAVES>
   static constexpr int kItemLds = WAVES * (4 * kStepBytes + 16 * 8);
   template <int WAVES, int REC>
