@@ -198,7 +198,9 @@ class BatchStep:
     swiglu = True writes silu(gate) * up itself (laq.linear_swiglu: up to 4
     rows).  k_pages / v_pages: fp16 [num_pages][kv_heads][page_size][128] per
     layer (the same pages of every layer belong together: one page table serves
-    them all).  window > 0: a row sees its own and the window - 1 positions
+    them all).  With k_scales / v_scales (float8_e8m0fnu [num_pages][kv_heads]
+    [page_size / 16] per layer) the caches are of 8 bits, k_pages / v_pages
+    float8_e4m3fn.  window > 0: a row sees its own and the window - 1 positions
     before it.
 
     Before run() the caller writes the step's rows into the step's tensors:
@@ -216,13 +218,25 @@ class BatchStep:
     and the settings temperature, top_k, top_p and min_p (tensors [T], filled
     with the values that leave the distribution as it is); it returns tokens
     int32 [T] and probs fp32 [T].  A row whose token nobody wants (a prompt's
-    inner rows, padding) costs its pass and can be ignored."""
+    inner rows, padding) costs its pass and can be ignored.
 
-    def __init__(self, shape, linears, norms, final_norm, k_pages, v_pages, B, T, pages, device, lm_head=None, window=0):
+    history, biases, grammar: what sample() applies to the logits before it
+    draws (laq.adjust_logits; the logits stay as they are, `adjusted` holds the
+    result).  history > 0: room for a row's tokens, in history int32 [T][room],
+    history_len and prompt_len int32 [T], with the settings repetition, frequency
+    and presence fp32 [T]; biases > 0: bias_token int32 and bias_value fp32 [T]
+    [biases]; grammar: mask int32 [T][(vocab + 31) // 32].  They start as what
+    changes nothing.  All of it is read on the device: a captured graph follows
+    what is written there between replays."""
+
+    def __init__(self, shape, linears, norms, final_norm, k_pages, v_pages, B, T, pages, device, lm_head=None, window=0,
+                 k_scales=None, v_scales=None, history=0, biases=0, grammar=False):
         import torch
         self.s = shape
         self.linears, self.norms, self.final_norm, self.lm_head = linears, norms, final_norm, lm_head
         self.k_pages, self.v_pages, self.window = k_pages, v_pages, window
+        assert (k_scales is None) == (v_scales is None)
+        self.k_scales, self.v_scales = k_scales, v_scales
         D, Hq, Hkv, I = shape["hidden"], shape["heads"], shape["kv_heads"], shape["mlp"]
         capacity = pages * k_pages[0].shape[2]
         self.cos_sin = rope_table(capacity, shape["rope_theta"], device)
@@ -251,6 +265,20 @@ class BatchStep:
             self.temperature, self.top_p = torch.ones((T,), **f32), torch.ones((T,), **f32)
             self.min_p, self.top_k = torch.zeros((T,), **f32), torch.zeros((T,), **i32)
             self.tokens, self.probs = torch.zeros((T,), **i32), torch.zeros((T,), **f32)
+            self._adjust = {}
+            if history:
+                self.history, self.history_len = torch.full((T, history), -1, **i32), torch.zeros((T,), **i32)
+                self.prompt_len, self.repetition = torch.zeros((T,), **i32), torch.ones((T,), **f32)
+                self.frequency, self.presence = torch.zeros((T,), **f32), torch.zeros((T,), **f32)
+                for n in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence"):
+                    self._adjust[n] = getattr(self, n)
+            if biases:
+                self.bias_token, self.bias_value = torch.full((T, biases), -1, **i32), torch.zeros((T, biases), **f32)
+                self._adjust.update(bias_token=self.bias_token, bias_value=self.bias_value)
+            if grammar:
+                self.mask = torch.full((T, (shape["vocab"] + 31) // 32), -1, **i32)
+                self._adjust["mask"] = self.mask
+            self.adjusted = torch.empty_like(self.logits) if self._adjust else self.logits
 
     def run(self):
         s = self.s
@@ -261,10 +289,15 @@ class BatchStep:
             w_in, w_post, qn, kn = self.norms[l]
             laq.add_rmsnorm(self.residual, delta, w_in, eps, out=self.h)
             f_qkv(self.h, self.qkv)
-            laq.paged_append(self.qkv, qn, kn, self.cos_sin, self.k_pages[l], self.v_pages[l], self.page_table,
-                             self.token_start, self.seq_len, Hq, eps, q_out=self.q)
-            laq.paged_attention(self.q, self.k_pages[l], self.v_pages[l], self.page_table, self.token_start,
-                                self.seq_len, window=self.window, out=self.attn, workspace=self.workspace)
+            rows = (self.page_table, self.token_start, self.seq_len)
+            if self.k_scales is None:
+                cache = (self.k_pages[l], self.v_pages[l])
+                append, attention = laq.paged_append, laq.paged_attention
+            else:
+                cache = (self.k_pages[l], self.v_pages[l], self.k_scales[l], self.v_scales[l])
+                append, attention = laq.paged_append_e4m3, laq.paged_attention_e4m3
+            append(self.qkv, qn, kn, self.cos_sin, *cache, *rows, Hq, eps, q_out=self.q)
+            attention(self.q, *cache, *rows, window=self.window, out=self.attn, workspace=self.workspace)
             f_o(self.attn.view(T, Hq * HEAD_DIM), self.o)
             laq.add_rmsnorm(self.residual, self.o, w_post, eps, out=self.h)
             if getattr(f_gu, "swiglu", False):
@@ -281,5 +314,7 @@ class BatchStep:
         return self.logits
 
     def sample(self):
-        return laq.sample(self.logits, self.u, self.temperature, self.top_k, self.top_p, self.min_p, out=self.tokens,
+        if self._adjust:
+            laq.adjust_logits(self.logits, **self._adjust, out=self.adjusted)
+        return laq.sample(self.adjusted, self.u, self.temperature, self.top_k, self.top_p, self.min_p, out=self.tokens,
                           probs=self.probs)

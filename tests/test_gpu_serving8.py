@@ -24,7 +24,7 @@ import torch
 from oracle import serving as OS
 from oracle.compare import linear_check
 from paper_2605_08755_amd import decode, laq
-from test_gpu_serving import Batch, attention_check, dev, f16, say
+from test_gpu_serving import SHAPE, Batch, attention_check, dev, f16, make_step, say, set_rows
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda:0")
@@ -733,3 +733,131 @@ def test_adjust_in_a_graph():
         g.replay()
         torch.cuda.synchronize()
         adjust_check(logits, a, out.cpu().numpy())
+
+
+# ---------------------------------------------------------------------------
+# the operators together, as decode.BatchStep runs them
+# ---------------------------------------------------------------------------
+def make_step8(rng, T, B, ps, pages, window=0, seen=None, **kw):
+    """A BatchStep over caches of 8 bits, of make_step's weights; `seen` receives
+    (what, layer, input, output, q, codes and scales after it)."""
+    base = make_step(rng, T, B, ps, pages, window)
+    num, Hkv = base.k_pages[0].shape[:2]
+
+    def watched(f, what, l):
+        def g(x, out):
+            f(x, out)
+            if seen is not None:
+                seen[what, l] = [x.clone(), out.clone(), step.q.clone()] + [
+                    t.view(torch.uint8).clone() for t in (step.k_pages[l], step.v_pages[l], step.k_scales[l], step.v_scales[l])]
+        return g
+    lins = [tuple(watched(f, what, l) for f, what in zip(fs, ("qkv", "o", "gu", "down"))) for l, fs in enumerate(base.linears)]
+    kp, vp = ([torch.zeros((num, Hkv, ps, 128), dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2)] for _ in range(2))
+    ks, vs = ([torch.zeros((num, Hkv, ps // 16), dtype=torch.uint8, device=DEV).view(E8M0) for _ in range(2)] for _ in range(2))
+    step = decode.BatchStep(SHAPE, lins, base.norms, base.final_norm, kp, vp, B, T, pages, DEV, lm_head=base.lm_head,
+                            window=window, k_scales=ks, v_scales=vs, **kw)
+    step.page_table.copy_(base.page_table)
+    return step
+
+
+@pytest.mark.parametrize("window", [0, 9])
+def test_batch_step(window):
+    """A prompt's chunk, a second chunk beside a decoding sequence, then decoding
+    with padding rows: append and attention against the oracle from the stage's
+    own inputs on the GPU, then penalties, biases and a mask, and the draw."""
+    say("batch step8", window)
+    rng = np.random.default_rng(170 + window)
+    T, B, ps, pages, H, N = 12, 3, 16, 3, 20, 4
+    seen = {}
+    step = make_step8(rng, T, B, ps, pages, window, seen, history=H, biases=N, grammar=True)
+    Hq, Hkv, V = SHAPE["heads"], SHAPE["kv_heads"], SHAPE["vocab"]
+    cs = step.cos_sin.cpu().numpy()
+    first = True
+    for tokens, before in (([12, 0, 0], [0, 0, 0]), ([6, 5, 1], [12, 0, 0]), ([1, 1, 1], [18, 5, 1]),
+                           ([1, 1, 1], [19, 6, 2])):
+        set_rows(step, tokens, before, rng)
+        step.u.copy_(dev(rng.random(T).astype(np.float32)))
+        step.temperature.fill_(0.8)
+        step.top_k.fill_(50)
+        old = [[host(t) for t in ts] for ts in zip(step.k_pages, step.v_pages, step.k_scales, step.v_scales)]
+        logits = step.run()
+        if first:  # what changes nothing
+            tok, prob = step.sample()
+            assert torch.equal(step.adjusted.view(torch.int16), logits.view(torch.int16))
+            first = False
+        _, a = adjust_case(rng, T, V, H, N, True)
+        for n, t in to_dev(a).items():
+            getattr(step, n).copy_(t)
+        tok, prob = step.sample()
+        torch.cuda.synchronize()
+        table, start, lens = (t.cpu().numpy() for t in (step.page_table, step.token_start, step.seq_len))
+        mine = sum(tokens)
+        for l in range(2):
+            bt = Batch8.__new__(Batch8)
+            bt.kc, bt.vc, bt.ks, bt.vs = old[l]
+            bt.tokens, bt.table, bt.start, bt.lens, bt.T, bt.ps, bt.Hkv, bt.P = tokens, table, start, lens, T, ps, Hkv, len(bt.kc)
+            qkv = seen["qkv", l][1].cpu().numpy()
+            x, _, q, k, v, ks, vs = (t.cpu().numpy() for t in seen["o", l])
+            check_append(rng, bt, qkv, *(w.cpu().numpy() for w in step.norms[l][2:]), step.cos_sin, Hq,
+                         np.zeros((T, Hq, 128), np.float16), got=((k, ks), (v, vs)))
+            bt.kc, bt.vc, bt.ks, bt.vs = k, v, ks, vs
+            bt.values()
+            check_rows(bt, Hq, q, np.concatenate([x.reshape(T, Hq, 128)[:mine], np.zeros((T - mine, Hq, 128), np.float16)]),
+                       window, np.zeros((T, Hq, 128), np.float16))
+        plain, adjusted = logits.cpu().numpy(), step.adjusted.cpu().numpy()
+        adjust_check(plain, a, adjusted)
+        for r in range(mine):
+            want, p = OS.sample_row(adjusted[r], float(step.u[r]), temperature=float(np.float32(0.8)), top_k=50)
+            assert int(tok[r]) == want and abs(float(prob[r]) - p) <= 2.0**-23 * p
+
+
+def test_batch_step_in_a_graph():
+    """A decoding loop that feeds each step's tokens into the next and into the
+    histories, as graph replays and as eager calls: the same tokens, caches and
+    logits; and penalties that forbid what was said are kept."""
+    say("batch step8 graph")
+    T, B, ps, pages, H = 4, 4, 16, 4, 16
+    runs = []
+    for graphed in (False, True):
+        rng = np.random.default_rng(90)
+        step = make_step8(rng, T, B, ps, pages, history=H)
+        table = dev(rng.standard_normal((SHAPE["vocab"], SHAPE["hidden"])).astype(np.float32))
+        one = torch.ones_like(step.seq_len)
+        step.token_start.copy_(torch.arange(B + 1, device=DEV, dtype=torch.int32))
+        step.temperature.copy_(torch.tensor([0.0, 0.7, 1.0, 1.3], device=DEV))
+        step.top_k.fill_(20)
+        step.presence.fill_(60000.0)  # no token twice
+
+        def one_step():
+            step.seq_len.add_(one)
+            step.run()
+            tok, _ = step.sample()
+            step.history.scatter_(1, step.history_len.long()[:, None], tok[:, None])
+            step.history_len.add_(one)
+            torch.index_select(table, 0, tok, out=step.x0)
+        state = [step.seq_len, step.x0, step.history, step.history_len] + [
+            t.view(torch.uint8) for ts in (step.k_pages, step.v_pages, step.k_scales, step.v_scales) for t in ts]
+        g, got = None, []
+        uniform = rng.random((8, T)).astype(np.float32)
+        step.x0.copy_(table[:T])
+        for i in range(8):
+            step.u.copy_(dev(uniform[i]))
+            if graphed and i == 1:  # the first step, eager, warms up
+                torch.cuda.synchronize()
+                g = torch.cuda.CUDAGraph()
+                saved = [t.clone() for t in state]
+                with torch.cuda.graph(g):
+                    one_step()
+                for t, s in zip(state, saved):
+                    t.copy_(s)
+            if g is not None:
+                g.replay()
+            else:
+                one_step()
+            torch.cuda.synchronize()
+            got.append([step.tokens.clone(), step.logits.view(torch.int16).clone(), step.adjusted.view(torch.int16).clone()])
+        runs.append(got + [[t.clone() for t in state]])
+        said = torch.stack([x[0] for x in got[:8]]).cpu().numpy()
+        assert all(len(set(said[:, r])) == 8 for r in range(T))
+    for a, b in zip(*runs):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
