@@ -287,6 +287,8 @@ hipError_t launch_paged_append_codes(const PagedCodes& pb, const uint16_t* qkv, 
                                      const uint16_t* kw, const float* cos_sin, int64_t rope_rows, int64_t Hq,
                                      int64_t Hkv, float eps, uint16_t* q_out, hipStream_t stream,
                                      const LaunchEvents& ev);
+int64_t paged_attention_codes_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+int64_t paged_attention_codes_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
 hipError_t launch_paged_attention_codes(const PagedCodes& pb, const uint16_t* q, int64_t Hq, int64_t Hkv,
                                         int64_t window, uint16_t* out, float* ws, hipStream_t stream,
                                         const LaunchEvents& ev);

@@ -171,6 +171,9 @@ struct CacheF16 {
   typedef PagedBatch Batch;
   static constexpr int kBytes = 2;
   static int split_from(int64_t, int64_t) { return 0; }
+  static constexpr bool kTileRanges = false;
+  static constexpr bool kFourWaves = false;
+  static bool four_waves(int64_t) { return false; }
   template <int WAVES>
   static constexpr int kItemLds = WAVES * (2 * kKeyBytes + 16 * kRowBytes);
   template <int WAVES, int REC>
@@ -189,7 +192,7 @@ __device__ __forceinline__ void CacheF16::rows16_item(const PagedBatch& pb, cons
   const int n = lane & 15, j = lane >> 4;
   const int rows = min(it.n * R - it.tile * kSmallRows, kSmallRows);
   const int r0 = it.tile * kSmallRows;
-  const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
+  const Span sp = span_of<kTileRanges>(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
 
   // q as matrix operand: lane (m, j), window i: dimensions 32 i + 8 j .. + 7 of row m.
   u32x4 qa[4];
@@ -439,12 +442,12 @@ hipError_t launch_paged_append(const PagedBatch& pb, const uint16_t* qkv, int64_
 }
 
 int64_t paged_attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
-  return attention_plan(B, T, Hq / Hkv, Hkv, capacity).floats * (int64_t)sizeof(float);
+  return attention_plan<CacheF16>(B, T, Hq / Hkv, Hkv, capacity).floats * (int64_t)sizeof(float);
 }
 
 int64_t paged_attention_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
-  const AttentionPlan p = attention_plan(B, T, Hq / Hkv, Hkv, capacity);
-  return p.items * Hkv * (p.large ? kLargeThreads : 64 * kWaves);
+  const AttentionPlan p = attention_plan<CacheF16>(B, T, Hq / Hkv, Hkv, capacity);
+  return p.items * Hkv * (p.rows == kSmallRows ? 64 * kWaves : 512);
 }
 
 hipError_t launch_paged_attention(const PagedBatch& pb, const uint16_t* q, int64_t Hq, int64_t Hkv, int64_t window,

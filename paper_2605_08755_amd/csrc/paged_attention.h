@@ -116,7 +116,9 @@ __device__ __forceinline__ int wave_sum(int v) {
 // since a sequence of x units has ceil(x / chunk) < x / chunk + 1 ranges, at
 // most 2 x / chunk where it is split, and chunk >= (sum of tiles x units) Hkv / kItems.
 constexpr int kUnit = 64;
-constexpr int kSmallRows = 16, kLargeRows = 256;
+constexpr int kSmallRows = 16;
+template <int WAVES>
+constexpr int kChunkRows = 32 * WAVES;  // of a block of the chunks' kernel
 // Blocks of 16 rows that run at once, two a compute unit; twice the blocks of
 // 256.  (Measured on MI355X with 256 and 1024: 16 decoding sequences 44 us -> 54
 // and 44, three long ones 160 -> 149 and 159, a chunk beside 15 decoding rows 70
@@ -134,7 +136,11 @@ struct Seq {
   int tiles, units;
 };
 
-template <int BM>
+// TILE: each tile's own positions are cut into equal ranges, as many as the
+// sequence's other tiles have (a window's tiles, or a fresh prompt's, see unlike
+// parts of the sequence); else the sequence's are, and a tile skips what it does
+// not see.  The chunk then is an upper bound of a range.
+template <int BM, bool TILE>
 __device__ __forceinline__ Seq load_seq(const PagedBatch& pb, int b, int R, int window) {
   Seq q{0, 0, 0, 0, 0, 0, 0};
   if (b < pb.B) {
@@ -148,6 +154,10 @@ __device__ __forceinline__ Seq load_seq(const PagedBatch& pb, int b, int R, int 
     if (q.n > 0) {
       q.tiles = (q.n * R + BM - 1) / BM;
       q.units = max((q.end - q.lo + kUnit - 1) / kUnit, 1);  // rows that see nothing are an item too
+      if (TILE && window > 0) {  // the window of a tile's first token, up to its last one, from a unit's start
+        const int tokens = min(q.n, (BM + R - 2) / R + 1);
+        q.units = min(q.units, (int)(((int64_t)window + tokens + 2 * (kUnit - 1) - 1) / kUnit));
+      }
     }
   }
   return q;
@@ -186,7 +196,7 @@ constexpr int kGroup = 64;
 __host__ __device__ constexpr int64_t plan_groups(int64_t B) { return B > kGroup ? (B + kGroup - 1) / kGroup : 0; }
 
 constexpr int kPlanWaves = 16;
-template <int BM>
+template <int BM, bool TILE>
 __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(PagedBatch pb, int R, int Hkv,
                                                                                int window, int min_chunk,
                                                                                int* __restrict__ plan) {
@@ -196,7 +206,7 @@ __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(P
   const int groups = (int)plan_groups(pb.B);
   double total = 0.0;
   for (int g = w; g < groups; g += kPlanWaves) {
-    const Seq q = load_seq<BM>(pb, g * kGroup + lane, R, window);
+    const Seq q = load_seq<BM, TILE>(pb, g * kGroup + lane, R, window);
     total += wave_sum_exact((double)q.tiles * q.units);
   }
   if (lane == 0) totals[w] = total;
@@ -209,7 +219,7 @@ __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(P
   int upto[3] = {0, 0, 0};
   for (int g0 = 0; g0 < groups; g0 += kPlanWaves) {
     const int g = g0 + w;
-    const Seq q = load_seq<BM>(pb, min(g, groups) * kGroup + lane, R, window);  // (none past the last group)
+    const Seq q = load_seq<BM, TILE>(pb, min(g, groups) * kGroup + lane, R, window);  // (none past the last group)
     const int splits = (q.units + chunk - 1) / chunk;
     const int items = wave_sum(q.tiles * splits), split = wave_sum(splits > 1 ? q.tiles : 0),
               recs = wave_sum(splits > 1 ? q.tiles * splits : 0);
@@ -226,7 +236,7 @@ __global__ __launch_bounds__(64 * kPlanWaves) void paged_attention_plan_kernel(P
 }
 
 // Item `idx` of a key/value head (SPLIT: the idx-th split tile).
-template <int BM, bool SPLIT>
+template <int BM, bool TILE, bool SPLIT>
 __device__ __forceinline__ Item find_item(const PagedBatch& pb, const Out& o, int idx, int R, int Hkv, int window,
                                           int lane) {
   const int* const plan = o.plan;
@@ -251,9 +261,9 @@ __device__ __forceinline__ Item find_item(const PagedBatch& pb, const Out& o, in
     it.chunk = uniform(plan[0]);
     items = uniform(first[g]);
     recs = uniform(before[groups + g]);
-    q = load_seq<BM>(pb, b0 + lane, R, window);
+    q = load_seq<BM, TILE>(pb, b0 + lane, R, window);
   } else {
-    q = load_seq<BM>(pb, lane, R, window);
+    q = load_seq<BM, TILE>(pb, lane, R, window);
     // That chunk, then up to 3/8 and one unit larger until the items are no more
     // than the blocks that run at once (a few more would run alone).
     const int least = least_chunk(wave_sum_exact((double)q.tiles * q.units), Hkv, o.min_chunk);
@@ -299,13 +309,24 @@ struct Span {
   int lo, hi;          // lo a multiple of kUnit
   int all_lo, all_hi;  // positions that every row sees
 };
+template <bool TILE>
 __device__ __forceinline__ Span span_of(const Item& it, int j0, int j1, int window) {
   Span s;
   const int first = it.pos0 + j0, last = it.pos0 + j1;
   const int lo = window > 0 ? max(first - window + 1, 0) & -kUnit : 0;
-  s.lo = max(lo, it.lo + it.split * it.chunk * kUnit);
   s.hi = min(last + 1, it.end);
-  if (it.split + 1 < it.splits) s.hi = min(s.hi, it.lo + (it.split + 1) * it.chunk * kUnit);
+  if constexpr (TILE) {
+    s.lo = lo;
+    if (it.splits > 1) {
+      const int units = (max(s.hi - lo, 0) + kUnit - 1) / kUnit;
+      const int range = uniform((units + it.splits - 1) / it.splits) * kUnit;
+      s.lo = lo + it.split * range;  // (below hi + splits * kUnit)
+      s.hi = min(s.hi, s.lo + range);
+    }
+  } else {
+    s.lo = max(lo, it.lo + it.split * it.chunk * kUnit);
+    if (it.split + 1 < it.splits) s.hi = min(s.hi, it.lo + (it.split + 1) * it.chunk * kUnit);
+  }
   s.all_lo = window > 0 ? max(last - window + 1, 0) : 0;
   s.all_hi = min(first + 1, it.end);
   return s;
@@ -409,20 +430,19 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // lane: ^ (r & 1) too): reads and stores touch each bank once.
 constexpr int kTile = 64;
 constexpr int kTileBytes = kTile * kHeadDim * 2;
-constexpr int kLargeThreads = 512;
-template <class C>
-constexpr int kLargeLds = std::max(4 * kTileBytes + 64, C::template kItemLds<kLargeThreads / 64>);
+template <class C, int WAVES>
+constexpr int kChunkLds = std::max(4 * kTileBytes + 64, C::template kItemLds<WAVES>);
 constexpr float kProbLog2 = 8.0f, kLagLog2 = 7.0f;
 constexpr float kFarLog2 = 65536.0f;
 
 // C: the type of cache: C::Batch, the bytes of an element C::kBytes (2: fp16, 1:
 // e4m3 codes, which become fp16 on their way to LDS), and rows16_item, the way
 // of items of up to 16 rows, with the LDS that its waves need.
-template <class C>
-__global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kernel(typename C::Batch pb,
-                                                                                   const uint16_t* __restrict__ q,
-                                                                                   int R, int Hkv, int window,
-                                                                                   Out o_) {
+template <class C, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(typename C::Batch pb,
+                                                                              const uint16_t* __restrict__ q, int R,
+                                                                              int Hkv, int window, Out o_) {
+  constexpr int kLargeRows = kChunkRows<WAVES>, kThreads = 64 * WAVES;
   constexpr bool kCodes = C::kBytes == 1;
   extern __shared__ u32x4 large_lds[];
   char* const lds = reinterpret_cast<char*>(large_lds);
@@ -432,15 +452,15 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   const int w = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kLargeRows, false>(pb, o_, at_item, R, Hkv, window, lane);
+  const Item it = find_item<kLargeRows, C::kTileRanges, false>(pb, o_, at_item, R, Hkv, window, lane);
   if (!it.found) return;
   if (it.n * R <= kSmallRows) {
-    C::template rows16_item<kLargeThreads / 64, kLargeRows>(pb, q, R, window, o_, it, g, lds);
+    C::template rows16_item<WAVES, kLargeRows>(pb, q, R, window, o_, it, g, lds);
     return;
   }
   const int r0 = it.tile * kLargeRows;
   const int rows = min(it.n * R - r0, kLargeRows);
-  const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
+  const Span sp = span_of<C::kTileRanges>(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
 
   // This lane's query row and what it sees; its operand: dimensions 16 s + 8 h .. + 7.
   const int my = 32 * w + n;
@@ -497,7 +517,8 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   // Staging: thread (row tid / 16 of each half of the tile, piece tid % 16);
   // a wave's rows of a half lie in one group of 16.
   // (codes: row tid / 8, piece tid % 8, of 16 bytes that become two pieces)
-  constexpr int kLoads = C::kBytes;
+  constexpr int kLoads = kTile * 8 * C::kBytes / kThreads;
+  constexpr int kPass = kTile / kLoads;  // rows that a load takes, of all waves
   const int sr = kCodes ? tid >> 3 : tid >> 4, spc = kCodes ? tid & 7 : tid & 15;
   const uint32_t src_at = (uint32_t)(sr & 15) * pb.slot_stride * C::kBytes + 16 * spc;
   u32x4 kreg[kLoads], vreg[kLoads];
@@ -506,7 +527,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
     const int i = (t - set_first) & (kSet - 1);
     return (int)(~(t >= set_first ? set_there : old_there) >> 4 * i) & 15;
   };
-  auto group_of = [&](int i) { return kCodes ? w >> 1 : 2 * i + (w >> 2); };  // of 16 rows, that load i is in
+  auto group_of = [&](int i) { return kPass / 16 * i + (kCodes ? w >> 1 : w >> 2); };  // of 16 rows, that load i is in
   auto load_rows = [&](u32x4(&r)[kLoads], const char* head, int t) {
     const int i0 = (t - set_first) & (kSet - 1);
     const bool now = t >= set_first;
@@ -532,38 +553,42 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
   const int whole_last = max(min(sp.all_hi, sp.hi) - sp.lo, 0) / kTile;
   auto is_masked = [&](int t) { return (bad_of(t) != 0) | (t < whole_first) | (t >= whole_last); };
   // Codes of a row to LDS as two pieces of fp16, whose places go by XOR with `swap`.
-  auto store_codes = [&](char* d, const u32x4& r, float scale, int swap) {
+  auto store_codes = [&](char* d, int row, const u32x4& r, float scale, int swap) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t a = i ? r.z : r.x, b = i ? r.w : r.y;
-      *reinterpret_cast<u32x4*>(d + sr * 256 + 16 * ((2 * spc + i) ^ swap)) =
+      *reinterpret_cast<u32x4*>(d + row * 256 + 16 * ((2 * spc + i) ^ swap)) =
           u32x4{values01(a, scale), values23(a, scale), values01(b, scale), values23(b, scale)};
     }
   };
-  auto scale_of = [&](int now, int old, int t) {
-    const int l = 4 * ((t - set_first) & (kSet - 1)) + group_of(0);
+  auto scale_of = [&](int now, int old, int t, int i) {
+    const int l = 4 * ((t - set_first) & (kSet - 1)) + group_of(i);
     return block_scale(readlane(t >= set_first ? now : old, l));
   };
   auto store_keys = [&](int t) {
     char* const d = lds + (t & 1) * 2 * kTileBytes;
     if constexpr (kCodes) {
-      store_codes(d, kreg[0], scale_of(set_ks, old_ks, t), sr & 15);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) store_codes(d, kPass * i + sr, kreg[i], scale_of(set_ks, old_ks, t, i), sr & 15);
       return;
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      *reinterpret_cast<u32x4*>(d + (32 * i + sr) * 256 + 16 * (spc ^ (sr & 15))) = kreg[i];
+      *reinterpret_cast<u32x4*>(d + (kPass * i + sr) * 256 + 16 * (spc ^ (sr & 15))) = kreg[i];
   };
   // Values that are infinite or NaN stay out of masked tiles: 0 times one is NaN.
   auto store_values = [&](int t) {
     char* const d = lds + (t & 1) * 2 * kTileBytes + kTileBytes;
     if constexpr (kCodes) {
-      u32x4 r = vreg[0];
-      if (is_masked(t)) {
-        if (nan_codes(r.x) | nan_codes(r.y) | nan_codes(r.z) | nan_codes(r.w)) flags[t & 3] = t;
-        r = u32x4{number_codes(r.x), number_codes(r.y), number_codes(r.z), number_codes(r.w)};
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        u32x4 r = vreg[i];
+        if (is_masked(t)) {
+          if (nan_codes(r.x) | nan_codes(r.y) | nan_codes(r.z) | nan_codes(r.w)) flags[t & 3] = t;
+          r = u32x4{number_codes(r.x), number_codes(r.y), number_codes(r.z), number_codes(r.w)};
+        }
+        store_codes(d, kPass * i + sr, r, scale_of(set_vs, old_vs, t, i), 4 * (sr & 3) ^ (sr & 1));
       }
-      store_codes(d, r, scale_of(set_vs, old_vs, t), 4 * (sr & 3) ^ (sr & 1));
       return;
     }
     if (is_masked(t)) {
@@ -576,7 +601,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      *reinterpret_cast<u32x4*>(d + (32 * i + sr) * 256 + 16 * (spc ^ (4 * (sr & 3)))) = vreg[i];
+      *reinterpret_cast<u32x4*>(d + (kPass * i + sr) * 256 + 16 * (spc ^ (4 * (sr & 3)))) = vreg[i];
   };
 
   float ref = kNoMax, l = 0.0f;
@@ -811,7 +836,7 @@ __global__ __launch_bounds__(kLargeThreads, 2) void paged_attention_rows256_kern
 // kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
 // prompts whose tiles are not split, 16.4 -> 4.9 us; a chunk beside 15 decoding
 // rows, 14.5 -> 15.5, of the bytes of its records; twice the blocks, 8.7 and 17.)
-template <int BM, int WAVES>
+template <int BM, bool TILE, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
   constexpr int kRec = BM * (kHeadDim + 2);
@@ -820,7 +845,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<BM, true>(pb, o_, at_item, R, Hkv, window, lane);
+  const Item it = find_item<BM, TILE, true>(pb, o_, at_item, R, Hkv, window, lane);
   if (!it.found || it.rec + it.splits > o_.rec_bound) return;
   const int r0 = it.tile * BM;
   const int rows = min(it.n * R - r0, BM);
@@ -902,8 +927,9 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
 
 // Which kernel takes a batch, and its bounds: a pure function of the sizes.
 struct AttentionPlan {
-  bool large;
+  int rows;  // of a block: 16, or the chunks' kernel
   int64_t items, split_tiles, records;  // per key/value head
+  int64_t most_ranges;                  // of a tile, by the capacity
   int64_t floats;                       // workspace: the records, then the plan
   int64_t plan_at;
   int min_chunk;
@@ -913,7 +939,7 @@ struct AttentionPlan {
 template <int BM>
 AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity, int split_from) {
   AttentionPlan p;
-  p.large = BM == kLargeRows;
+  p.rows = BM;
   const int64_t tiles = (T * R + std::min(B, T) * (BM - 1)) / BM;
   const int64_t per_head = (kItems + Hkv - 1) / Hkv;
   // (with kItems heads and more a head's share of the items is one: no sequence is split)
@@ -922,6 +948,7 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
   p.items = tiles + (split ? per_head : 0);
   p.split_tiles = split ? std::min(per_head, tiles) : 0;
   const int64_t most = (capacity + kMinChunk<BM> * kUnit - 1) / (kMinChunk<BM> * kUnit);
+  p.most_ranges = most;
   p.records = split ? std::min(2 * kItems / Hkv, tiles * most) : 0;
   p.plan_at = p.records * Hkv * BM * (kHeadDim + 2);
   p.floats = p.plan_at + (B > kGroup ? 1 + 3 * plan_groups(B) : 0);
@@ -936,9 +963,14 @@ AttentionPlan plan_of(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capa
 // chunk of 193 rows, all at 500 or at 2000, 67 -> 82 and 161 -> 189; a chunk of 256
 // rows at 6000 beside 63 waiting sequences 180 -> 119, of 16 rows 30 -> 42; 64
 // decoding rows and 193 of padding 98 -> 97, 16 and 49 of padding 35 -> 38.)
-AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity, int split_from = 0) {
+//
+// C::four_waves: chunks whose blocks of 256 rows are few take blocks of 128.
+template <class C>
+AttentionPlan attention_plan(int64_t B, int64_t T, int64_t R, int64_t Hkv, int64_t capacity) {
+  const int split_from = C::split_from(B, Hkv);
   if (T * R <= kSmallRows * B) return plan_of<kSmallRows>(B, T, R, Hkv, capacity, split_from);
-  return plan_of<kLargeRows>(B, T, R, Hkv, capacity, split_from);
+  if (C::four_waves(T * R * Hkv)) return plan_of<kChunkRows<4>>(B, T, R, Hkv, capacity, split_from);
+  return plan_of<kChunkRows<8>>(B, T, R, Hkv, capacity, split_from);
 }
 
 // Up to 16 rows per tile: an item a block.
@@ -949,9 +981,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
                                                                              int Hkv, int window, Out o_) {
   extern __shared__ u32x4 small_lds[];
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
-  const Item it = find_item<kSmallRows, false>(pb, o_, at_item, R, Hkv, window, threadIdx.x & 63);
+  const Item it = find_item<kSmallRows, C::kTileRanges, false>(pb, o_, at_item, R, Hkv, window, threadIdx.x & 63);
   if (!it.found) return;
   C::template rows16_item<kWaves, kSmallRows>(pb, q, R, window, o_, it, g, reinterpret_cast<char*>(small_lds));
+}
+
+template <class C, int BM>
+void launch_chunks(const typename C::Batch& pb, const uint16_t* q, int64_t R, int64_t Hkv, int64_t window, const Out& o,
+                   dim3 grid, dim3 join, bool by_16, hipStream_t stream, const LaunchEvents& e1, const LaunchEvents& e2) {
+  const PagedBatch& rows = pb;
+  constexpr int kWavesOf = BM / 32;
+  launch((paged_attention_chunk_kernel<C, kWavesOf>), grid, dim3(64 * kWavesOf), kChunkLds<C, kWavesOf>, stream, e1, pb, q,
+         (int)R, (int)Hkv, (int)window, o);
+  if (join.x == 0) return;
+  if (by_16)
+    launch((paged_attention_join_kernel<BM, C::kTileRanges, 1>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
+  else
+    launch((paged_attention_join_kernel<BM, C::kTileRanges, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
 }
 
 template <class C>
@@ -959,8 +1005,7 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
                             uint16_t* out, float* ws, hipStream_t stream, const LaunchEvents& ev) {
   const PagedBatch& rows = pb;
   const int64_t R = Hq / Hkv;
-  const AttentionPlan p = attention_plan(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift,
-                                         C::split_from(pb.B, Hkv));
+  const AttentionPlan p = attention_plan<C>(pb.B, pb.T, R, Hkv, (int64_t)pb.table_pages << pb.page_shift);
   LaunchEvents e0, e1 = ev, e2;
   if (p.split_tiles > 0) {  // the measurement hook spans all kernels
     e1.stop = nullptr;
@@ -970,36 +1015,37 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
   if (pb.B > kGroup) {
     e0.start = e1.start;
     e1.start = nullptr;
-    auto* const kernel = p.large ? paged_attention_plan_kernel<kLargeRows> : paged_attention_plan_kernel<kSmallRows>;
+    auto* const kernel = p.rows == kSmallRows ? paged_attention_plan_kernel<kSmallRows, C::kTileRanges>
+                         : p.rows == kChunkRows<4> ? paged_attention_plan_kernel<kChunkRows<4>, C::kTileRanges>
+                                              : paged_attention_plan_kernel<kChunkRows<8>, C::kTileRanges>;
     launch(kernel, dim3(1), dim3(64 * kPlanWaves), 0, stream, e0, rows, (int)R, (int)Hkv, (int)window, p.min_chunk, plan);
   }
   const Out o{out, ws, plan, (int)Hq, (int)p.records, p.min_chunk};
   const dim3 grid((unsigned)(p.items * Hkv));
-  // A block joins one row; 16 rows where the tiles (most of them not split) would make many blocks.
-  constexpr int64_t kFewTiles = 32, kJoinBlocks = 2048;
-  const bool many = p.large && p.split_tiles * Hkv > kFewTiles;
-  const int64_t most_rows = std::min<int64_t>(p.large ? kLargeRows : kSmallRows, pb.T * R);
+  // A block joins one row; 16 rows where the tiles (most of them not split) would
+  // make many blocks.  (Tiles of 128 rows, measured on MI355X, by row -> by 16: 8 of
+  // up to 8 ranges 3.9 -> 5.6 us, 16 of up to 25, 8.8 -> 14.2, of up to 16, 7.8 and
+  // 7.8, of up to 3, 7.7 -> 4.5; 32 of up to 9, 13.0 -> 7.0.)
+  constexpr int64_t kJoinBlocks = 2048;
+  const int64_t few_tiles = p.rows != kChunkRows<4> ? 32 : p.most_ranges >= 16 ? 16 : 8;
+  const bool many = p.rows != kSmallRows && p.split_tiles * Hkv > few_tiles;
+  const int64_t most_rows = std::min<int64_t>(p.rows, pb.T * R);
   const int64_t by_16 = std::min((most_rows + 15) / 16, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
   // (A block per row where that is about as many as run at once, else fewer that
   // go on: where nothing is split, each costs its search.  Measured on MI355X, 64
   // sequences of 400 positions, 64:8 heads, e4m3 codes: 25 -> 19 us.)
   const int64_t by_row = std::min(most_rows, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
   const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_16 : by_row));
-  if (p.large) {
-    launch((paged_attention_rows256_kernel<C>), grid, dim3(kLargeThreads), kLargeLds<C>, stream, e1, pb, q,
-           (int)R, (int)Hkv, (int)window, o);
-    if (p.split_tiles > 0 && p.split_tiles * Hkv <= kFewTiles)
-      launch((paged_attention_join_kernel<kLargeRows, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv,
-             (int)window, o);
-    else if (p.split_tiles > 0)
-      launch((paged_attention_join_kernel<kLargeRows, 1>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv,
-             (int)window, o);
-  } else {
+  if (p.rows == kSmallRows) {
     launch((paged_attention_rows16_kernel<C>), grid, dim3(64 * kWaves), C::template kItemLds<kWaves>, stream, e1, pb, q,
            (int)R, (int)Hkv, (int)window, o);
     if (p.split_tiles > 0)
-      launch((paged_attention_join_kernel<kSmallRows, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window,
-             o);
+      launch((paged_attention_join_kernel<kSmallRows, C::kTileRanges, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv,
+             (int)window, o);
+  } else if (p.rows == kChunkRows<8>) {
+    launch_chunks<C, kChunkRows<8>>(pb, q, R, Hkv, window, o, grid, join, many, stream, e1, e2);
+  } else if constexpr (C::kFourWaves) {
+    launch_chunks<C, kChunkRows<4>>(pb, q, R, Hkv, window, o, grid, join, many, stream, e1, e2);
   }
   return hipGetLastError();
 }

@@ -340,6 +340,16 @@ struct CacheE4M3 {
   // 16 of 1000, 18.7 -> 14.1; 64 of 1000, 30.5 -> 27.3.  Up to 16 units: where one
   // sequence is long among short ones, a block walks it alone.)
   static int split_from(int64_t B, int64_t Hkv) { return (int)std::min<int64_t>(8 + B * Hkv / 16, 16); }
+  static constexpr bool kTileRanges = true;
+  static constexpr bool kFourWaves = true;
+  // Blocks of 128 query rows (two a compute unit) below 512 blocks of 256, whose
+  // every compute unit then has two turns: less is left over in the last one, and
+  // fewer rows are split over positions and joined.  (Measured on MI355X, blocks of
+  // 256 -> 128, 32:8 heads: chunks of 64 rows at 500 positions 25.2 -> 21.3 us, of
+  // 512 at 0, 25.8 -> 20.9, at 2000, 58 -> 46, of 2048 at 0, 85 -> 69, of 4096 at 0
+  // (512 blocks) 161 -> 182; 64:8, 2048 at 0 (512) 96 -> 103; 8:1, 4096 at 0 (128),
+  // 76 -> 83.)
+  static bool four_waves(int64_t rows) { return rows < 512 * kChunkRows<8>; }
   template <int WAVES>
   static constexpr int kItemLds = WAVES * (4 * kStepBytes + 16 * 8);
   template <int WAVES, int REC>
@@ -358,7 +368,7 @@ __device__ __forceinline__ void CacheE4M3::rows16_item(const PagedCodes& pb, con
   const int n = lane & 15, j = lane >> 4;
   const int rows = min(it.n * R - it.tile * kSmallRows, kSmallRows);
   const int r0 = it.tile * kSmallRows;
-  const Span sp = span_of(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
+  const Span sp = span_of<kTileRanges>(it, uniform(r0 / R), uniform((r0 + rows - 1) / R), window);
 
   // q as matrix operand: lane (n, j), window 2a + b: dimensions 64 a + 16 j + 8 b .. + 7 of row n.
   const int mine = min(n, rows - 1);
@@ -658,6 +668,15 @@ hipError_t launch_paged_attention_codes(const PagedCodes& pb, const uint16_t* q,
                                         int64_t window, uint16_t* out, float* ws, hipStream_t stream,
                                         const LaunchEvents& ev) {
   return launch_attention<CacheE4M3>(pb, q, Hq, Hkv, window, out, ws, stream, ev);
+}
+
+int64_t paged_attention_codes_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  return attention_plan<CacheE4M3>(B, T, Hq / Hkv, Hkv, capacity).floats * (int64_t)sizeof(float);
+}
+
+int64_t paged_attention_codes_threads(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  const AttentionPlan p = attention_plan<CacheE4M3>(B, T, Hq / Hkv, Hkv, capacity);
+  return p.items * Hkv * (p.rows == kSmallRows ? 64 * kWaves : 2 * p.rows);
 }
 
 }  // namespace laq
