@@ -655,13 +655,19 @@ laq_status laq_paged_append_e4m3(const laq_paged_batch *batch, uint8_t *k_scales
                                  const float *cos_sin, int64_t rope_rows, int64_t Hq, int64_t Hkv, int64_t head_dim,
                                  float eps, void *q_out, void *stream);
 
+/* laq_paged_attention_e4m3_workspace_bytes -- workspace (bytes) with which
+ * laq_paged_attention_e4m3 runs a batch, as laq_paged_attention_workspace_bytes
+ * and never more than that; 0 when the call needs none (short tables), and for
+ * invalid sizes. */
+int64_t laq_paged_attention_e4m3_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity);
+
 /* laq_paged_attention_e4m3 -- laq_paged_attention_f16 over a cache of 8 bits:
  * the attention over the values that its codes stand for, which are fp16
  * numbers, so that nothing is rounded on reading them.  Probabilities of
  * sequences with at most 16 / (Hq / Hkv) rows keep 22 bits (two fp16 numbers
  * whose sum has them) whatever else the batch holds; those of longer chunks as
- * for laq_paged_attention_f16.  The workspace is
- * laq_paged_attention_workspace_bytes', whatever the cache.
+ * for laq_paged_attention_f16.
+ *   workspace  as there, of laq_paged_attention_e4m3_workspace_bytes.
  * Errors: as laq_paged_attention_f16's (strides of the pages: MISALIGNED unless
  * multiples of 16); NULL_POINTER also for the scales. */
 laq_status laq_paged_attention_e4m3(const laq_paged_batch *batch, const uint8_t *k_scales, const uint8_t *v_scales,

@@ -639,12 +639,6 @@ laq_status check_append(const char* fn, const laq_paged_batch* batch, const void
   return LAQ_OK;
 }
 
-// One workspace serves both types of cache.
-int64_t attention_workspace(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
-  return std::max(laq::paged_attention_workspace(B, T, Hq, Hkv, capacity),
-                  laq::paged_attention_codes_workspace(B, T, Hq, Hkv, capacity));
-}
-
 laq_status check_attention(const char* fn, const laq_paged_batch* batch, const void* q, int64_t Hq, int64_t Hkv,
                            int64_t head_dim, int64_t window, const void* out, const void* workspace,
                            int64_t workspace_bytes, int bytes, bool* nothing) {
@@ -655,10 +649,11 @@ laq_status check_attention(const char* fn, const laq_paged_batch* batch, const v
   if (!q || !out) return fail(LAQ_ERR_NULL_POINTER, fn, "null pointer argument");
   if ((st = check_batch_pointers(fn, batch)) != LAQ_OK) return st;
   const int64_t capacity = batch->table_pages * batch->page_size;
-  const int64_t need = attention_workspace(batch->B, batch->T, Hq, Hkv, capacity);
+  const int64_t need = (bytes == 2 ? laq::paged_attention_workspace : laq::paged_attention_codes_workspace)(
+      batch->B, batch->T, Hq, Hkv, capacity);
   if (need > 0 && !workspace) return fail(LAQ_ERR_NULL_POINTER, fn, "null workspace");
   if (workspace_bytes < need)
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below laq_paged_attention_workspace_bytes");
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "workspace_bytes below the call's workspace_bytes query");
   const int64_t threads = (bytes == 2 ? laq::paged_attention_threads : laq::paged_attention_codes_threads)(
       batch->B, batch->T, Hq, Hkv, capacity);
   if (threads > 0xFFFFFFFFLL)
@@ -715,11 +710,17 @@ laq_status laq_paged_append_e4m3(const laq_paged_batch* batch, uint8_t* k_scales
                             static_cast<uint16_t*>(q_out), static_cast<hipStream_t>(stream), ev));
 }
 
+static bool attention_sizes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  return !(B < 1 || B > (1 << 20) || T < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096 || T > (1LL << 30) ||
+           T * Hq > (1LL << 30) || capacity < 1 || capacity > (1LL << 30));
+}
+
 int64_t laq_paged_attention_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
-  if (B < 1 || B > (1 << 20) || T < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > 4096 || T > (1LL << 30) ||
-      T * Hq > (1LL << 30) || capacity < 1 || capacity > (1LL << 30))
-    return 0;
-  return attention_workspace(B, T, Hq, Hkv, capacity);
+  return attention_sizes(B, T, Hq, Hkv, capacity) ? laq::paged_attention_workspace(B, T, Hq, Hkv, capacity) : 0;
+}
+
+int64_t laq_paged_attention_e4m3_workspace_bytes(int64_t B, int64_t T, int64_t Hq, int64_t Hkv, int64_t capacity) {
+  return attention_sizes(B, T, Hq, Hkv, capacity) ? laq::paged_attention_codes_workspace(B, T, Hq, Hkv, capacity) : 0;
 }
 
 laq_status laq_paged_attention_f16(const laq_paged_batch* batch, const void* q, int64_t Hq, int64_t Hkv,

@@ -256,8 +256,9 @@ class BatchStep:
         self.m = torch.empty((T, I), **f16)
         self.down = torch.empty((T, D), **f16)
         self.out = torch.empty((T, D), **f16)
-        self.workspace = torch.empty(max(laq.paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity), 16),
-                                     dtype=torch.uint8, device=device)
+        nbytes = (laq.paged_attention_workspace_bytes if k_scales is None else
+                  laq.paged_attention_e4m3_workspace_bytes)(B, T, Hq, Hkv, capacity)
+        self.workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
         self.logits = self.u = None
         if lm_head is not None:
             self.logits = torch.empty((T, shape["vocab"]), **f16)

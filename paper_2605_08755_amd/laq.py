@@ -37,7 +37,7 @@ EXPORTS = ("laq_abi_version", "laq_status_string", "laq_last_error", "laq_profil
            "laq_mlp_workspace_bytes", "laq_add_rmsnorm_mlp_w3g128", "laq_linear_residual_w3g128",
            "laq_linear_residual_w4g128", "laq_paged_append_f16", "laq_paged_attention_workspace_bytes",
            "laq_paged_attention_f16", "laq_sample_f16", "laq_paged_append_e4m3", "laq_paged_attention_e4m3",
-           "laq_adjust_logits_f16")
+           "laq_paged_attention_e4m3_workspace_bytes", "laq_adjust_logits_f16")
 HEAD_DIM = 128
 
 
@@ -144,6 +144,8 @@ def lib():
         L.laq_sample_f16.restype = ctypes.c_int32
         L.laq_paged_append_e4m3.argtypes = [P, P, P, P, I64, P, P, P, I64, I64, I64, I64, F32, P, P]
         L.laq_paged_append_e4m3.restype = ctypes.c_int32
+        L.laq_paged_attention_e4m3_workspace_bytes.argtypes = [I64, I64, I64, I64, I64]
+        L.laq_paged_attention_e4m3_workspace_bytes.restype = I64
         L.laq_paged_attention_e4m3.argtypes = [P, P, P, P, I64, I64, I64, I64, P, P, I64, P]
         L.laq_paged_attention_e4m3.restype = ctypes.c_int32
         L.laq_adjust_logits_f16.argtypes = [P, P, I64, I64, I64, P, I64, P]
@@ -554,7 +556,7 @@ def silu_mul(gate_up, out=None):
 # append of 16 rows 8.5 -> 7.5 us a call, attention of one token 11.4 -> 10.3.)
 class _Torch:
     """torch's names that a call needs, filled in at the first one."""
-    f16 = f32 = i32 = u8 = e4m3 = e8m0 = empty = zeros = current = stream = guard = None
+    f16 = f32 = i32 = u8 = e4m3 = e8m0 = empty = empty_like = zeros = current = stream = guard = None
 
 
 def _torch():
@@ -562,7 +564,7 @@ def _torch():
         import torch
         _Torch.f32, _Torch.i32, _Torch.u8 = torch.float32, torch.int32, torch.uint8
         _Torch.e4m3, _Torch.e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
-        _Torch.empty, _Torch.zeros = torch.empty, torch.zeros
+        _Torch.empty, _Torch.empty_like, _Torch.zeros = torch.empty, torch.empty_like, torch.zeros
         _Torch.current, _Torch.stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
         _Torch.guard = torch.cuda.device
         _Torch.f16 = torch.float16
@@ -686,7 +688,13 @@ def paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity):
     return int(lib().laq_paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity))
 
 
-def _attention_args(dev, t, q, batch, out, workspace):
+@functools.lru_cache(maxsize=4096)
+def paged_attention_e4m3_workspace_bytes(B, T, Hq, Hkv, capacity):
+    """That of paged_attention_e4m3: at most paged_attention_workspace_bytes."""
+    return int(lib().laq_paged_attention_e4m3_workspace_bytes(B, T, Hq, Hkv, capacity))
+
+
+def _attention_args(dev, t, q, batch, workspace_bytes, out, workspace):
     """(out, workspace, its bytes) of an attention's tensors, checked, made where not given."""
     _, Hkv, B, capacity = batch
     shape = q.shape
@@ -697,7 +705,7 @@ def _attention_args(dev, t, q, batch, out, workspace):
     else:
         assert out.dtype is t.f16 and out.shape == shape and out.is_contiguous() and out.get_device() == dev
     if workspace is None:
-        nbytes = paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity)
+        nbytes = workspace_bytes(B, T, Hq, Hkv, capacity)
         if nbytes:
             workspace = t.empty(nbytes, dtype=t.u8, device=q.device)
     else:
@@ -716,7 +724,7 @@ def paged_attention(q, k_pages, v_pages, page_table, token_start, seq_len, windo
     t = _torch()
     dev = q.get_device()
     batch = _paged_batch(dev, t.f16, k_pages, v_pages, page_table, token_start, seq_len, q.shape[0])
-    out, workspace, nbytes = _attention_args(dev, t, q, batch, out, workspace)
+    out, workspace, nbytes = _attention_args(dev, t, q, batch, paged_attention_workspace_bytes, out, workspace)
     _launch(dev, lib().laq_paged_attention_f16, batch[0], q.data_ptr(), q.shape[1], batch[1], HEAD_DIM, window,
             out.data_ptr(), None if workspace is None else workspace.data_ptr(), nbytes)
     return out
@@ -730,10 +738,18 @@ def paged_attention_e4m3(q, k_pages, v_pages, k_scales, v_scales, page_table, to
     dev = q.get_device()
     batch = _paged_batch(dev, t.e4m3, k_pages, v_pages, page_table, token_start, seq_len, q.shape[0])
     ks, vs = _scales(dev, t, k_pages, k_scales, v_scales)
-    out, workspace, nbytes = _attention_args(dev, t, q, batch, out, workspace)
+    out, workspace, nbytes = _attention_args(dev, t, q, batch, paged_attention_e4m3_workspace_bytes, out, workspace)
     _launch(dev, lib().laq_paged_attention_e4m3, batch[0], ks, vs, q.data_ptr(), q.shape[1], batch[1], HEAD_DIM, window,
             out.data_ptr(), None if workspace is None else workspace.data_ptr(), nbytes)
     return out
+
+
+def _rows_of(dev, x, dtype, rows):
+    """(pointer, stride between rows, width) of a tensor [rows][width]."""
+    n, width = x.shape
+    stride, one = x.stride()
+    assert n == rows and x.dtype is dtype and (one == 1 or width == 1) and x.get_device() == dev
+    return x.data_ptr(), stride if n > 1 else width, width
 
 
 def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None,
@@ -755,34 +771,26 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
     stride, one = logits.stride()
     assert dev >= 0 and logits.dtype is t.f16 and (one == 1 or V == 1)
     if out is None:
-        out = t.empty((rows, V), dtype=t.f16, device=logits.device)
+        out = t.empty_like(logits)
     else:
         assert out.dtype is t.f16 and out.shape == (rows, V) and out.get_device() == dev
     out_stride, one = out.stride()
     assert one == 1 or V == 1
-
-    def rows_of(x, dtype, width=None):
-        """(pointer, stride between rows, width) of a tensor [rows][width]"""
-        n, w = x.shape
-        a, b = x.stride()
-        assert x.dtype is dtype and n == rows and (width is None or w == width) and (b == 1 or w == 1)
-        assert x.get_device() == dev
-        return x.data_ptr(), a if n > 1 else w, w
     h = b = (0, 0, 0)
-    v = m = 0
+    v = m = m_stride = 0
     if history is not None:
-        h = rows_of(history, t.i32)
+        h = _rows_of(dev, history, t.i32, rows)
     else:
         assert history_len is None and prompt_len is None
     if bias_token is not None:
-        b = rows_of(bias_token, t.i32)
-        v, v_stride, _ = rows_of(bias_value, t.f32, b[2])
-        assert v_stride == b[1] or rows == 1
+        b = _rows_of(dev, bias_token, t.i32, rows)
+        v, v_stride, n = _rows_of(dev, bias_value, t.f32, rows)
+        assert n == b[2] and v_stride == b[1]
     else:
         assert bias_value is None
-    m_stride = 0
     if mask is not None:
-        m, m_stride, _ = rows_of(mask, t.i32, (V + 31) // 32)
+        m, m_stride, n = _rows_of(dev, mask, t.i32, rows)
+        assert n == (V + 31) // 32
     ptr = []
     for x, dtype in ((history_len, t.i32), (prompt_len, t.i32), (repetition, t.f32), (frequency, t.f32), (presence, t.f32)):
         if x is not None:

@@ -150,7 +150,13 @@ int main() {
           for (int64_t capacity : {kMin, (int64_t)0, (int64_t)16, (int64_t)128, (int64_t)129, (int64_t)4096, (int64_t)1 << 30, kMax}) {
             const int64_t Hq = Hkv > 0 && Hkv <= 4096 ? Hkv * R : Hkv;
             const int64_t n = laq_paged_attention_workspace_bytes(B, T, Hq, Hkv, capacity);
-            ++g_checks;
+            const int64_t n8 = laq_paged_attention_e4m3_workspace_bytes(B, T, Hq, Hkv, capacity);
+            g_checks += 2;
+            if (n8 < 0 || n8 > n) {
+              std::printf("laq_paged_attention_e4m3_workspace_bytes(%lld, %lld, %lld, %lld, %lld) = %lld\n", (long long)B,
+                          (long long)T, (long long)Hq, (long long)Hkv, (long long)capacity, (long long)n8);
+              ++g_bad;
+            }
             if (n < 0 || n > 140 * 1000 * 1000) {
               std::printf("laq_paged_attention_workspace_bytes(%lld, %lld, %lld, %lld, %lld) = %lld\n", (long long)B,
                           (long long)T, (long long)Hq, (long long)Hkv, (long long)capacity, (long long)n);

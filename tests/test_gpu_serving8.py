@@ -473,6 +473,47 @@ def test_attention_chunks_over_many_tiles(tokens, before, Hq, Hkv, ps, window):
     assert np.array_equal(out.view(np.uint16), clean.view(np.uint16))
 
 
+@pytest.mark.parametrize("window", [0, 300])
+def test_attention_large_batches(window):
+    """As many query rows as the kernel of 256 rows a block takes: chunks beside a
+    decoding sequence, missing pages, NaN among values that some rows do not see.
+    Some rows of every sequence against 64 bits."""
+    say("attention8 large", window)
+    rng = np.random.default_rng(40 + window)
+    Hq, Hkv, ps, tokens, before = 64, 8, 32, [1500, 1, 600], [100, 1700, 700]
+    bt = Batch8(rng, tokens, before, ps, Hkv, pad=5)
+    bt.table[2, [3, 30]] = [-1, bt.P]
+    seen_by_few = int(bt.lens[0]) - 3
+    bt.vc[bt.table[0, seen_by_few // ps], 1, seen_by_few % ps, ::7] = 0x7F
+    bt.values()
+    assert bt.T * Hq >= 512 * 256
+    q = f16(rng, (bt.T, Hq, 128))
+    canary = f16(rng, (bt.T, Hq, 128))
+    got = attend(bt, q, window, dev(canary))
+    again = attend(bt, q, window, dev(canary))
+    assert np.array_equal(got.view(np.uint16), again.view(np.uint16))
+    assert np.array_equal(got[-5:], canary[-5:])
+    rows = [(r, b, pos) for r, b, pos in OS.rows(bt.start, bt.lens)]
+    picked = [rows[i] for i in sorted(set(rng.integers(0, len(rows), 40).tolist()) |
+                                      {0, 1, 31, 32, 255, 256, 1496, 1497, 1499, 1500, 1501, len(rows) - 1})]
+    few = small(bt, Hq)
+    for r, b, pos in picked:
+        t = np.arange(max(0, pos - window + 1) if window else 0, pos + 1)
+        pages = bt.table[b, t // ps]
+        t, pages = t[(pages >= 0) & (pages < bt.P)], pages[(pages >= 0) & (pages < bt.P)]
+        for g in range(Hkv):
+            K, V = (c[pages, g, t % ps].astype(np.float64) for c in (bt.k, bt.v))
+            x = q[r, 8 * g:8 * g + 8].astype(np.float64)
+            s = x @ K.T / 128**0.5
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            out, nan = got[r, 8 * g:8 * g + 8], np.isnan(V).any(0)
+            assert np.isnan(out[:, nan]).all()
+            V = np.where(nan, 0.0, V)
+            reach = (np.abs(x) @ np.abs(K).T).max(1) / 128**0.5
+            attention_check(np.where(nan, np.float16(0), out), p @ V, p @ np.abs(V), reach + 2.0, len(t), not few[b])
+
+
 @pytest.mark.parametrize("tokens,before,kw", [([1, 1], [2999, 40000], {}), ([40], [6000], {}), ([1] * 80, [700] * 80, {}),
                                               ([150, 1, 1], [3000, 5000, 20], {"pad": 2})])
 def test_attention_is_that_of_the_values(tokens, before, kw):
@@ -543,7 +584,7 @@ def test_in_a_graph():
         qkv = torch.zeros((B, (Hq + 2 * Hkv) * 128), dtype=torch.float16, device=DEV)
         q = torch.zeros((B, Hq, 128), dtype=torch.float16, device=DEV)
         out = torch.zeros_like(q)
-        ws = torch.empty(max(laq.paged_attention_workspace_bytes(B, B, Hq, Hkv, width * ps), 16), dtype=torch.uint8, device=DEV)
+        ws = torch.empty(max(laq.paged_attention_e4m3_workspace_bytes(B, B, Hq, Hkv, width * ps), 16), dtype=torch.uint8, device=DEV)
 
         def step():
             laq.paged_append_e4m3(qkv, None, None, cs, k, v, ks, vs, table, start, lens, Hq, EPS, q_out=q)
@@ -583,7 +624,7 @@ def test_two_streams_at_once():
         bt = Batch8(rng, tokens, before, 16, Hkv)
         q = dev(f16(rng, (bt.T, Hq, 128)))
         d = bt.device8()
-        nbytes = laq.paged_attention_workspace_bytes(len(tokens), bt.T, Hq, Hkv, d[4].shape[1] * 16)
+        nbytes = laq.paged_attention_e4m3_workspace_bytes(len(tokens), bt.T, Hq, Hkv, d[4].shape[1] * 16)
         sets.append((q, d, torch.empty(nbytes, dtype=torch.uint8, device=DEV), torch.zeros_like(q)))
         alone.append(laq.paged_attention_e4m3(q, *d))
     torch.cuda.synchronize()

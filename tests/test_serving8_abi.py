@@ -88,7 +88,8 @@ def test_append_refusals(L):
 
 def test_attention_refusals(L):
     big = dict(table_pages=1000, table_stride=1000)
-    need = L.laq_paged_attention_workspace_bytes(2, 3, 32, 8, 16000)
+    need = L.laq_paged_attention_e4m3_workspace_bytes(2, 3, 32, 8, 16000)
+    assert need > 0
     for f in ("q", "out"):
         assert attention(L, **{f: 0}) == laq.LAQ_ERR_NULL_POINTER
     assert attention(L, ws=0, **big) == laq.LAQ_ERR_NULL_POINTER
@@ -100,6 +101,22 @@ def test_attention_refusals(L):
         assert attention(L, **{f: FAKE + o}) == laq.LAQ_ERR_MISALIGNED
     for Hq, Hkv, B, T in ((1024, 1024, 1 << 20, 1 << 20), (16, 16, 1 << 20, (1 << 26) - 1)):
         assert attention(L, Hq=Hq, Hkv=Hkv, B=B, T=T) == laq.LAQ_ERR_BAD_SHAPE
+
+
+def test_attention_workspace_query(L):
+    f, f16 = L.laq_paged_attention_e4m3_workspace_bytes, L.laq_paged_attention_workspace_bytes
+    for args in ((0, 1, 8, 8, 100), (1, 0, 8, 8, 100), (1, 1, 0, 8, 100), (1, 1, 8, 3, 100), (1, 1, 8, 8, 0),
+                 (KMAX, 1, 8, 8, 100), (1, KMAX, 8, 8, 100), (1, 1, KMAX, 1, 100), (1, 1, 8, KMIN, 100),
+                 (1, 1, 8, 8, KMAX), (KMIN, KMIN, KMIN, KMIN, KMIN)):
+        assert f(*args) == 0
+    assert f(1, 1, 64, 8, 512) == 0 < f(1, 1, 64, 8, 1024)  # not split; split
+    for Hkv in (1, 2, 3, 8, 40, 512, 4096):
+        for R in (1, 3, 5, 8, 24):
+            for B in (1, 2, 3, 7, 64, 65, 300):
+                for T in (1, 2, 16, 17, 33, 129, 700, 5000, 40000):
+                    for capacity in (16, 300, 600, 1100, 4096, 1 << 20, 1 << 30):
+                        if Hkv * R <= 4096:
+                            assert 0 <= f(B, T, Hkv * R, Hkv, capacity) <= f16(B, T, Hkv * R, Hkv, capacity), (B, T, R, Hkv)
 
 
 ADJUST = ("history", "history_len", "prompt_len", "history_stride", "history_room", "repetition", "frequency", "presence",
