@@ -61,6 +61,11 @@ __device__ __forceinline__ float row_max(float v) {
   v = fmaxf(v, dpp_f<0x141>(v));
   return fmaxf(v, dpp_f<0x140>(v));
 }
+// The larger, NaN where one is: one instruction for three numbers, while fmaxf
+// first quiets each that may be a signalling NaN, as it holds a matrix product to
+// be.  (Measured on MI355X, two prompts of 8192 and 4001 rows, e4m3
+// codes, 32:8 heads: 728 -> 705 us.)
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // Inclusive prefix sum over the 64 lanes: shifts by 1, 2, 4, 8 within each
 // 16-lane row (lanes shifted in read 0), then the rows' totals.
 __device__ __forceinline__ int wave_scan(int v, int lane) {
@@ -426,8 +431,7 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // Tiles of keys and values go memory -> registers -> LDS, two buffers, so that
 // a tile's loads are in flight while the one before is computed and a block
 // meets once per tile.  Piece p (16 bytes) of key row r sits at p ^ (r & 15)
-// and of value row r at p ^ 4 (r & 3) (codes, whose rows are stored two pieces a
-// lane: ^ (r & 1) too): reads and stores touch each bank once.
+// and of value row r at p ^ 4 (r & 3): the operand reads touch each bank once.
 constexpr int kTile = 64;
 constexpr int kTileBytes = kTile * kHeadDim * 2;
 template <class C, int WAVES>
@@ -553,6 +557,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
   const int whole_last = max(min(sp.all_hi, sp.hi) - sp.lo, 0) / kTile;
   auto is_masked = [&](int t) { return (bad_of(t) != 0) | (t < whole_first) | (t >= whole_last); };
   // Codes of a row to LDS as two pieces of fp16, whose places go by XOR with `swap`.
+  // (Two lanes' stores meet in a bank; with half of the lanes beginning at the odd
+  // piece none do, but the selects cost as much.)
   auto store_codes = [&](char* d, int row, const u32x4& r, float scale, int swap) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -587,7 +593,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
           if (nan_codes(r.x) | nan_codes(r.y) | nan_codes(r.z) | nan_codes(r.w)) flags[t & 3] = t;
           r = u32x4{number_codes(r.x), number_codes(r.y), number_codes(r.z), number_codes(r.w)};
         }
-        store_codes(d, kPass * i + sr, r, scale_of(set_vs, old_vs, t, i), 4 * (sr & 3) ^ (sr & 1));
+        store_codes(d, kPass * i + sr, r, scale_of(set_vs, old_vs, t, i), 4 * (sr & 3));
       }
       return;
     }
@@ -649,14 +655,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
     float m4[4];  // four chains
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      m4[i] = fmaxf(s[0][i], s[1][i]);
+      m4[i] = maximum(s[0][i], s[1][i]);
 #pragma unroll
-      for (int r = 4; r < 16; r += 4) m4[i] = fmaxf(m4[i], fmaxf(s[0][r + i], s[1][r + i]));
+      for (int r = 4; r < 16; r += 4) m4[i] = maximum(maximum(m4[i], s[0][r + i]), s[1][r + i]);
     }
-    float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+    float mx = maximum(maximum(m4[0], m4[1]), maximum(m4[2], m4[3]));  // (of a row with a NaN score all is NaN)
     auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, mx), __builtin_bit_cast(uint32_t, mx), false,
                                               false);
-    mx = fmaxf(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
+    mx = maximum(__builtin_bit_cast(float, (uint32_t)x[0]), __builtin_bit_cast(float, (uint32_t)x[1])) * kScaleLog2;
     // (the difference, which is exact where they are near: ref + 7 may be rounded to ref + 8)
     const bool ahead = mx - ref > kLagLog2;
     scale = kScaleLog2;
@@ -709,7 +715,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
   // Value sums: 16 lanes read 4 positions x 16 dimensions and receive a column each.
   const int vrow = 4 * h + (lane & 15) / 4;
   const int vcol = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);  // dimension within 32
-  const int vswap = 4 * (vrow & 3) ^ (kCodes ? vrow & 1 : 0);
   auto value_sums = [&](const half8_t(&pf)[4], int B) {
     typedef short short4_t __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) short4_t lds_short4;
@@ -719,7 +724,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         const int piece = (32 * d + vcol) >> 3;
-        const char* const a = vd + (16 * ks + vrow) * 256 + 16 * (piece ^ vswap) + 2 * (vcol & 7);
+        const char* const a = vd + (16 * ks + vrow) * 256 + 16 * (piece ^ (4 * (vrow & 3))) + 2 * (vcol & 7);
         const short4_t x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a));
         const short4_t x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(a + 8 * 256));
         const half8_t v = __builtin_bit_cast(half8_t, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));

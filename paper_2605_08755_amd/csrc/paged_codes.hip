@@ -490,9 +490,10 @@ __device__ __forceinline__ void CacheE4M3::rows16_item(const PagedCodes& pb, con
         }
       }
     }
-    float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                     fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-    mx = over_quarters(mx, [](float a, float b) { return fmaxf(a, b); });
+    float mx = maximum(maximum(sc[0][0], sc[0][1]), sc[0][2]);
+    mx = maximum(maximum(mx, sc[0][3]), sc[1][0]);
+    mx = maximum(maximum(mx, sc[1][1]), maximum(sc[1][2], sc[1][3]));  // (of a row with a NaN score all is NaN)
+    mx = over_quarters(mx, [](float a, float b) { return maximum(a, b); });
     const bool ahead = mx - ref > kLag;
     if (__ballot(ahead)) {
       const float to = ahead ? mx - kBelow : ref;  // each query by itself
