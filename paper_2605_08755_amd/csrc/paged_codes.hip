@@ -126,8 +126,9 @@ __device__ __forceinline__ float wave_max(float v) {
 // whole block and the scale needs no exchange between waves); or one row and
 // every q_waves-th group of eight query heads.  Eight lanes a row or head: lane i
 // holds dimensions 8i .. 8i + 7 and their partners.  What bounds it: the bytes of
-// the rows in and out where there are many; few rows are a launch and the chain
-// of dependent reads: sequence, page, the block's old scale.
+// the rows in and out where there are many (16384 rows, 32:8 heads: 78 us, 4.8
+// TB/s on MI355X, a large copy moves 5.2); few rows are a launch and the chain of
+// dependent reads: sequence, page, the block's old scale (16 rows: 4.4 us).
 __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedCodes pb, const uint16_t* __restrict__ qkv,
                                                                  int64_t qkv_stride, const uint16_t* __restrict__ qw,
                                                                  const uint16_t* __restrict__ kw,
@@ -281,7 +282,10 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedCodes pb, 
 // is the sum of two fp16 numbers, and each value product two instructions.
 // Piece p (16 bytes) of key row r sits at p ^ (r / 2 & 7) and of value row r at
 // p ^ (r / 2 & 3 | r / 16 << 2): the operand reads touch each bank once.
-// Two blocks per compute unit.
+// Two blocks per compute unit.  (Measured on MI355X, kernel alone: sequences of
+// 131072, 120002, 77777 and 901 positions, 64:8 heads, 107 us, 6.3 TB/s, a plain
+// read reaches 7.0; 16 of up to 8192, 32:8, 21 us, 4.1 TB/s; one of 300, 64:8, not
+// split, 8 to 9 us.)
 constexpr int kStep = 32;
 constexpr int kStepBytes = kStep * kHeadDim;  // of keys; and of values
 constexpr int kStreamed = 2;                  // keys and values pass once: loads that do not keep their lines

@@ -260,6 +260,7 @@ class BatchStep:
                   laq.paged_attention_e4m3_workspace_bytes)(B, T, Hq, Hkv, capacity)
         self.workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
         self.logits = self.u = None
+        assert lm_head is not None or not (history or biases or grammar), "what sample() applies needs an LM head"
         if lm_head is not None:
             self.logits = torch.empty((T, shape["vocab"]), **f16)
             self.u = torch.zeros((T,), **f32)

@@ -306,6 +306,66 @@ def test_attention_every_code_and_scale(few):
         assert np.array_equal(got[i][fine], want[fine]), scales[i]
 
 
+@pytest.mark.parametrize("tokens,before,Hq,Hkv,kw", [
+    ([1, 1], [50, 61], 8, 2, {}),
+    ([1], [2100], 16, 2, {}),                              # split over ranges of positions
+    ([1, 1, 150, 1, 2], [33, 60, 20, 47, 40], 8, 2, {}),   # decoding rows beside a chunk
+    ([1, 1], [50, 61], 8, 2, {"pad": 60}),                 # decoding rows of a batch with padding
+    ([4], [44], 4, 1, {"pad": 1}),                         # 16 query rows
+])
+def test_attention_of_few_rows_keeps_22_bits(tokens, before, Hq, Hkv, kw):
+    """Sequences of up to 16 query rows a key/value head, whatever stands beside
+    them: probabilities are not rounded to 16 bits.
+
+    Scores are small sums of four products and values are +1 and -1, as many of
+    the one as of the other, so that outputs are near 0 and their own fp16
+    rounding is small.  The bound, relative to the weights' sum of |v| = 1: scores
+    are fp32 sums (136 x 2^-24 of the sum of magnitudes, in a weight and in the
+    denominator), L x 2^-24 in the value sums and in the denominator, 2^-20 of a
+    probability cut off (2^-10 of its first part's remainder, itself below 2^-10),
+    and the rounding of the output, 2^-11 of it."""
+    say("few rows8", tokens, Hq, kw)
+    rng = np.random.default_rng(sum(tokens) + sum(before) + Hq)
+    bt = Batch8(rng, tokens, before, 16, Hkv, **kw)
+    bt.vs[:] = 127
+    for b, n in enumerate(bt.lens):
+        for g in range(Hkv):
+            signs = np.array([rng.permutation(np.resize([0x38, 0xB8], n)) for _ in range(128)])
+            for t in range(n):
+                bt.vc[bt.table[b, t // 16], g, t % 16] = signs[:, t]
+    bt.values()
+    q = np.zeros((bt.T, Hq, 128), dtype=np.float16)
+    q[..., 5::32] = f16(rng, (bt.T, Hq, 4), 0.5)
+    got = attend(bt, q).astype(np.float64)
+    ref, weight, reach = OS.paged_attention(q, bt.k, bt.v, bt.table, bt.start, bt.lens, 0, np.zeros_like(got))
+    few = small(bt, Hq)
+    mine = [(r, pos) for r, b, pos in OS.rows(bt.start, bt.lens) if few[b]]
+    rows = [r for r, _ in mine]
+    assert len(rows) >= 1 and np.allclose(weight[rows], 1)
+    L = np.array([pos + 1 for _, pos in mine])[:, None, None]
+    tol = 2.0**-11 * np.abs(ref[rows]) + 2 * 136 * 2.0**-24 * reach[rows][..., None] + 2 * L * 2.0**-24 + 2.0**-20 + 2.0**-25
+    err = np.abs(got[rows] - ref[rows])
+    assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("tokens,before", [([1, 1], [60, 1500]), ([40], [90]), ([300, 1], [50, 700])])
+def test_attention_huge_scores(tokens, before):
+    """Scores from 2^20 on, some a few steps of 32 bits apart: all values are 1, so
+    that outputs are 1 whatever the weights (each probability's rounding 2^-11 of
+    it, the output's 2^-11, sums over L positions 2 L x 2^-24)."""
+    say("huge scores8", tokens)
+    rng = np.random.default_rng(5 + sum(tokens))
+    bt = Batch8(rng, tokens, before, 16, 2)
+    bt.ks[:] = rng.choice([126, 131, 134], bt.ks.shape)
+    bt.vs[:] = 127
+    bt.vc[np.broadcast_to(bt.used[:, None], bt.vc.shape[:3])] = 0x38
+    q = f16(rng, (bt.T, 4, 128), 2000.0)
+    got = attend(bt, q)
+    mine = slice(bt.start[0], bt.start[-1])
+    tol = 2 * 2.0**-11 + 2 * int(bt.lens.max()) * 2.0**-24
+    assert (np.abs(got[mine].astype(np.float64) - 1) <= tol).all()
+
+
 CASES = [
     # decoding: one row a sequence, lengths around steps, blocks and ranges
     (32, 8, 16, [1], [0], 0, {}),
