@@ -633,8 +633,9 @@ laq_status laq_paged_attention_f16(const laq_paged_batch *batch, const void *q, 
  * bytes outside are taken as the nearer of the two. */
 
 /* laq_paged_append_e4m3 -- laq_paged_append_f16 into a cache of 8 bits: q_out as
- * there; keys (normalized and rotated, in fp32) and values become codes.  For every block of 16 positions that gets new rows, and each
- * of keys and values of a head:
+ * there; keys (normalized and rotated, in fp32) and values become codes.  For
+ * every block of 16 positions that gets new rows, and each of keys and values of
+ * a head:
  *   scale = the least of 112..134 with max |x| <= 448 * 2^(scale - 127), x the
  *           block's new values that are finite; not below the scale that the
  *           block has, when it holds earlier positions of the sequence, whose
@@ -682,7 +683,8 @@ typedef struct laq_logits_adjust {
     /* tokens so far: row r's are history[r * history_stride + i], i <
      * history_len[r] (taken into 0..history_room), the first prompt_len[r] of
      * them the prompt's and the others generated (NULL: all are generated).
-     * Entries outside 0..V-1 name nothing. */
+     * Entries outside 0..V-1 name nothing.  A row's history_room entries are
+     * memory that may be read, whatever its length is. */
     const int32_t *history;
     const int32_t *history_len; /* [rows] */
     const int32_t *prompt_len;  /* [rows], or NULL */
@@ -719,8 +721,9 @@ typedef struct laq_logits_adjust {
  * rows == 0: nothing is done.
  * Errors: NULL_POINTER (adjust, logits, out; history without history_len,
  * bias_token without bias_value); BAD_SHAPE (V outside 1..2^24, rows < 0 or >=
- * 2^22, sizes above, strides of logits and out below V or above 2^32, partial
- * overlap, logits that would take 2^32 threads and more); MISALIGNED (logits
+ * 2^22, sizes above, strides of logits and out below V (of several rows) or
+ * above 2^32, partial overlap, logits that would take 2^32 threads and more);
+ * MISALIGNED (logits
  * and out 2-byte, the others 4-byte). */
 laq_status laq_adjust_logits_f16(const laq_logits_adjust *adjust, const void *logits, int64_t logits_stride,
                                  int64_t rows, int64_t V, void *out, int64_t out_stride, void *stream);

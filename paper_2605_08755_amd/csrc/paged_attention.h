@@ -1,7 +1,7 @@
 // Attention over paged key/value caches: what its kernels share for every type
 // of cache.  The work of a batch and its division into items, the kernel for
-// prompts' chunks (256 query rows a block), the joining of split sequences, and
-// the sizes that follow.  fp32 sums and softmax statistics, fixed reduction
+// prompts' chunks (256 or 128 query rows a block), the joining of split
+// sequences, and the sizes that follow.  fp32 sums and softmax statistics, fixed reduction
 // orders (deterministic).  Head dimension 128.
 //
 // A batch of B sequences: sequence b owns rows token_start[b] ..
@@ -30,7 +30,6 @@ constexpr float kNoMax = -1e30f;  // running maximum before the first visible sc
 
 typedef float float16_t __attribute__((ext_vector_type(16)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
-
 
 __device__ __forceinline__ int readlane(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -338,10 +337,11 @@ __device__ __forceinline__ Span span_of(const Item& it, int j0, int j1, int wind
 }
 
 // Sixteen positions from t on (t a multiple of 16, in one page) of one head of a
-// cache whose elements take BYTES, in bytes from the head's first row: rows from `end` on, and all rows of a page
-// that is not there, lie past the extent and read as zeros.  Scalar arithmetic
-// without branches: it stands before every tile's loads (page and slot strides
-// are below 2^32 bytes, so the products are 32 x 32 -> 64 bits).
+// cache whose elements take BYTES, in bytes from the head's first row: rows from
+// `end` on, and all rows of a page that is not there, lie past the extent and
+// read as zeros.  Scalar arithmetic without branches: it stands before every
+// tile's loads (page and slot strides are below 2^32 bytes, so the products are
+// 32 x 32 -> 64 bits).
 struct Rows16 {
   uint64_t at;
   uint32_t bytes;
@@ -393,8 +393,8 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // attention of prompts' chunks: the matrix cores bound it
 // ---------------------------------------------------------------------------
 
-// A block of eight waves holds 256 query rows of one item, 32 a wave, and walks
-// the positions in tiles of 64.  Scores are formed transposed, keys (rows) x
+// A block of eight or four waves holds the query rows of one item, 32 a wave, and
+// walks the positions in tiles of 64.  Scores are formed transposed, keys (rows) x
 // queries (columns), so that a lane holds 32 scores of one query: the running
 // maximum and the denominator need one exchange between the two halves of the
 // wave, and the probabilities are already the second product's operand
@@ -409,8 +409,8 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // the fp32 sum of the unrounded ones.
 // A sequence of up to 16 rows (decoding rows beside a chunk, or of a batch with
 // much padding) would fill half a wave's rows: the block takes its items as the
-// 16-row kernel does, with probabilities in 32 bits and eight waves along the
-// positions.  Its records have the place of 256 rows.  (Measured on MI355X: a
+// 16-row kernel does, with its probabilities and all waves along the positions.
+// Its records have the place of a block's rows.  (Measured on MI355X: a
 // chunk beside 15 decoding rows 77.8 -> 78.2 us; two waves more for the
 // probabilities' remainders instead, 84.8.)
 //
@@ -420,8 +420,9 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // 42 % of the SIMDs' cycles, vector instructions 48 %; LDS active 27 % of the
 // compute units' cycles, no bank conflicts.  Kernel alone, without the joining:
 // 874 us, 780 TFLOP/s, the median of 24 calls under a kernel trace, 823 the
-// shortest; a call with the joining 768 to 804, 847 to 887 TFLOP/s, untraced; a
-// library's fp16 8192^3 product reaches 1150.  As two blocks of 128 rows, with
+// shortest, before the maxima were single instructions; a call with the joining
+// 750 to 793, 859 to 908 TFLOP/s, untraced, 705 to 730 over codes; a library's
+// fp16 8192^3 product reaches 1150.  As two blocks of 128 rows, with
 // twice the staging instructions, 945.  With 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
 // exponentials, 850 the value sums, 1100 issuing the next tile's loads and
@@ -835,8 +836,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
 // Joins the ranges of the split tiles in position order.  Records are weighted
 // by 2^(their maximum - the largest of all); a lane holds two dimensions.
 // WAVES == 4: a block takes a row at a time (every gridDim.y-th of its tile), its
-// waves every fourth record, and they meet in LDS (decoding: few rows, many ranges).  WAVES == 1: a wave per four rows,
-// 16 rows a block at a time (a chunk's rows have few ranges each).  Most blocks
+// waves every fourth record, and they meet in LDS (decoding: few rows, many
+// ranges).  WAVES == 1: a wave per four rows, 16 rows a block at a time (a chunk's
+// rows have few ranges each).  Most blocks
 // of the grid can find nothing to do and cost their search, so there are about
 // kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
 // prompts whose tiles are not split, 16.4 -> 4.9 us; a chunk beside 15 decoding

@@ -625,6 +625,48 @@ def test_far_pages():
         assert torch.equal(a.view(torch.uint8)[far:], b.view(torch.uint8))
 
 
+def test_shared_pages():
+    """Sequences with the same pages in front (a shared prompt), the same sequence
+    twice, and appends behind the shared pages: as with pages of their own."""
+    say("shared pages8")
+    rng = np.random.default_rng(31)
+    Hq, Hkv, ps = 8, 2, 16
+    for tokens, before in (([1, 1, 1], [80, 83, 95]), ([20, 1, 33], [64, 70, 66])):
+        bt = Batch8(rng, tokens, before, ps, Hkv)
+        for b in (1, 2):  # the first four pages of all hold the same
+            for x in (bt.kc, bt.vc, bt.ks, bt.vs):
+                x[bt.table[b, :4]] = x[bt.table[0, :4]]
+        bt.values()
+        own = bt.device8()
+        table = bt.table.copy()
+        table[1:, :4] = table[0, :4]
+        shared = own[:4] + (dev(table),) + own[5:]
+        shared = tuple(t.clone() for t in shared)
+        qkv = dev(f16(rng, (bt.T, (Hq + 2 * Hkv) * 128)))
+        cs = decode.rope_table(300, 1e6, DEV)
+        outs = []
+        for d in (own, shared):
+            q = laq.paged_append_e4m3(qkv, None, None, cs, *d, Hq, EPS)
+            outs.append((q, laq.paged_attention_e4m3(q, *d)))
+        torch.cuda.synchronize()
+        for x, y in zip(*outs):
+            assert torch.equal(x, y)
+        for x, y in zip(own[:4], shared[:4]):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    # one sequence's new row as two sequences of a batch
+    bt = Batch8(rng, [1], [700], ps, Hkv)
+    q = f16(rng, (1, Hq, 128))
+    kc, vc, ks, vs, table, _, lens = bt.device8()
+    twice = laq.paged_attention_e4m3(dev(np.repeat(q, 2, 0)), kc, vc, ks, vs, table.repeat(2, 1), dev(np.array([0, 1, 2], np.int32)),
+                                     lens.expand(2).contiguous())
+    assert torch.equal(twice[0], twice[1])
+    once = attend(bt, q)[0].astype(np.float64)
+    # (ranges may differ: both outputs' roundings, 2^-20 of |v| cut off each, sums over 701 positions in 32 bits)
+    size = np.abs(bt.v.transpose(0, 2, 1, 3)[bt.used].astype(np.float64)).max()
+    tol = 2.0**-10 * np.abs(once) + 2 * size * 2.0**-20 + 4 * 701 * 2.0**-24 * size
+    assert (np.abs(twice[0].cpu().numpy().astype(np.float64) - once) <= tol).all()
+
+
 def test_in_a_graph():
     """Append and attention captured once; the replays follow the arrays that
     change between them."""
@@ -810,6 +852,50 @@ def test_adjust_parts():
     assert (got == -np.inf).all()
     tok, prob = laq.sample(dev(got), dev(np.zeros(R, dtype=np.float32)))
     assert bool((tok == -1).all()) and not prob.any()
+
+
+def test_adjust_far_rows():
+    """Rows that begin past 2^32 elements, in place and from there to others, and
+    more rows than 2^16."""
+    say("adjust far rows")
+    rng = np.random.default_rng(9)
+    R, V, stride = 3, 4001, 2**31 + 24
+    logits, a = adjust_case(rng, R, V, 200, 5, True)
+    want = laq.adjust_logits(dev(logits), **to_dev(a))
+    far = torch.empty(2 * stride + V, dtype=torch.float16, device=DEV).as_strided((R, V), (stride, 1))
+    near = torch.zeros((R, V), dtype=torch.float16, device=DEV)
+    far.copy_(dev(logits))
+    laq.adjust_logits(far, **to_dev(a), out=near)
+    laq.adjust_logits(far, **to_dev(a), out=far)
+    torch.cuda.synchronize()
+    assert torch.equal(near.view(torch.int16), want.view(torch.int16))
+    assert torch.equal(far.contiguous().view(torch.int16), want.view(torch.int16))
+    del far
+    R, V = 70001, 3
+    logits, a = adjust_case(rng, R, V, 6, 2, True)
+    got = laq.adjust_logits(dev(logits), **to_dev(a)).cpu().numpy()
+    picked = np.unique(np.concatenate([rng.integers(0, R, 300), [0, 65535, 65536, R - 1]]))
+    adjust_check(logits[picked], {k: None if v is None else v[picked] for k, v in a.items()}, got[picked])
+
+
+def test_adjust_on_two_streams():
+    """Two calls at once, each on a stream of its own: what each gives alone."""
+    say("adjust two streams")
+    rng = np.random.default_rng(10)
+    sets = []
+    for R, V, H in ((5, 20001, 900), (40, 3000, 50)):
+        logits, a = adjust_case(rng, R, V, H, 7, True)
+        x, d = dev(logits), to_dev(a)
+        sets.append((x, d, torch.zeros_like(x), laq.adjust_logits(x, **d)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(20):
+        for s, (x, d, out, _) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                laq.adjust_logits(x, **d, out=out)
+    torch.cuda.synchronize()
+    for _, _, out, want in sets:
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16))
 
 
 def test_adjust_in_a_graph():
