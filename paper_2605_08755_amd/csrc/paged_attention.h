@@ -837,18 +837,23 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
 // by 2^(their maximum - the largest of all); a lane holds two dimensions.
 // WAVES == 4: a block takes a row at a time (every gridDim.y-th of its tile), its
 // waves every fourth record, and they meet in LDS (decoding: few rows, many
-// ranges).  WAVES == 1: a wave per four rows, 16 rows a block at a time (a chunk's
-// rows have few ranges each).  Most blocks
+// ranges).  WAVES == 1: a wave per kJoinRows rows, four times that a block at a
+// time (a chunk's rows have few ranges each).  Most blocks
 // of the grid can find nothing to do and cost their search, so there are about
 // kJoinBlocks of them, which go on to further rows.  (Measured on MI355X: two
-// prompts whose tiles are not split, 16.4 -> 4.9 us; a chunk beside 15 decoding
-// rows, 14.5 -> 15.5, of the bytes of its records; twice the blocks, 8.7 and 17.)
+// prompts whose tiles are not split, 16.4 -> 4.9 us.)  A wave of two rows and two
+// records at a time takes few registers, so that all blocks run at once.  (Calls
+// over codes, 4 rows and 4 records a wave -> 4 and 2 -> 2 and 2 -> 1 and 4: a chunk
+// of 500 rows beside 15 decoding ones, 40:8 heads, 68.5 -> 65.2 -> 63.6, 66.0 ->
+// 61.2 -> 62.7; 1024 rows at 0, 32:8, 41 -> 36 -> 34 -> 38; 512 at 2000, 64:8, 72 ->
+// 68 -> 65 -> 68.  Twice the blocks: 63.0, 34.7 and 64.9.)
+constexpr int kJoinRows = 2;
 template <int BM, bool TILE, int WAVES>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
   constexpr int kRec = BM * (kHeadDim + 2);
-  constexpr int kRows = WAVES == 4 ? 1 : 4;  // rows of a wave
-  constexpr int kB = WAVES == 4 ? 8 : 4;     // records loaded at a time
+  constexpr int kRows = WAVES == 4 ? 1 : kJoinRows;  // rows of a wave
+  constexpr int kB = WAVES == 4 ? 8 : 2;             // records loaded at a time
   const int lane = threadIdx.x & 63;
   const int w = uniform(threadIdx.x >> 6);
   const int at_item = uniform(blockIdx.x / Hkv), g = (int)blockIdx.x - at_item * Hkv;
@@ -858,9 +863,9 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
   const int rows = min(it.n * R - r0, BM);
   const int first = WAVES == 4 ? w : 0;
   const float* const base = o_.ws + ((int64_t)g * o_.rec_bound + it.rec) * kRec;
-  // WAVES == 4: every gridDim.y-th row, the same for the whole block; else group of 16
+  // WAVES == 4: every gridDim.y-th row, the same for the whole block; else group of 4 kRows
 #pragma unroll 1
-  for (int row = WAVES == 4 ? blockIdx.y : blockIdx.y * 16 + w * 4; row < rows; row += (WAVES == 4 ? 1 : 16) * gridDim.y) {
+  for (int row = WAVES == 4 ? blockIdx.y : (blockIdx.y * 4 + w) * kRows; row < rows; row += (WAVES == 4 ? 1 : 4 * kRows) * gridDim.y) {
     const float *stat[kRows], *sums[kRows];
     float2_t x[kRows][kB], st[kRows][kB], num[kRows];
     float M[kRows], den[kRows];
@@ -995,13 +1000,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_attention_rows16_kernel(
 
 template <class C, int BM>
 void launch_chunks(const typename C::Batch& pb, const uint16_t* q, int64_t R, int64_t Hkv, int64_t window, const Out& o,
-                   dim3 grid, dim3 join, bool by_16, hipStream_t stream, const LaunchEvents& e1, const LaunchEvents& e2) {
+                   dim3 grid, dim3 join, bool by_group, hipStream_t stream, const LaunchEvents& e1, const LaunchEvents& e2) {
   const PagedBatch& rows = pb;
   constexpr int kWavesOf = BM / 32;
   launch((paged_attention_chunk_kernel<C, kWavesOf>), grid, dim3(64 * kWavesOf), kChunkLds<C, kWavesOf>, stream, e1, pb, q,
          (int)R, (int)Hkv, (int)window, o);
   if (join.x == 0) return;
-  if (by_16)
+  if (by_group)
     launch((paged_attention_join_kernel<BM, C::kTileRanges, 1>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
   else
     launch((paged_attention_join_kernel<BM, C::kTileRanges, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
@@ -1029,20 +1034,24 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
   }
   const Out o{out, ws, plan, (int)Hq, (int)p.records, p.min_chunk};
   const dim3 grid((unsigned)(p.items * Hkv));
-  // A block joins one row; 16 rows where the tiles (most of them not split) would
-  // make many blocks.  (Tiles of 128 rows, measured on MI355X, by row -> by 16: 8 of
-  // up to 8 ranges 3.9 -> 5.6 us, 16 of up to 25, 8.8 -> 14.2, of up to 16, 7.8 and
-  // 7.8, of up to 3, 7.7 -> 4.5; 32 of up to 9, 13.0 -> 7.0.)
+  // A block joins one row; 4 kJoinRows where the tiles (most of them not split)
+  // would make many blocks.  (Tiles of 128 rows, calls measured on MI355X, by row ->
+  // by 8: 5 tiles of up to 3 ranges 18.5 -> 17.4 us, of up to 9, 19.8 -> 20.5, of up
+  // to 17, 21.9 -> 25.1, of up to 65, 28.4 -> 42.7; 9 of up to 25, 30.7 -> 33.1.  The
+  // joining alone, by row -> by 16: 16 of up to 25, 8.8 -> 14.2, of up to 3, 7.7 ->
+  // 4.5; 32 of up to 9, 13.0 -> 7.0.)
   constexpr int64_t kJoinBlocks = 2048;
   const int64_t few_tiles = p.rows != kChunkRows<4> ? 32 : p.most_ranges >= 16 ? 16 : 8;
   const bool many = p.rows != kSmallRows && p.split_tiles * Hkv > few_tiles;
   const int64_t most_rows = std::min<int64_t>(p.rows, pb.T * R);
-  const int64_t by_16 = std::min((most_rows + 15) / 16, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
+  const int64_t groups = (most_rows + 4 * kJoinRows - 1) / (4 * kJoinRows);
+  const int64_t turns = (groups * (p.split_tiles * Hkv + 1) + kJoinBlocks - 1) / kJoinBlocks;
+  const int64_t by_group = (groups + turns - 1) / turns;  // (as many turns for each)
   // (A block per row where that is about as many as run at once, else fewer that
   // go on: where nothing is split, each costs its search.  Measured on MI355X, 64
   // sequences of 400 positions, 64:8 heads, e4m3 codes: 25 -> 19 us.)
   const int64_t by_row = std::min(most_rows, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
-  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_16 : by_row));
+  const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_group : by_row));
   if (p.rows == kSmallRows) {
     launch((paged_attention_rows16_kernel<C>), grid, dim3(64 * kWaves), C::template kItemLds<kWaves>, stream, e1, pb, q,
            (int)R, (int)Hkv, (int)window, o);
