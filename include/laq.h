@@ -717,14 +717,15 @@ typedef struct laq_logits_adjust {
  * the formulas give is what is written.
  *   out  [out] fp16 [rows][V], out_stride elements between rows: logits itself
  *        with the same stride (logits that nothing touches are then not
- *        written), or memory that does not overlap it.
+ *        written), or rows that share no element with the logits' rows (both
+ *        may be columns of one array).
  * rows == 0: nothing is done.
  * Errors: NULL_POINTER (adjust, logits, out; history without history_len,
  * bias_token without bias_value); BAD_SHAPE (V outside 1..2^24, rows < 0 or >=
  * 2^22, sizes above, strides of logits and out below V (of several rows) or
- * above 2^32, partial overlap, logits that would take 2^32 threads and more);
- * MISALIGNED (logits
- * and out 2-byte, the others 4-byte). */
+ * above 2^32, elements that logits and out share otherwise, logits that would
+ * take 2^32 threads and more); MISALIGNED (logits and out 2-byte, the others
+ * 4-byte). */
 laq_status laq_adjust_logits_f16(const laq_logits_adjust *adjust, const void *logits, int64_t logits_stride,
                                  int64_t rows, int64_t V, void *out, int64_t out_stride, void *stream);
 

@@ -663,10 +663,22 @@ laq_status check_attention(const char* fn, const laq_paged_batch* batch, const v
   return LAQ_OK;
 }
 
-// Bytes [a, a + an) and [b, b + bn) have some in common.
-bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
+// Some element lies both in the rows [a + i as, + V) and in the rows [b + j bs, + V),
+// i and j below `rows`; strides of V and more (or one row), so that rows of either
+// follow one another.  Steps past the rows that end first, as far as they meet
+// others: no more than 2 rows steps, and one where the arrays lie apart.
+bool overlap(const uint16_t* a, int64_t as, const uint16_t* b, int64_t bs, int64_t rows, int64_t V) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+  auto row = [](uintptr_t p, int64_t stride, int64_t i) { return p + 2 * (uintptr_t)(i * stride); };
+  const uintptr_t width = 2 * (uintptr_t)V;
+  if (row(x, as, rows - 1) + width <= y || row(y, bs, rows - 1) + width <= x) return false;
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
+    const uintptr_t p = row(x, as, i), q = row(y, bs, j);
+    if (p + width <= q) ++i;
+    else if (q + width <= p) ++j;
+    else return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -786,8 +798,8 @@ laq_status laq_adjust_logits_f16(const laq_logits_adjust* adjust, const void* lo
                         (const void*)a.bias_token, (const void*)a.bias_value, (const void*)a.mask})
     if (!aligned(p, 4)) return fail(LAQ_ERR_MISALIGNED, fn, "the arrays of adjust must be 4-byte aligned");
   const bool same = out == logits && (rows == 1 || out_stride == logits_stride);
-  if (!same && overlap(logits, ((rows - 1) * logits_stride + V) * 2, out, ((rows - 1) * out_stride + V) * 2))
-    return fail(LAQ_ERR_BAD_SHAPE, fn, "out must be logits itself or not overlap it");
+  if (!same && overlap(static_cast<const uint16_t*>(logits), logits_stride, static_cast<const uint16_t*>(out), out_stride, rows, V))
+    return fail(LAQ_ERR_BAD_SHAPE, fn, "out must be logits itself or share no element with it");
   laq::Adjust d{};
   d.logits = static_cast<const uint16_t*>(logits);
   d.out = static_cast<uint16_t*>(out);

@@ -756,7 +756,8 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
                   presence=None, bias_token=None, bias_value=None, mask=None, out=None):
     """Penalties, biases and a mask on fp16 logits [rows][V] (rows may be
     strided) before `sample`; returns out (fp16 [rows][V], new when not given;
-    logits itself: in place).  laq_adjust_logits_f16 of include/laq.h defines it.
+    logits itself: in place; columns beside them in the same array).
+    laq_adjust_logits_f16 of include/laq.h defines it.
 
     history int32 [rows][room] (rows may be strided or one expanded): the tokens
     so far, of which history_len int32 [rows] are there and the first prompt_len
