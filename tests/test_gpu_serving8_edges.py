@@ -6,11 +6,146 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2605_08755_amd import laq
+from oracle import serving as OS
+from oracle.compare import linear_check
+from paper_2605_08755_amd import decode, laq
 from test_gpu_serving import dev, f16, say
-from test_gpu_serving8 import DEV, adjust_case, adjust_check, to_dev
+from test_gpu_serving8 import DEV, EPS, Batch8, adjust_case, adjust_check, half_step, host, to_dev
 
 pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------------
+# append
+# ---------------------------------------------------------------------------
+def append_shape(T, Hq, Hkv):
+    """(rows of a window of the key and value waves, waves of a row's query
+    heads): windows of 1, 2, 4, 8 or 16 rows whose waves are at most 8192, and as
+    many query waves as 8192 leave a row, one per eight heads at most."""
+    window = 1
+    while window < 16 and -(-T // window) * 2 * Hkv > 8192:
+        window *= 2
+    return window, max(1, min((Hq + 7) // 8, 8192 // T))
+
+
+def append_all(rng, bt, qkv, qw, kw, cs, Hq, qkv_dev=None, start=None, table=None):
+    """An append on the batch's caches, everything that it writes against the
+    oracle: query rows and those of no sequence, scales, values' codes, new keys
+    (check_append's tolerance); and the key codes of all other positions, which
+    are as they were or, where their scale grew, the oracle's (NaN for NaN only).
+    start, table: what the call gets in the place of the batch's own."""
+    k, v, ks, vs, own_table, own_start, lens = bt.device8()
+    canary = f16(rng, (bt.T, Hq, 128))
+    q = laq.paged_append_e4m3(dev(qkv) if qkv_dev is None else qkv_dev, None if qw is None else dev(qw),
+                              None if kw is None else dev(kw), cs, k, v, ks, vs, own_table if table is None else table,
+                              own_start if start is None else dev(start), lens, Hq, EPS, q_out=dev(canary))
+    torch.cuda.synchronize()
+    want_q, want = OS.paged_append_e4m3(qkv, qw, kw, cs.cpu().numpy(), ((bt.kc, bt.ks), (bt.vc, bt.vs)), bt.table, bt.start,
+                                        bt.lens, Hq, EPS, canary)
+    q = q.cpu().numpy()
+    r = linear_check(q, want_q)
+    assert r["ok"], r
+    rest = np.setdiff1d(np.arange(len(q)), [r for r, _, _ in OS.rows(bt.start, bt.lens)])
+    assert np.array_equal(q[rest].view(np.uint16), canary[rest].view(np.uint16))
+    for name, codes, scales, (wcodes, wscales, exact) in zip("kv", (host(k), host(v)), (host(ks), host(vs)), want):
+        assert np.array_equal(scales, wscales), name
+        same = (codes == wcodes) | ((codes & 127) == 127) & ((wcodes & 127) == 127)
+        new = ~np.isnan(exact)
+        assert same[~new].all(), name
+        if name == "v":
+            assert same.all()
+            continue
+        x, got = exact[new.any(-1)], OS.e4m3_values()[codes[new.any(-1)]]  # [rows][128]
+        pair = np.hypot(x[:, :64], x[:, 64:])
+        slack = 2.0**-16 * np.concatenate([pair, pair], axis=-1)
+        x = np.clip(x, -448, 448)
+        assert (np.abs(got - x) <= half_step(np.abs(x) + slack) + slack).all()
+
+
+def append_inputs(rng, bt, Hq, Hkv):
+    """Rows of unlike magnitudes, norm weights."""
+    width = (Hq + 2 * Hkv) * 128
+    qkv = (rng.standard_normal((bt.T, width)) * np.exp(1.5 * rng.standard_normal((bt.T, 1)))).astype(np.float16)
+    return (qkv,) + tuple((1 + 0.2 * rng.standard_normal(128)).astype(np.float16) for _ in range(2))
+
+
+@pytest.mark.parametrize("window,q_waves,Hq,Hkv,ps,tokens,before,kw", [
+    (8, 8, 64, 64, 16, [300], [5], {}),
+    (8, 8, 64, 64, 32, [1, 2, 3, 0, 5, 40, 1, 1, 17, 225], [7, 15, 40, 0, 14, 3, 31, 16, 90, 11], {"pad": 3, "first": 2}),
+    (8, 8, 64, 64, 16, [1] * 290, [7 * i % 48 for i in range(290)], {}),
+    (16, 8, 64, 64, 16, [600], [9], {}),
+    (16, 8, 64, 64, 64, [37, 1, 500, 80], [30, 63, 5, 0], {"slot_major": True}),
+    (16, 8, 64, 64, 16, [1, 2, 0, 3, 20] * 23, [7, 15, 40, 30, 1] * 23, {"pad": 5, "first": 1}),
+    (16, 3, 32, 32, 16, [2100], [3], {}),          # three waves for four groups of eight query heads
+    (2, 1, 33, 1, 32, [2500, 1, 2499], [40, 17, 0], {}),  # one wave for five, the last of one head
+    (1, 2, 24, 1, 16, [4095], [1], {}),            # two for three
+])
+def test_append_windows(window, q_waves, Hq, Hkv, ps, tokens, before, kw):
+    """Windows of 8 and of 16 rows, with sequences that begin inside a block and
+    several in one window; query waves that go on to further groups of heads."""
+    say("append8 windows", window, q_waves, Hq, Hkv, ps, len(tokens), sum(tokens))
+    rng = np.random.default_rng(sum(tokens) + Hq + ps)
+    bt = Batch8(rng, tokens, before, ps, Hkv, garbage=None, spread=3, **kw)
+    assert append_shape(bt.T, Hq, Hkv) == (window, q_waves)
+    cs = decode.rope_table(int(bt.lens.max()) + 1, 1e6, DEV)
+    append_all(rng, bt, *append_inputs(rng, bt, Hq, Hkv), cs, Hq)
+
+
+@pytest.mark.parametrize("T,window", [(300, 8), (600, 16)])
+def test_append_windows_of_places_that_are_not_there(T, window):
+    """Missing pages and pages outside the cache, negative positions, positions
+    past the rotation table and past the page table, among the rows of a window;
+    row starts below 0 and past T."""
+    say("append8 windows, bad places", T)
+    rng = np.random.default_rng(T)
+    Hq = Hkv = 64
+    n = T // 6
+    tokens, before = [n] * 5 + [T - 5 * n], [3, 30, 17, 0, 9, 100]
+    bt = Batch8(rng, tokens, before, 16, Hkv, garbage=None)
+    assert append_shape(T, Hq, Hkv)[0] == window
+    bt.table[0, 1], bt.table[2, 2], bt.table[4, 0] = -1, bt.P, 2**31 - 1
+    bt.lens[1] = n - 7  # the first seven at negative positions
+    bt.lens[3] = -5     # all of them
+    bt.lens[5] = bt.table.shape[1] * 16 + 20  # the last 20 past the page table
+    inputs = append_inputs(rng, bt, Hq, Hkv)
+    start = bt.start.copy()
+    start[0], start[-1] = -50, T + 1000
+    for positions in (400, 70):
+        cs = decode.rope_table(positions, 1e6, DEV)
+        append_all(rng, bt, *inputs, cs, Hq)
+        append_all(rng, bt, *inputs, cs, Hq, start=start)
+
+
+def test_append_query_rows_of_views():
+    """Query rows where rows and page tables are views of wider arrays."""
+    say("append8 views")
+    rng = np.random.default_rng(2)
+    Hq, Hkv = 6, 2
+    bt = Batch8(rng, [5, 1, 18], [9, 40, 3], 16, Hkv, garbage=None)
+    qkv, qw, kw = append_inputs(rng, bt, Hq, Hkv)
+    wide = np.full((bt.T, qkv.shape[1] + 40), 9.0, dtype=np.float16)
+    wide[:, 8:8 + qkv.shape[1]] = qkv
+    table = torch.full((3, bt.table.shape[1] + 5), 77, dtype=torch.int32, device=DEV)
+    table[:, 2:2 + bt.table.shape[1]] = dev(bt.table)
+    append_all(rng, bt, qkv, qw, kw, decode.rope_table(64, 1e6, DEV), Hq, qkv_dev=dev(wide)[:, 8:8 + qkv.shape[1]],
+               table=table[:, 2:2 + bt.table.shape[1]])
+
+
+def test_append_keeps_key_codes():
+    """Every key code before a block's new row, NaN among them, kept where the
+    scale stays and rounded again where it grows; what belongs to others as it was."""
+    say("append8 key codes")
+    rng = np.random.default_rng(6)
+    Hq, Hkv, ps = 2, 2, 16
+    cs = torch.cat([torch.ones(600, 64), torch.zeros(600, 64)], dim=1).to(DEV).contiguous()  # no rotation
+    for grow in (0, 1, 2, 7, 11, 22):
+        bt = Batch8(rng, [1, 1, 3], [2, 15, 7], ps, Hkv, garbage=None)
+        bt.kc = rng.permutation(np.resize(np.arange(256, dtype=np.uint8), bt.kc.size)).reshape(bt.kc.shape)
+        bt.ks[:], bt.vs[:] = 112, 112
+        qkv = f16(rng, (bt.T, (Hq + 2 * Hkv) * 128)).astype(np.float64)
+        qkv = (np.clip(qkv, -4, 4) * 1.7 * 2.0**(grow - 15 + 6)).astype(np.float16)
+        qkv[:, Hq * 128] = 1.75 * 2.0**(grow - 15 + 8)  # the largest key of head 0 fits scale 112 + grow
+        append_all(rng, bt, qkv, None, None, cs, Hq)
 
 
 # ---------------------------------------------------------------------------
