@@ -9,8 +9,9 @@ import torch
 from oracle import serving as OS
 from oracle.compare import linear_check
 from paper_2605_08755_amd import decode, laq
-from test_gpu_serving import dev, f16, say
-from test_gpu_serving8 import DEV, EPS, Batch8, adjust_case, adjust_check, half_step, host, to_dev
+from test_gpu_serving import attention_check, dev, f16, say
+from test_gpu_serving8 import (DEV, EPS, Batch8, adjust_case, adjust_check, attend, half_step, host, small,
+                               to_dev)
 
 pytestmark = pytest.mark.gpu
 
@@ -146,6 +147,120 @@ def test_append_keeps_key_codes():
         qkv = (np.clip(qkv, -4, 4) * 1.7 * 2.0**(grow - 15 + 6)).astype(np.float16)
         qkv[:, Hq * 128] = 1.75 * 2.0**(grow - 15 + 8)  # the largest key of head 0 fits scale 112 + grow
         append_all(rng, bt, qkv, None, None, cs, Hq)
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+def check_picked(bt, Hq, q, got, picked, window=0):
+    """Some rows (row, sequence, position) of an attention against the definition in 64 bits."""
+    R, few = Hq // bt.Hkv, small(bt, Hq)
+    for r, b, pos in picked:
+        t = np.arange(max(0, pos - window + 1) if window else 0, pos + 1)
+        pages = bt.table[b, t // bt.ps]
+        t, pages = t[(pages >= 0) & (pages < bt.P)], pages[(pages >= 0) & (pages < bt.P)]
+        for g in range(bt.Hkv):
+            K, V = (c[pages, g, t % bt.ps].astype(np.float64) for c in (bt.k, bt.v))
+            x = q[r, R * g:R * (g + 1)].astype(np.float64)
+            s = x @ K.T / 128**0.5
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            weight, reach = p @ np.abs(V), (np.abs(x) @ np.abs(K).T).max(1) / 128**0.5
+            if few[b]:  # (2^-20 of the weights, with the output's own rounding)
+                weight, reach = weight * (1 + 2.0**-7), reach + 2.0
+            attention_check(got[r, R * g:R * (g + 1)], p @ V, weight, reach, len(t), not few[b])
+
+
+SCALES = list(range(112, 135)) + [0, 111, 135, 255]
+
+
+@pytest.mark.parametrize("n,Hq,Hkv", [(1, 2, 2), (20, 2, 2), (80, 64, 8)])
+def test_attention_every_key_code_and_scale(n, Hq, Hkv):
+    """A sequence for every scale, and those outside the range as its borders:
+    position t holds code t (of odd heads 128 + t) in dimension t alone, and rows
+    hold what makes each score a moderate number (as far as fp16 reaches), so that
+    every code weighs its position's values.  By the kernel of 16 rows, and those
+    of 128 and of 256 rows a block."""
+    say("attention8 key codes", n, Hq, Hkv)
+    rng = np.random.default_rng(n)
+    tokens = [n] * len(SCALES)
+    bt = Batch8(rng, tokens, [128] * len(SCALES), 16, Hkv)
+    assert {1: bt.T * Hq <= 16 * Hkv * len(tokens), 20: 16 * Hkv * len(tokens) < bt.T * Hq < 512 * 256,
+            80: bt.T * Hq >= 512 * 256}[n] and (n == 1 or n * (Hq // Hkv) > 16)
+    code = np.arange(128)
+    code[127] = 0  # (127 is NaN)
+    bt.kc[bt.used[:, None].repeat(Hkv, 1)] = 0  # the rows' own keys are 0
+    for i, s in enumerate(SCALES):
+        for g in range(Hkv):
+            for t in range(128):
+                bt.kc[bt.table[i, t // 16], g, t % 16, t] = code[t] + 128 * (g & 1)
+            bt.ks[bt.table[i, :8], g] = s
+    bt.values()
+    exponent = np.repeat([min(max(s, 112), 134) - 127 for s in SCALES], n)
+    size = np.ldexp(np.maximum(OS.e4m3_values()[code], 2.0**-9), exponent[:, None])  # [T][128]
+    wish = 2 * rng.standard_normal((bt.T, Hq, 128)) * 128**0.5 / size[:, None]
+    q = np.clip(wish, -60000, 60000).astype(np.float16)
+    got = attend(bt, q)
+    again = attend(bt, q)
+    assert np.array_equal(got.view(np.uint16), again.view(np.uint16))
+    rows = list(OS.rows(bt.start, bt.lens))
+    check_picked(bt, Hq, q, got, rows if n < 80 else [rows[n * i + j] for i in range(len(SCALES)) for j in (0, 37, n - 1)])
+
+
+@pytest.mark.parametrize("tokens,before,Hq", [([1, 1], [60, 1500], 4), ([40], [90], 4), ([300, 1], [50, 700], 4),
+                                              ([1] * 70, [40 + 9 * i for i in range(70)], 2)])
+def test_attention_huge_scores_choose_a_value(tokens, before, Hq):
+    """Scores from 2^20 on: where the largest is past all others by more than what
+    32 bits can be off (136 x 2^-24 of the products' magnitudes, each) and 30, the
+    output is the value of its position, e^-30 of the others apart."""
+    say("huge scores8, values", tokens[:3])
+    rng = np.random.default_rng(7 + sum(tokens))
+    bt = Batch8(rng, tokens, before, 16, 2)
+    bt.ks[:] = rng.choice([126, 131, 134], bt.ks.shape)
+    bt.values()
+    q = f16(rng, (bt.T, Hq, 128), 2000.0)
+    got = attend(bt, q).astype(np.float64)
+    clear = total = 0
+    for r, b, pos in OS.rows(bt.start, bt.lens):
+        t = np.arange(pos + 1)
+        for h in range(Hq):
+            K, V = (c[bt.table[b, t // 16], h // (Hq // 2), t % 16].astype(np.float64) for c in (bt.k, bt.v))
+            x = q[r, h].astype(np.float64)
+            s, off = K @ x / 128**0.5, 136 * 2.0**-24 * (np.abs(K) @ np.abs(x)) / 128**0.5
+            top = int(np.argmax(s))
+            rest = np.delete(s + off, top)
+            total += 1
+            if len(rest) and s[top] - off[top] - rest.max() <= 30:
+                continue
+            clear += 1
+            tol = 2.0**-10 * np.abs(V[top]) + 2.0**-25 + len(t) * np.exp(-30.0) * np.abs(V).max()
+            assert (np.abs(got[r, h] - V[top]) <= tol).all(), (r, h)
+    assert clear >= 0.9 * total
+
+
+@pytest.mark.parametrize("tokens,before,Hq,Hkv,window", [
+    ([1] * 80, [37 * i % 800 for i in range(79)] + [3000], 8, 2, 100),
+    ([1] * 80, [37 * i % 800 for i in range(79)] + [3000], 8, 2, 700),
+    ([2, 0, 1] * 60, [100, 5, 1400] * 60, 4, 4, 333),
+    ([5] * 40 + [300] + [5] * 30, [20] * 40 + [1500] + [100] * 30, 4, 2, 200),
+    ([1] * 50 + [170, 0, 33] * 6, [600] * 50 + [1800, 9, 64] * 6, 8, 2, 900),
+    ([40] * 66, [1100] * 66, 4, 1, 64),
+])
+def test_attention_of_many_sequences_within_a_window(tokens, before, Hq, Hkv, window):
+    """More than 64 sequences, whose plan a kernel of its own makes, with windows:
+    each tile's own positions are its ranges."""
+    say("attention8 many, window", tokens[:3], len(tokens), window)
+    rng = np.random.default_rng(len(tokens) + window)
+    bt = Batch8(rng, tokens, before, 16, Hkv, pad=3)
+    for b, p in enumerate(before):  # pages that no row sees were given back
+        bt.table[b, :max(0, p - window + 1) // 16] = -1
+    q, canary = f16(rng, (bt.T, Hq, 128), 1.5), f16(rng, (bt.T, Hq, 128))
+    got = attend(bt, q, window, dev(canary))
+    assert np.array_equal(got[-3:], canary[-3:])
+    assert np.array_equal(got.view(np.uint16), attend(bt, q, window, dev(canary)).view(np.uint16))
+    rows = list(OS.rows(bt.start, bt.lens))
+    picked = rows if len(rows) <= 200 else [rows[i] for i in sorted(rng.choice(len(rows), 200, replace=False))]
+    check_picked(bt, Hq, q, got, picked, window)
 
 
 # ---------------------------------------------------------------------------
