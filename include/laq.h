@@ -665,9 +665,10 @@ int64_t laq_paged_attention_e4m3_workspace_bytes(int64_t B, int64_t T, int64_t H
 /* laq_paged_attention_e4m3 -- laq_paged_attention_f16 over a cache of 8 bits:
  * the attention over the values that its codes stand for, which are fp16
  * numbers, so that nothing is rounded on reading them.  Probabilities of
- * sequences with at most 16 / (Hq / Hkv) rows keep 22 bits (two fp16 numbers
- * whose sum has them) whatever else the batch holds; those of longer chunks as
- * for laq_paged_attention_f16.
+ * sequences with at most 16 / (Hq / Hkv) rows are each the sum of two fp16
+ * numbers, whatever else the batch holds: 22 bits, cut off, of those down to
+ * 2^-11 of the row's largest, and of smaller ones what is above 2^-32 of it;
+ * those of longer chunks as for laq_paged_attention_f16.
  *   workspace  as there, of laq_paged_attention_e4m3_workspace_bytes.
  * Errors: as laq_paged_attention_f16's (strides of the pages: MISALIGNED unless
  * multiples of 16); NULL_POINTER also for the scales. */

@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256) void paged_append_codes_kernel(PagedCodes pb, 
 // is the order in which the second product takes the probabilities as its
 // columns, if the values' operand has the same positions.  That comes from the
 // transposing LDS reads: 16 lanes read eight positions x 16 dimensions and
-// receive a dimension's eight codes each.  The probabilities keep 22 bits: each
+// receive a dimension's eight codes each.  The probabilities keep up to 22 bits: each
 // is the sum of two fp16 numbers, and each value product two instructions.
 // Piece p (16 bytes) of key row r sits at p ^ (r / 2 & 7) and of value row r at
 // p ^ (r / 2 & 3 | r / 16 << 2): the operand reads touch each bank once.
@@ -443,8 +443,11 @@ __device__ __forceinline__ void CacheE4M3::rows16_item(const PagedCodes& pb, con
   };
 
   // A probability is 2^(score - ref); ref lies 8 below the maximum when it is
-  // set and follows once that has grown by 7 more, so that both fp16 parts of a
-  // probability (below 2^15) are normal numbers down to 2^-11 of the largest.
+  // set and follows once that has grown by 7 more, so that it is below 2^15 and the
+  // largest so far 2^8 or more.  Its second part, cut off like the first, has steps
+  // of 2^-21 of the probability, but none below 2^-24 (fp16's least): 22 bits down
+  // to 2^-3, 2^-11 of the largest, and an error below 2^-32 of the largest from
+  // there on.
   constexpr float kBelow = 8.0f, kLag = 15.0f;
   float ref = kNoMax, l = 0.0f;
   float4_t o[8];

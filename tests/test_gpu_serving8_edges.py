@@ -263,6 +263,50 @@ def test_attention_of_many_sequences_within_a_window(tokens, before, Hq, Hkv, wi
     check_picked(bt, Hq, q, got, picked, window)
 
 
+@pytest.mark.parametrize("beside", [False, True])
+def test_attention_of_few_rows_cuts_small_probabilities_off(beside):
+    """Probabilities of a sequence of up to 16 query rows are cut off at 22 bits, or
+    at 2^-32 of the largest where that is more.
+
+    Every 32nd position has the score that all others are some 2^-10 to 2^-20 of, and
+    values of 0.  The others' values are A and -A with one score for each sign, so
+    that what is cut off adds up.  Scores are one product each (exact) times a
+    constant in 32 bits, less a reference, and an exponential: four roundings of
+    the exponent's size (2^-24 of it) and two of the result; sums of L positions in
+    32 bits: L x 2^-24 of the magnitudes; the output's rounding 2^-11."""
+    say("few rows8, small probabilities", beside)
+    rng = np.random.default_rng(77)
+    n, L = 48, 64
+    tokens, before = [1] * n + [900] * beside, [L - 1] * n + [40] * beside  # (900: the kernel of chunks)
+    bt = Batch8(rng, tokens, before, 16, 1)
+    bt.kc[:], bt.vc[:] = 0, 0
+    bt.ks[:], bt.vs[:] = 127, 134
+    q = f16(rng, (bt.T, 1, 128))
+    for b in range(n):
+        sign = rng.permutation(np.resize([0, 1], L))
+        for t in range(L):
+            at = bt.table[b, t // 16], 0, t % 16
+            bt.kc[at][0] = 0x40 if t % 32 == 0 else 0  # 2
+            bt.kc[at][1] = 0x38 if t % 32 and sign[t] else 0  # 1
+            bt.vc[at] = 0 if t % 32 == 0 else 0xFE if sign[t] else 0x7E  # 57344 or less
+        q[b, 0] = 0
+        q[b, 0, 0] = (10 + 10 * b / n) * np.log(2) * 128**0.5 / 2
+        q[b, 0, 1] = rng.uniform(-0.2, 0.2)
+    bt.values()
+    got = attend(bt, q).astype(np.float64)
+    for b in range(n):
+        t = np.arange(L)
+        K, V = (c[bt.table[b, t // 16], 0, t % 16].astype(np.float64) for c in (bt.k, bt.v))
+        s = K @ q[b, 0].astype(np.float64) / 128**0.5
+        p = np.exp(s - s.max())
+        den, V = p.sum(), V[:, 0]
+        ref = p @ V / den
+        moved = 4 * 2.0**-24 * np.abs(s).max() + 2 * 2.0**-24 + 2 * L * 2.0**-24
+        cut = (np.maximum(2.0**-21 * p, 2.0**-32) @ np.abs(V)) / den
+        tol = 2.0**-11 * abs(ref) + 2 * moved * (p @ np.abs(V)) / den + cut + 2.0**-25
+        assert (np.abs(got[b, 0] - ref) <= tol).all(), (b, float(np.abs(got[b, 0] - ref).max()), tol)
+
+
 # ---------------------------------------------------------------------------
 # logits before sampling
 # ---------------------------------------------------------------------------
