@@ -835,7 +835,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
 
 // Joins the ranges of the split tiles in position order.  Records are weighted
 // by 2^(their maximum - the largest of all); a lane holds two dimensions.
-// WAVES == 4: a block takes a row at a time (every gridDim.y-th of its tile), its
+// WAVES == 4: a block takes a row (ONE) or every gridDim.y-th of its tile, its
 // waves every fourth record, and they meet in LDS (decoding: few rows, many
 // ranges).  WAVES == 1: a wave per kJoinRows rows, four times that a block at a
 // time (a chunk's rows have few ranges each).  Most blocks
@@ -848,7 +848,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_attention_chunk_kernel(ty
 // 61.2 -> 62.7; 1024 rows at 0, 32:8, 41 -> 36 -> 34 -> 38; 512 at 2000, 64:8, 72 ->
 // 68 -> 65 -> 68.  Twice the blocks: 63.0, 34.7 and 64.9.)
 constexpr int kJoinRows = 2;
-template <int BM, bool TILE, int WAVES>
+template <int BM, bool TILE, int WAVES, bool ONE>
 __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb, int R, int Hkv, int window, Out o_) {
   __shared__ float2_t part[4][64];
   constexpr int kRec = BM * (kHeadDim + 2);
@@ -920,11 +920,14 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
     if constexpr (WAVES == 4) {
       part[w][lane] = num[0];
       __syncthreads();
+      if (ONE && w > 0) return;
       num[0] = part[0][lane];
 #pragma unroll
       for (int i = 1; i < 4; ++i) num[0] += part[i][lane];
-      __syncthreads();  // the next row's sums take their place
-      if (w > 0) continue;
+      if constexpr (!ONE) {
+        __syncthreads();  // the next row's sums take their place
+        if (w > 0) continue;
+      }
     }
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
@@ -934,6 +937,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedBatch pb
       *reinterpret_cast<half2_t*>(o_.out + ((int64_t)(it.s0 + r / R) * o_.Hq + g * R + r % R) * kHeadDim + 2 * lane) =
           half2_t{(_Float16)(num[k][0] * inv), (_Float16)(num[k][1] * inv)};
     }
+    if constexpr (ONE) return;  // (known before: a loop's code costs a row 1.6 to 3 us more)
   }
 }
 
@@ -1007,9 +1011,9 @@ void launch_chunks(const typename C::Batch& pb, const uint16_t* q, int64_t R, in
          (int)R, (int)Hkv, (int)window, o);
   if (join.x == 0) return;
   if (by_group)
-    launch((paged_attention_join_kernel<BM, C::kTileRanges, 1>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
+    launch((paged_attention_join_kernel<BM, C::kTileRanges, 1, false>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
   else
-    launch((paged_attention_join_kernel<BM, C::kTileRanges, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
+    launch((paged_attention_join_kernel<BM, C::kTileRanges, 4, true>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
 }
 
 template <class C>
@@ -1035,11 +1039,13 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
   const Out o{out, ws, plan, (int)Hq, (int)p.records, p.min_chunk};
   const dim3 grid((unsigned)(p.items * Hkv));
   // A block joins one row; 4 kJoinRows where the tiles (most of them not split)
-  // would make many blocks.  (Tiles of 128 rows, calls measured on MI355X, by row ->
-  // by 8: 5 tiles of up to 3 ranges 18.5 -> 17.4 us, of up to 9, 19.8 -> 20.5, of up
-  // to 17, 21.9 -> 25.1, of up to 65, 28.4 -> 42.7; 9 of up to 25, 30.7 -> 33.1.  The
-  // joining alone, by row -> by 16: 16 of up to 25, 8.8 -> 14.2, of up to 3, 7.7 ->
-  // 4.5; 32 of up to 9, 13.0 -> 7.0.)
+  // would make many blocks.  (Calls measured on MI355X, 8:1 heads, by row -> by 8.
+  // Tiles of 128 rows over codes: 9 of up to 3 ranges 19.1 -> 18.1 us, of up to 9, 20.8
+  // -> 21.4, of up to 65, 33.1 -> 44.3; 16 of up to 9, 23.4 -> 22.8, of up to 17, 29.5
+  // -> 31.7; 32 of up to 17, 35.9 -> 33.6.  Tiles of 256 over fp16: 8 of up to 9, 26.5
+  // -> 25.8, of up to 65, 50.5 -> 59.3; 16 of up to 9, 33.1 -> 29.5; 32 of up to 9, 49.7
+  // -> 40.0; 64 of up to 65, 197 -> 174: their border of 32 is above where the two
+  // meet, and stays, as they add ranges up in unlike orders.)
   constexpr int64_t kJoinBlocks = 2048;
   const int64_t few_tiles = p.rows != kChunkRows<4> ? 32 : p.most_ranges >= 16 ? 16 : 8;
   const bool many = p.rows != kSmallRows && p.split_tiles * Hkv > few_tiles;
@@ -1047,17 +1053,26 @@ hipError_t launch_attention(const typename C::Batch& pb, const uint16_t* q, int6
   const int64_t groups = (most_rows + 4 * kJoinRows - 1) / (4 * kJoinRows);
   const int64_t turns = (groups * (p.split_tiles * Hkv + 1) + kJoinBlocks - 1) / kJoinBlocks;
   const int64_t by_group = (groups + turns - 1) / turns;  // (as many turns for each)
-  // (A block per row where that is about as many as run at once, else fewer that
-  // go on: where nothing is split, each costs its search.  Measured on MI355X, 64
-  // sequences of 400 positions, 64:8 heads, e4m3 codes: 25 -> 19 us.)
-  const int64_t by_row = std::min(most_rows, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
+  // 16-row tiles: a block a row, or fewer blocks that go on where there would be more
+  // than run at once, unless rows fill at least half of up to twice as many: where a
+  // tile has fewer rows than 16, or is not split, each block costs its search.
+  // (Calls measured on MI355X, a block a row -> 2048 / tiles blocks a tile, decoding
+  // sequences of 2000 positions, fp16 caches: 64 of four rows a head 99 -> 93 us, 24
+  // 54.8 -> 52.7, 16 36.0 -> 35.6; of sixteen rows, 64 100.7 -> 94.2, 16 (half of the
+  // blocks have a row) 41.0 -> 42.6.)  Chunks' tiles, few where they are joined by
+  // rows: a block a row (of the same sizes, 200 rows at 900, 40:8 heads, 38.8 -> 42.0).
+  const int64_t slots = most_rows * p.split_tiles * Hkv;
+  const bool one = p.rows != kSmallRows || slots <= kJoinBlocks || (slots <= 2 * kJoinBlocks && 2 * pb.T * R * Hkv >= slots);
+  const int64_t by_row = one ? most_rows : std::min(most_rows, std::max<int64_t>(1, kJoinBlocks / (p.split_tiles * Hkv + 1)));
   const dim3 join((unsigned)(p.split_tiles * Hkv), (unsigned)(many ? by_group : by_row));
   if (p.rows == kSmallRows) {
     launch((paged_attention_rows16_kernel<C>), grid, dim3(64 * kWaves), C::template kItemLds<kWaves>, stream, e1, pb, q,
            (int)R, (int)Hkv, (int)window, o);
-    if (p.split_tiles > 0)
-      launch((paged_attention_join_kernel<kSmallRows, C::kTileRanges, 4>), join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv,
-             (int)window, o);
+    if (p.split_tiles > 0) {
+      auto* const kernel = one ? paged_attention_join_kernel<kSmallRows, C::kTileRanges, 4, true>
+                               : paged_attention_join_kernel<kSmallRows, C::kTileRanges, 4, false>;
+      launch(kernel, join, dim3(256), 0, stream, e2, rows, (int)R, (int)Hkv, (int)window, o);
+    }
   } else if (p.rows == kChunkRows<8>) {
     launch_chunks<C, kChunkRows<8>>(pb, q, R, Hkv, window, o, grid, join, many, stream, e1, e2);
   } else if constexpr (C::kFourWaves) {

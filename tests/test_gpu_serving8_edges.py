@@ -9,7 +9,7 @@ import torch
 from oracle import serving as OS
 from oracle.compare import linear_check
 from paper_2605_08755_amd import decode, laq
-from test_gpu_serving import attention_check, dev, f16, say
+from test_gpu_serving import Batch, attention_check, dev, f16, say
 from test_gpu_serving8 import (DEV, EPS, Batch8, adjust_case, adjust_check, attend, half_step, host, small,
                                to_dev)
 
@@ -261,6 +261,32 @@ def test_attention_of_many_sequences_within_a_window(tokens, before, Hq, Hkv, wi
     rows = list(OS.rows(bt.start, bt.lens))
     picked = rows if len(rows) <= 200 else [rows[i] for i in sorted(rng.choice(len(rows), 200, replace=False))]
     check_picked(bt, Hq, q, got, picked, window)
+
+
+@pytest.mark.parametrize("codes", [True, False])
+@pytest.mark.parametrize("tokens,before,Hq,Hkv", [
+    ([1] * 60 + [1] * 4, [100] * 60 + [5000, 3001, 2500, 4000], 64, 8),
+    ([2] * 50 + [1, 2, 2], [70] * 50 + [4000, 4100, 1500], 64, 8),
+    ([1] * 90 + [1] * 3, [20 + i for i in range(90)] + [3000, 6000, 2222], 128, 8),
+    ([1] * 40, [50 * i for i in range(40)], 56, 8),
+])
+def test_attention_rows_joined_in_turns(tokens, before, Hq, Hkv, codes):
+    """Batches with more rows to join than blocks that run at once: a block joins
+    one row after another.  Over both types of cache."""
+    say("joined in turns", len(tokens), Hq, Hkv, codes)
+    rng = np.random.default_rng(len(tokens) + Hq)
+    R, T, B = Hq // Hkv, sum(tokens), len(tokens)
+    split_tiles = min(-(-512 // Hkv), (T * R + B * 15) // 16) * Hkv  # as many as can be split
+    assert 16 * split_tiles > 4096 and 2048 // (split_tiles + 1) < max(tokens) * R and T * R <= 16 * B
+    bt = (Batch8 if codes else Batch)(rng, tokens, before, 16, Hkv)
+    q, canary = f16(rng, (T, Hq, 128), 1.5), f16(rng, (T, Hq, 128))
+    if codes:
+        got = attend(bt, q, 0, dev(canary))
+    else:
+        got = laq.paged_attention(dev(q), *bt.device(), out=dev(canary))
+        torch.cuda.synchronize()
+        got = got.cpu().numpy()
+    check_picked(bt, Hq, q, got, list(OS.rows(bt.start, bt.lens)))
 
 
 @pytest.mark.parametrize("beside", [False, True])
