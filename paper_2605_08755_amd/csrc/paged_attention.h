@@ -62,8 +62,9 @@ __device__ __forceinline__ float row_max(float v) {
 }
 // The larger, NaN where one is: one instruction for three numbers, while fmaxf
 // first quiets each that may be a signalling NaN, as it holds a matrix product to
-// be.  (Measured on MI355X, two prompts of 8192 and 4001 rows, 32:8 heads, fp16
-// caches: 811 -> 793 us.)
+// be.  (Measured on MI355X, two prompts of 8192 and 4001 rows, 32:8 heads, both
+// ways in turn in two runs: fp16 caches 757 -> 751 and 758 -> 750 us, codes 721 ->
+// 707 and 721 -> 708.)
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 // Inclusive prefix sum over the 64 lanes: shifts by 1, 2, 4, 8 within each
 // 16-lane row (lanes shifted in read 0), then the rows' totals.
@@ -406,7 +407,11 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 // where the reference ref only follows the maximum once that has grown by more
 // than 2^7: so they stay below 2^15 and full precision reaches down to 2^-22
 // of the largest, and the value sums are rarely rescaled.  The denominator is
-// the fp32 sum of the unrounded ones.
+// the fp32 sum of the unrounded ones.  (As two fp16 numbers each, with twice the
+// value products, outputs are as near to 64-bit ones as those of fp32
+// probabilities: two prompts of 8192 and 4001 rows over codes, 0.000135 of their
+// norm instead of 0.000151, where the rounding of the output alone makes most of
+// either; they then take 877 us instead of 707, over fp16 caches 988 instead of 751.)
 // A sequence of up to 16 rows (decoding rows beside a chunk, or of a batch with
 // much padding) would fill half a wave's rows: the block takes its items as the
 // 16-row kernel does, with its probabilities and all waves along the positions.
@@ -416,14 +421,14 @@ __device__ __forceinline__ uint32_t number_codes(uint32_t x) { return x & ~((nan
 //
 // What bounds it: the issue of matrix and vector instructions by two waves a
 // SIMD that do little of the one while the other does the other.  (Counters of
-// two prompts of 8192 and 4001 rows, 32:8 heads, on MI355X: matrix instructions
-// 42 % of the SIMDs' cycles, vector instructions 48 %; LDS active 27 % of the
-// compute units' cycles, no bank conflicts.  Kernel alone, without the joining:
-// 874 us, 780 TFLOP/s, the median of 24 calls under a kernel trace, 823 the
-// shortest, before the maxima were single instructions; a call with the joining
-// 750 to 793, 859 to 908 TFLOP/s, untraced, 705 to 730 over codes; a library's
-// fp16 8192^3 product reaches 1150.  As two blocks of 128 rows, with
-// twice the staging instructions, 945.  With 128 rows a tile took a wave
+// two prompts of 8192 and 4001 rows, 32:8 heads, on MI355X, fp16 caches and codes:
+// matrix instructions 43 and 41 % of the SIMDs' cycles, vector instructions 43 and
+// 51 %; LDS active 27 and 31 % of the compute units' cycles.  Kernel alone, without
+// the joining, under a kernel trace: 788 and 728 us, the medians of 24 calls, 761
+// and 706 the shortest; a call with the joining, untraced, 751 and 707, 907 and 963
+// TFLOP/s; a library's fp16 8192^3 product reaches 1150.  Earlier, fp16, where the
+// kernel alone took 874: as two blocks of 128 rows, with
+// twice the staging instructions, 945; with 128 rows a tile took a wave
 // about 5000 cycles: 1400 to 2100 its scores, 240 the maximum, 700 the
 // exponentials, 850 the value sums, 1100 issuing the next tile's loads and
 // stores.  Not faster: the two waves of a SIMD kept a phase apart, the operands

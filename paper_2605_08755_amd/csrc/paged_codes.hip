@@ -638,10 +638,10 @@ __device__ __forceinline__ void CacheE4M3::rows16_item(const PagedCodes& pb, con
 // its search; one whose rows begin many blocks takes them one after another).
 // Waves of a row's query heads: one where rows alone fill the chip, else one per
 // group of eight.  (Measured on MI355X, kernel alone, windows of 1 / 2 / 4 / 8 /
-// 16 rows: 16 decoding rows, 32:8 heads, 4.3 / 6.1 / 9.9 / 17.5 / 32 us; 1617
-// rows of nine sequences, 28:4, 13.6 / 10.7 / 11.0 / 14.4 / 13.9; 16384 of four,
-// 32:8, 225 / 221 / 132 / 98 / 79, of which 72 are the bytes as a large copy
-// moves them.)
+// 16 rows: 16 decoding rows, 32:8 heads, 4.4 / 6.3 / 9.9 / 17.2 / 32 us; 1659
+// rows of nine sequences and 21 of none, 28:4, 13.6 / 10.4 / 10.8 / 14.6 / 13.9;
+// 16384 of four, 32:8, 224 / 221 / 132 / 97 / 78, of which 72 are the bytes as a
+// large copy moves them.)
 struct AppendShape {
   int64_t window, q_waves, kv_waves, waves;
 };

@@ -762,8 +762,9 @@ def adjust_logits(logits, history=None, history_len=None, prompt_len=None, repet
     history int32 [rows][room] (rows may be strided or one expanded): the tokens
     so far, of which history_len int32 [rows] are there and the first prompt_len
     int32 [rows] (None: none) the prompt's.  repetition, frequency, presence
-    fp32 [rows] or None.  bias_token int32 and bias_value fp32 [rows][n]: added
-    to listed tokens (-1: none).  mask int32 [rows][(V + 31) // 32]: bit v % 32
+    fp32 [rows] or None.  bias_token int32 and bias_value fp32 [rows][n], of one
+    stride between rows (both expanded, or neither): added to listed tokens (-1:
+    none).  mask int32 [rows][(V + 31) // 32]: bit v % 32
     of word v // 32 is set for tokens that may be drawn (one row may be expanded
     to all)."""
     t = _torch()
